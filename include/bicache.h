@@ -339,9 +339,107 @@ int32_t bicache_depth_from_similarity(const float* sim, int32_t num_layers, floa
 int32_t bicache_build_depth_table(const int32_t* ratio_idx, const int32_t* depth, int32_t n,
                                   int32_t num_layers, int32_t* table_out);
 
+/* ---- Token eviction: a stored prefix reduced to the tokens that are attended to --------------------
+ * The store evicts whole prefixes (FIFO).  These calls shorten one: the attention weight that its tokens
+ * receive is accumulated over requests, layers or steps (bicache_prefix_weights, next to
+ * bicache_attend, whose log-sum-exps it takes), the tokens to keep are chosen
+ * (bicache_select_tokens) and copied into a shorter prefix inside the store (bicache_compact_prefix),
+ * which the attention calls then read like any other.  Keys keep the rotary positions they were stored
+ * with.  The paper has no counterpart: it keeps prefixes whole.
+ *
+ * These calls and the rotary calls below upload nothing and keep nothing between calls, so they can be
+ * captured into a CUDA graph without a run before it (the graph holds the page lists: it is valid as long
+ * as the prefixes it names are live).  They run on the context's device whichever device is current. */
+
+/* Attention weight received by every cached token of the prefixes of a ragged batch, one layer:
+ *   out[j][t] = decay * in[j][t] + sum over rows a of the prefix's requests and query heads h of KV head j of
+ *               exp(softmax_scale * q[a][h] . k[t][j] - lse[a][h]).
+ * prefix_id, row_off, seqlen, q, q_row_stride: as for bicache_attend (ids contiguous, -1: the request is
+ * passed over).  lse: device fp32 [rows][Hq] (dense), natural log, as bicache_attend writes it: over the
+ * cached keys AND the request's own, so that the weights are those of the attention itself.  A row whose
+ * lse is +inf or -inf adds nothing (padding rows, rows without keys); a NaN spreads.
+ * scores_out: device fp32; the block of request i's prefix starts score_off[i] elements after it and holds
+ * [Hkv][m] with score_head_stride (>= m) elements between KV heads.  The requests of one prefix name the same
+ * offset; blocks of different prefixes must not overlap.  scores_in: the same layout, read if decay is not
+ * 0 (may be scores_out itself, else must not overlap it; NULL allowed only with decay 0).  A prefix whose
+ * requests are all empty gets decay * in.  Elements of other tokens are left as they are.
+ * Sums in fp32 with the rounding error carried along (bf16, head_dim 128) or in fp64, in a fixed order: the
+ * same call gives the same bits.  Uses the context's workspace as scratch.  Errors as for bicache_attend;
+ * INVALID also for decay or softmax_scale that is not finite. */
+int32_t bicache_prefix_weights(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
+                               const int64_t* row_off, const int32_t* seqlen, const void* q, int64_t q_row_stride,
+                               const float* lse, const float* scores_in, float* scores_out,
+                               const int64_t* score_off, int64_t score_head_stride, float decay,
+                               float softmax_scale, void* stream);
+
+/* The `keep` tokens of each of `rows` rows of scores (device fp32 [rows][n], score_row_stride elements between
+ * rows) that stay: the first protect_first and the last protect_last of them always, then the largest
+ * scores, equal scores by lower index; a NaN ranks as -inf, -0 equals +0.  idx_out: device int32 [rows][keep]
+ * (idx_row_stride elements between rows), ascending.  Protected ends longer than the row are cut to it.
+ * INVALID for keep outside 0 .. n, for fewer than the protected tokens, for bad strides or null pointers.
+ * rows, n and keep may be 0 (nothing is written). */
+int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const float* scores,
+                              int64_t score_row_stride, int32_t keep, int32_t protect_first, int32_t protect_last,
+                              int32_t* idx_out, int64_t idx_row_stride, void* stream);
+
+/* Fill the layers first_layer .. first_layer + num_layers - 1 of prefix dst_id (allocated by
+ * bicache_reserve_prefix*, or any other live prefix) from prefix src_id: token i of KV head j becomes token
+ * idx[(layer - first_layer) * idx_layer_stride + j * idx_head_stride + i] of the source, K and V, for
+ * every i below keep, which is the destination's length.  idx: device int32; a stride of 0 gives all layers or all heads one
+ * list; any order, repeats allowed.  Bit-exact copies; unused slots of the last page become zero.  An index
+ * outside 0 .. (source length - 1) gives a zero token and makes bicache_device_status report INVALID until
+ * it is cleared.  NOTFOUND for an unknown or evicted id; INVALID for src_id == dst_id, a keep that is not
+ * the destination's length, layers that either prefix does not own, negative strides. */
+int32_t bicache_compact_prefix(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_t first_layer,
+                               int32_t num_layers, int32_t keep, const int32_t* idx, int64_t idx_layer_stride,
+                               int64_t idx_head_stride, void* stream);
+
+/* ---- Rotary positions ------------------------------------------------------------------------------
+ * Q and K arrive position-encoded at the attention calls; these calls encode them.  Pair i of a row at
+ * position p turns by the angle p * inv_freq[i]; the angle is taken modulo whole turns in 64-bit fixed point,
+ * so far positions lose nothing.  inv_freq: HOST array of rot_dim / 2 doubles, from
+ * bicache_rope_frequencies or the model's own. */
+enum {
+  BICACHE_ROPE_NONE = 0,    /* base^(-2 i / rot_dim)                                                       */
+  BICACHE_ROPE_LINEAR = 1,  /* the same divided by `factor` (positions interpolated)                       */
+  BICACHE_ROPE_NTK = 2,     /* base * factor^(rot_dim / (rot_dim - 2)) as the base                         */
+  BICACHE_ROPE_YARN = 3,    /* divided by `factor` for slow pairs, kept for fast ones; between the pairs that
+                               turn high_turns and low_turns times over original_length the share of
+                               interpolation is linear in the pair's index                                */
+  BICACHE_ROPE_BANDS = 4    /* the same, linear in the number of turns over original_length               */
+};
+
+/* inv_freq[0 .. rot_dim / 2 - 1] (host) for one of the rules above.  factor is not read by NONE;
+ * original_length, low_turns and high_turns are read by YARN and BANDS only.  No context, no device work.
+ * INVALID for an odd or non-positive rot_dim or one above 256, a base that is not above 1, factor not above
+ * 0, original_length < 1 or not 0 < low_turns < high_turns where they are read. */
+int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                 int32_t original_length, double low_turns, double high_turns, double* inv_freq);
+
+/* Rotate `rows` rows of queries and of keys:  (a, b) -> attention_scale * (a cos - b sin, b cos + a sin)
+ * for every pair of the first rot_dim dims of every head, the other dims unchanged; in fp32, one rounding.
+ * interleaved 0: pair i is dims (i, i + rot_dim / 2) (what bicache_project_prefix_layer_rope rotates); 1: dims
+ * (2 i, 2 i + 1).  inverse != 0 undoes the rotation: angles negated, 1 / attention_scale.
+ * Row r has position positions[r] (device int32) or, with positions NULL, position0 + r.
+ * q, q_out: device [rows][Hq][D] of the context's dtype, k, k_out [rows][Hkv][D]; row strides in elements.
+ * A tensor may be rotated in place (the same pointer and stride); other overlap is not allowed.  q or k may be
+ * NULL together with its output (that tensor is left out).  INVALID for an odd rot_dim or one outside 2 .. D,
+ * frequencies or attention_scale that are not finite, attention_scale 0, bad pointers or strides. */
+int32_t bicache_rope(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
+                     int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale,
+                     const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride,
+                     const void* k, int64_t k_row_stride, void* k_out, int64_t k_out_row_stride, void* stream);
+
+/* The cosines and sines themselves, times attention_scale: table device fp32 [rows][rot_dim / 2][2], the
+ * layout bicache_project_prefix_layer_rope takes (with rot_dim 128).  rot_dim up to 256; other arguments
+ * and errors as for bicache_rope. */
+int32_t bicache_rope_table(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0,
+                           int32_t rot_dim, const double* inv_freq, float attention_scale, float* table,
+                           void* stream);
+
 /* Synchronises `stream` and returns the sticky device status: OK, or TIMEOUT if a kernel gave up
- * on a bounded wait (its outputs are then undefined), or CUDA for a runtime error.  `clear` != 0
- * resets the word. */
+ * on a bounded wait (its outputs are then undefined), INVALID if bicache_compact_prefix met an index
+ * outside its source, or CUDA for a runtime error.  `clear` != 0 resets the word. */
 int32_t bicache_device_status(bicache_ctx* ctx, void* stream, int32_t clear);
 
 /* Budget, in SM clock cycles, of every device-side wait of the tensor-core kernel (on a barrier that a

@@ -40,7 +40,11 @@ Parity status of each function (what pins it, see tests/test_oracle_*.py):
                    pair preserved, inner products depend on the position
                    difference only).  The paper names no position encoding: the
                    angles are an input.
+  token_ops        (a module of its own) pinned: scalar loops, hand-written ties
+                   and protected ends, quarter turns, rotation by a difference of
+                   positions, frequencies at the ends of each rule.
 """
+from . import token_ops  # noqa: F401
 from .bicache_oracle import (  # noqa: F401
     OracleError,
     InvalidArgument,

@@ -24,6 +24,9 @@
 #include "project_kv.cuh"
 #include "tc_attention_pair.cuh"
 #include "tc_decode.cuh"
+#include "evict.cuh"
+#include "rope.cuh"
+#include "tc_weights.cuh"
 
 using namespace bicache;
 
@@ -834,6 +837,8 @@ int run_attention(bicache_ctx* ctx, int kind, int32_t layer, int32_t R, const in
 
 }  // namespace
 
+#include "token_ops_host.cuh"
+
 extern "C" {
 
 size_t bicache_pool_bytes(const bicache_config* cfg) {
@@ -936,6 +941,11 @@ int32_t bicache_create(const bicache_config* cfg, bicache_ctx** out) {
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, cfg->device) == cudaSuccess && sms > 0)
     ctx->sm_count = sms;
   if (cudaMemset(ws, 0, kStatusBytes) != cudaSuccess) {
+    destroy_host_resources(ctx);
+    delete ctx;
+    return BICACHE_ERR_CUDA;
+  }
+  if (configure_token_ops(tensor_ok) != cudaSuccess) {
     destroy_host_resources(ctx);
     delete ctx;
     return BICACHE_ERR_CUDA;
@@ -1621,6 +1631,7 @@ int32_t bicache_device_status(bicache_ctx* ctx, void* stream, int32_t clear) {
   if (clear && word != 0) cudaMemset(ctx->d_status, 0, kStatusBytes);
   if (word == kDevOk) return BICACHE_OK;
   if (word == kDevTimeout) return fail(ctx, BICACHE_ERR_TIMEOUT, "device-side wait gave up");
+  if (word == kDevBadIndex) return fail(ctx, BICACHE_ERR_INVALID, "compact_prefix met a token index outside its source");
   return fail(ctx, BICACHE_ERR_CUDA, "a kernel reported an internal error");
 }
 

@@ -91,5 +91,6 @@ __host__ __device__ inline long long pool_slice_offset(const PoolView& p, int la
 constexpr int kDevOk = 0;
 constexpr int kDevTimeout = 5;
 constexpr int kDevInternal = 6;   // a kernel found its own launch state wrong (shared-memory alignment)
+constexpr int kDevBadIndex = 7;   // a compaction met a token index outside the prefix
 
 }  // namespace bicache
