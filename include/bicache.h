@@ -424,7 +424,7 @@ int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, 
  * q, q_out: device [rows][Hq][D] of the context's dtype, k, k_out [rows][Hkv][D]; row strides in elements.
  * A tensor may be rotated in place (the same pointer and stride); other overlap is not allowed.  q or k may be
  * NULL together with its output (that tensor is left out).  INVALID for an odd rot_dim or one outside 2 .. D,
- * frequencies or attention_scale that are not finite, attention_scale 0, bad pointers or strides. */
+ * frequencies that are not finite or beyond +-2^20, attention_scale not finite or 0, bad pointers or strides. */
 int32_t bicache_rope(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
                      int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale,
                      const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride,

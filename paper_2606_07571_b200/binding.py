@@ -5,6 +5,7 @@ buffers and streams.  A missing or unloadable library raises at first use: there
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 
@@ -127,10 +128,9 @@ def load_library():
     lib.bicache_attend_full_static.restype = C.c_int32
     lib.bicache_attend_full_static.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp,
                                                C.c_int64, C.c_int64, vp, C.c_int64, C.c_float, vp]
-    f64p = C.POINTER(C.c_double)
     lib.bicache_prefix_weights.restype = C.c_int32
-    lib.bicache_prefix_weights.argtypes = [vp, C.c_int32, C.c_int32, i32p, i64p, i32p, vp, C.c_int64, vp, vp, vp, i64p,
-                                           C.c_int64, C.c_float, C.c_float, vp]
+    lib.bicache_prefix_weights.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_int64, vp, vp, vp, vp, C.c_int64,
+                                           C.c_float, C.c_float, vp]
     lib.bicache_select_tokens.restype = C.c_int32
     lib.bicache_select_tokens.argtypes = [vp, C.c_int64, C.c_int32, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp,
                                           C.c_int64, vp]
@@ -139,12 +139,12 @@ def load_library():
                                            C.c_int64, vp]
     lib.bicache_rope_frequencies.restype = C.c_int32
     lib.bicache_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, C.c_double,
-                                             C.c_double, f64p]
+                                             C.c_double, vp]
     lib.bicache_rope.restype = C.c_int32
-    lib.bicache_rope.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, f64p, C.c_float,
+    lib.bicache_rope.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, C.c_float,
                                  vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp]
     lib.bicache_rope_table.restype = C.c_int32
-    lib.bicache_rope_table.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, f64p, C.c_float, vp, vp]
+    lib.bicache_rope_table.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, vp, C.c_float, vp, vp]
     lib.bicache_device_status.restype = C.c_int32
     lib.bicache_device_status.argtypes = [vp, vp, C.c_int32]
     lib.bicache_hash_tokens.restype = C.c_uint64
@@ -173,9 +173,22 @@ def _i64(a):
     return a, a.ctypes.data_as(C.POINTER(C.c_int64))
 
 
-def _f64(a):
-    a = np.ascontiguousarray(a, dtype=np.float64)
-    return a, a.ctypes.data_as(C.POINTER(C.c_double))
+_TYPE_CODES = {"i": np.int32, "q": np.int64, "d": np.float64}
+
+
+def _host(a, code):
+    """A host array argument as (what keeps it alive, its address, its length).  The calls of a single small
+    launch are bound by the host: a list through array.array costs a tenth of a numpy conversion."""
+    if isinstance(a, np.ndarray):
+        a = np.ascontiguousarray(a, dtype=_TYPE_CODES[code])
+        return a, a.ctypes.data, a.size
+    a = array.array(code, a)
+    address, n = a.buffer_info()
+    return a, address, n
+
+
+# torch.cuda.current_stream builds a Stream object (2 us); the bare handle is what the library takes
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _dtype_code(dtype):
@@ -414,11 +427,12 @@ class BiCache:
     # -- token eviction -----------------------------------------------------------------------
     def _on_stream(self):
         """The current stream of the context's device, whichever device is current."""
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+        if _raw_stream is not None:
+            return _raw_stream(self.device.index)
+        return torch.cuda.current_stream(self.device).cuda_stream
 
-    def _own(self, *tensors, dtype=None):
-        for t in tensors:
-            assert t.is_cuda and t.device == self.device and (dtype is None or t.dtype == dtype)
+    def _own(self, t, dtype):
+        assert t.device == self.device and t.dtype == dtype, "a %s tensor on %s is needed" % (dtype, self.device)
 
     def prefix_weights(self, layer, prefix_id, row_off, seqlen, q, lse, scores_out, score_off, scores_in=None,
                        decay=0.0, scale=None):
@@ -426,90 +440,98 @@ class BiCache:
         scores_out = decay * scores_in + weights.  q [rows, Hq, D], lse [rows, Hq] as attend takes and writes
         them; scores_out (and scores_in) float32 [..., Hkv, m_max], contiguous; score_off: per request, the
         element offset of its prefix's [Hkv, m_max] block, of which the first m columns are used."""
-        pid, ppid = _i32(prefix_id)
-        off, poff = _i64(row_off)
-        n, pn = _i32(seqlen)
-        so, pso = _i64(score_off)
-        assert len(pid) == len(off) == len(n) == len(so)
-        self._own(q, dtype=self.dtype)
-        assert q.dim() == 3 and q.shape[1:] == (self.Hq, self.D) and q.stride(2) == 1 and q.stride(1) == self.D
-        self._own(lse, scores_out, dtype=torch.float32)
-        assert lse.is_contiguous() and lse.shape == (q.shape[0], self.Hq)
-        assert scores_out.dim() >= 2 and scores_out.shape[-2] == self.Hkv and scores_out.is_contiguous()
-        if scores_in is not None:
-            self._own(scores_in, dtype=torch.float32)
-            assert scores_in.shape == scores_out.shape and scores_in.is_contiguous()
-        assert n.size == 0 or (off + n).max() <= q.shape[0], "a request's rows reach past q"
+        pid, ppid, count = _host(prefix_id, "i")
+        off, poff, n_off = _host(row_off, "q")
+        n, pn, n_len = _host(seqlen, "i")
+        so, pso, n_so = _host(score_off, "q")
+        assert count == n_off == n_len == n_so
+        self._own(q, self.dtype)
+        self._own(lse, torch.float32)
+        self._own(scores_out, torch.float32)
+        rows, hq, d = q.shape
+        assert hq == self.Hq and d == self.D and q.stride(2) == 1 and q.stride(1) == d
+        assert lse.is_contiguous() and lse.shape == (rows, hq)
         m_max = scores_out.shape[-1]
-        assert so.size == 0 or so.max() + self.Hkv * m_max <= scores_out.numel(), "a score block reaches past the tensor"
-        scale = self.D ** -0.5 if scale is None else scale
-        st = self.lib.bicache_prefix_weights(self.ctx, layer, len(n), ppid, poff, pn, q.data_ptr(), q.stride(0),
-                                             lse.data_ptr(), scores_in.data_ptr() if scores_in is not None else None,
-                                             scores_out.data_ptr(), pso, m_max, C.c_float(decay),
-                                             C.c_float(scale), self._on_stream())
+        assert scores_out.is_contiguous() and scores_out.shape[-2] == self.Hkv
+        pin = None
+        if scores_in is not None:
+            self._own(scores_in, torch.float32)
+            assert scores_in.shape == scores_out.shape and scores_in.is_contiguous()
+            pin = scores_in.data_ptr()
+        if count:
+            assert max(map(int.__add__, off, n) if isinstance(off, array.array) and isinstance(n, array.array)
+                       else np.add(off, n)) <= rows, "a request's rows reach past q"
+            blocks = so if min(pid) >= 0 else [o for o, p in zip(so, pid) if p >= 0] or [-self.Hkv * m_max]
+            assert max(blocks) + self.Hkv * m_max <= scores_out.numel(), "a score block reaches past the tensor"
+        st = self.lib.bicache_prefix_weights(self.ctx, layer, count, ppid, poff, pn, q.data_ptr(), q.stride(0),
+                                             lse.data_ptr(), pin, scores_out.data_ptr(), pso, m_max, decay,
+                                             d ** -0.5 if scale is None else scale, self._on_stream())
         self._check(st, "bicache_prefix_weights")
 
     def select_tokens(self, scores, keep, idx_out, protect_first=0, protect_last=0):
         """The `keep` tokens of every row of scores [rows, n] that stay, as ascending indices into idx_out
         [rows, keep] (int32): protected ends, then largest scores, ties to the lower index."""
-        self._own(scores, dtype=torch.float32)
-        self._own(idx_out, dtype=torch.int32)
-        assert scores.dim() == 2 and idx_out.dim() == 2 and idx_out.shape == (scores.shape[0], keep)
-        assert (scores.stride(1) == 1 or scores.shape[1] <= 1) and (idx_out.stride(1) == 1 or keep <= 1)
-        st = self.lib.bicache_select_tokens(self.ctx, scores.shape[0], scores.shape[1], scores.data_ptr(),
-                                            scores.stride(0), keep, protect_first, protect_last, idx_out.data_ptr(),
-                                            idx_out.stride(0), self._on_stream())
+        self._own(scores, torch.float32)
+        self._own(idx_out, torch.int32)
+        rows, n = scores.shape
+        assert idx_out.shape == (rows, keep)
+        assert (scores.stride(1) == 1 or n <= 1) and (idx_out.stride(1) == 1 or keep <= 1)
+        st = self.lib.bicache_select_tokens(self.ctx, rows, n, scores.data_ptr(), scores.stride(0), keep, protect_first,
+                                            protect_last, idx_out.data_ptr(), idx_out.stride(0), self._on_stream())
         self._check(st, "bicache_select_tokens")
 
     def compact_prefix(self, src_id, dst_id, idx, first_layer=0):
         """Layers first_layer .. of prefix dst_id from the tokens idx [layers, Hkv, keep] (int32) of prefix
         src_id, keep = the length of dst_id; idx [layers, 1, keep] gives all heads one list."""
-        self._own(idx, dtype=torch.int32)
-        assert idx.dim() == 3 and idx.shape[1] in (1, self.Hkv) and (idx.stride(2) == 1 or idx.shape[2] == 1)
-        st = self.lib.bicache_compact_prefix(self.ctx, src_id, dst_id, first_layer, idx.shape[0], idx.shape[2],
-                                             idx.data_ptr(), idx.stride(0), idx.stride(1) if idx.shape[1] > 1 else 0,
-                                             self._on_stream())
+        self._own(idx, torch.int32)
+        layers, heads, keep = idx.shape
+        assert heads in (1, self.Hkv) and (idx.stride(2) == 1 or keep == 1)
+        st = self.lib.bicache_compact_prefix(self.ctx, src_id, dst_id, first_layer, layers, keep, idx.data_ptr(),
+                                             idx.stride(0), idx.stride(1) if heads > 1 else 0, self._on_stream())
         self._check(st, "bicache_compact_prefix")
 
     # -- rotary positions ---------------------------------------------------------------------
     def _positions(self, positions, rows):
         if positions is None:
             return None
-        self._own(positions, dtype=torch.int32)
+        self._own(positions, torch.int32)
         assert positions.shape == (rows,) and (rows <= 1 or positions.is_contiguous())
         return positions.data_ptr()
+
+    def _rope_pair(self, x, y, heads):
+        """Pointers and strides of a tensor and its rotated form."""
+        if x is None:
+            assert y is None
+            return None, 0, None, 0
+        self._own(x, self.dtype)
+        self._own(y, self.dtype)
+        sx, h, d = x.stride()
+        sy, hy, dy = y.stride()
+        assert x.shape == y.shape and x.shape[1] == heads and x.shape[2] == self.D
+        assert h == hy == self.D and d == dy == 1
+        return x.data_ptr(), sx, y.data_ptr(), sy
 
     def rope(self, inv_freq, q, q_out, k=None, k_out=None, positions=None, position0=0, interleaved=False,
              attention_scale=1.0, inverse=False):
         """Rotate q [rows, Hq, D] into q_out and k [rows, Hkv, D] into k_out (each may be its own output; either
         pair may be None).  inv_freq: host array of rot_dim / 2 frequencies (rope_frequencies); positions:
         int32 [rows], or None for position0, position0 + 1, ..."""
-        f, pf = _f64(inv_freq)
-        rows, args = None, []
-        for x, y, heads in ((q, q_out, self.Hq), (k, k_out, self.Hkv)):
-            assert (x is None) == (y is None)
-            if x is None:
-                args += [None, 0, None, 0]
-                continue
-            self._own(x, y, dtype=self.dtype)
-            assert x.shape == y.shape and x.shape[1:] == (heads, self.D) and rows in (None, x.shape[0])
-            assert x.stride()[1:] == (self.D, 1) and y.stride()[1:] == (self.D, 1)
-            rows = x.shape[0]
-            args += [x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0)]
-        rows = rows or 0
-        st = self.lib.bicache_rope(self.ctx, rows, self._positions(positions, rows), position0, 2 * len(f),
-                                   1 if interleaved else 0, 1 if inverse else 0, pf, C.c_float(attention_scale), *args,
-                                   self._on_stream())
+        f, pf, pairs = _host(inv_freq, "d")
+        rows = (k if q is None else q).shape[0]
+        assert q is None or k is None or k.shape[0] == rows
+        st = self.lib.bicache_rope(self.ctx, rows, self._positions(positions, rows), position0, 2 * pairs,
+                                   interleaved, inverse, pf, attention_scale, *self._rope_pair(q, q_out, self.Hq),
+                                   *self._rope_pair(k, k_out, self.Hkv), self._on_stream())
         self._check(st, "bicache_rope")
 
     def rope_table(self, inv_freq, table, positions=None, position0=0, attention_scale=1.0):
         """The cosines and sines as project_prefix_layer takes them: table float32 [rows, len(inv_freq), 2]."""
-        f, pf = _f64(inv_freq)
-        self._own(table, dtype=torch.float32)
-        assert table.dim() == 3 and table.shape[1:] == (len(f), 2) and table.is_contiguous()
-        st = self.lib.bicache_rope_table(self.ctx, table.shape[0], self._positions(positions, table.shape[0]), position0,
-                                         2 * len(f), pf, C.c_float(attention_scale), table.data_ptr(),
-                                         self._on_stream())
+        f, pf, pairs = _host(inv_freq, "d")
+        self._own(table, torch.float32)
+        rows = table.shape[0]
+        assert table.shape == (rows, pairs, 2) and table.is_contiguous()
+        st = self.lib.bicache_rope_table(self.ctx, rows, self._positions(positions, rows), position0, 2 * pairs, pf,
+                                         attention_scale, table.data_ptr(), self._on_stream())
         self._check(st, "bicache_rope_table")
 
     def device_status(self, clear=False):
@@ -583,7 +605,7 @@ def rope_frequencies(rot_dim, base, scaling="none", factor=1.0, original_length=
         raise BiCacheError(ERR_INVALID, "bicache_rope_frequencies", "unknown scaling %r" % (scaling,))
     out = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
     st = lib.bicache_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_length, low_turns,
-                                      high_turns, out.ctypes.data_as(C.POINTER(C.c_double)))
+                                      high_turns, out.ctypes.data)
     if st != OK:
         raise BiCacheError(st, "bicache_rope_frequencies")
     return out

@@ -43,16 +43,16 @@ __device__ __forceinline__ float2 rope_cos_sin(const RopeAngles& a, long long po
 }
 
 // ---------------------------------------------------------------------------------------------
-// The table [rows][pairs][2] of bicache_rope_table: one thread per pair.
+// The table [rows][pairs][2] of bicache_rope_table.  A thread keeps its pair and walks down the rows.
 // ---------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kRopeThreads)
 rope_table_kernel(const __grid_constant__ RopeAngles a, long long rows, float2* __restrict__ table) {
-  const long long total = rows * a.pairs;
-  for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < total;
-       i += (long long)gridDim.x * blockDim.x) {
-    const long long row = i / a.pairs;
+  const int per_block = kRopeThreads / a.pairs;                  // rows a block handles at a time
+  const int r = (int)threadIdx.x / a.pairs, pair = (int)threadIdx.x - r * a.pairs;
+  if (r >= per_block) return;
+  for (long long row = (long long)blockIdx.x * per_block + r; row < rows; row += (long long)gridDim.x * per_block) {
     const long long pos = a.positions ? (long long)a.positions[row] : a.position0 + row;
-    table[i] = rope_cos_sin(a, pos, (int)(i - row * a.pairs));
+    table[row * a.pairs + pair] = rope_cos_sin(a, pos, pair);
   }
 }
 
@@ -84,9 +84,99 @@ template <> __device__ __forceinline__ uint4 rope_pack<__nv_bfloat16>(const floa
 }
 
 // ---------------------------------------------------------------------------------------------
-// Rows, simplest form: one thread per pair (and per dim beyond the rotated ones), element by element.
-// Serves every rotated width.  A block takes one row at a time; its cosines and sines are computed once
-// and shared by the row's heads.
+// Rows in 16-byte chunks, for rotated widths that fill whole chunks (half-split pairs: rot_dim / 2 a multiple of
+// the chunk, interleaved pairs: rot_dim).  Bound by memory: every chunk is read and written once.
+// A block takes kRows rows and computes their cosines and sines once for all heads.  A thread owns a unit - the
+// two chunks of one head whose dims pair up (half-split), one chunk (interleaved), or one chunk beyond the
+// rotated dims, which is copied - and does it for all the block's rows, so the index arithmetic is paid
+// once and kRows x 2 chunks are in flight; the first unit's loads are issued before the cosines and sines.
+// These lie in shared memory chunk by chunk, two pairs to 16 bytes, the units of a head side by side:
+// the lanes of a quarter warp read different banks.
+// ---------------------------------------------------------------------------------------------
+template <typename T, bool kInterleaved, int kRows>
+__global__ void __launch_bounds__(kRopeThreads)
+rope_chunks_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ RopeRows r) {
+  using Tr = ElemTraits<T>;
+  constexpr int kPer = Tr::kPerChunk;
+  constexpr int kPairs = kInterleaved ? kPer / 2 : kPer;           // pairs of a unit
+  __shared__ float4 cs[kRows][kRopeMaxPairs / 2];
+  const int turned = a.pairs / kPairs;                             // units of a head that rotate
+  const int first_rest = 2 * a.pairs / kPer;                       // first chunk beyond the rotated dims
+  const int rest = r.in_place ? 0 : r.head_bytes / 16 - first_rest;
+  const int per_head = turned + rest, units = per_head * (r.t[0].heads + r.t[1].heads);
+  const long long row0 = (long long)blockIdx.x * kRows;
+  const int rows = (int)min((long long)kRows, r.rows - row0);
+
+  uint4 x[kRows], y[kRows];
+  const char* in = nullptr;
+  char* out = nullptr;
+  long long in_stride = 0, out_stride = 0;
+  int c = 0;                                                       // unit of the head
+  auto load = [&](int u) {
+    int h = u / per_head;
+    c = u - h * per_head;
+    const int which = h >= r.t[0].heads ? 1 : 0;
+    const RopeTensor& t = r.t[which];
+    h -= which ? r.t[0].heads : 0;
+    const int chunk = c < turned ? c : first_rest + c - turned;
+    const long long off = (long long)h * r.head_bytes + chunk * 16;
+    in_stride = t.in_stride;
+    out_stride = t.out_stride;
+    in = t.in + row0 * in_stride + off;
+    out = t.out + row0 * out_stride + off;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      if (i < rows) {
+        x[i] = *reinterpret_cast<const uint4*>(in + i * in_stride);
+        if (!kInterleaved && c < turned) y[i] = *reinterpret_cast<const uint4*>(in + i * in_stride + turned * 16);
+      }
+  };
+  int u = threadIdx.x;
+  if (u < units) load(u);
+  for (int i = threadIdx.x; i < rows * a.pairs; i += blockDim.x) {
+    const int row = i / a.pairs, pair = i - row * a.pairs;
+    const long long pos = a.positions ? (long long)a.positions[row0 + row] : a.position0 + row0 + row;
+    const int unit = pair / kPairs, e = pair - unit * kPairs;
+    reinterpret_cast<float2*>(&cs[row][(e >> 1) * turned + unit])[e & 1] = rope_cos_sin(a, pos, pair);
+  }
+  __syncthreads();
+  for (; u < units; u += blockDim.x) {
+    if (u >= (int)blockDim.x) load(u);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      if (i >= rows) break;
+      if (c < turned) {
+        float p[kPer], q[kPer];
+        Tr::unpack(x[i], p);
+        if (!kInterleaved) Tr::unpack(y[i], q);
+#pragma unroll
+        for (int e = 0; e < kPairs; e += 2) {
+          const float4 w = cs[i][(e >> 1) * turned + c];
+          if (kInterleaved) {
+            const float p0 = p[2 * e], p1 = p[2 * e + 1], p2 = p[2 * e + 2], p3 = p[2 * e + 3];
+            p[2 * e] = p0 * w.x - p1 * w.y;
+            p[2 * e + 1] = p1 * w.x + p0 * w.y;
+            p[2 * e + 2] = p2 * w.z - p3 * w.w;
+            p[2 * e + 3] = p3 * w.z + p2 * w.w;
+          } else {
+            const float p0 = p[e], p1 = p[e + 1];
+            p[e] = p0 * w.x - q[e] * w.y;
+            q[e] = q[e] * w.x + p0 * w.y;
+            p[e + 1] = p1 * w.z - q[e + 1] * w.w;
+            q[e + 1] = q[e + 1] * w.z + p1 * w.w;
+          }
+        }
+        x[i] = rope_pack<T>(p);
+        if (!kInterleaved) *reinterpret_cast<uint4*>(out + i * out_stride + turned * 16) = rope_pack<T>(q);
+      }
+      *reinterpret_cast<uint4*>(out + i * out_stride) = x[i];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows, any rotated width: one thread per pair (and per dim beyond the rotated ones), element by element.
+// A block takes one row at a time.
 // ---------------------------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads)
@@ -122,6 +212,33 @@ rope_rows_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ R
       }
     }
   }
+}
+
+// Four rows to a block once that still gives every SM two blocks (it quarters the index arithmetic and the loads
+// in flight are what hides the latency); one row to a block below that.
+template <typename T>
+cudaError_t launch_rope(const RopeAngles& a, const RopeRows& r, bool interleaved, int sm_count, cudaStream_t stream) {
+  constexpr int kPer = ElemTraits<T>::kPerChunk;
+  if ((interleaved ? 2 * a.pairs : a.pairs) % kPer == 0) {
+    const int turned = a.pairs / (interleaved ? kPer / 2 : kPer);
+    const int rest = r.in_place ? 0 : (r.head_bytes / 16 - 2 * a.pairs / kPer);
+    const int units = (turned + rest) * (r.t[0].heads + r.t[1].heads);
+    const int threads = units >= kRopeThreads ? kRopeThreads : (units < 64 ? 64 : (units + 31) / 32 * 32);
+    const bool four = r.rows >= 8LL * sm_count;
+    const long long blocks = four ? (r.rows + 3) / 4 : r.rows;
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    if (interleaved) {
+      if (four) rope_chunks_kernel<T, true, 4><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      else rope_chunks_kernel<T, true, 1><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+    } else {
+      if (four) rope_chunks_kernel<T, false, 4><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      else rope_chunks_kernel<T, false, 1><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+    }
+  } else {
+    const long long blocks = r.rows < 16LL * sm_count ? r.rows : 16LL * sm_count;
+    rope_rows_kernel<T><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
+  }
+  return cudaGetLastError();
 }
 
 }  // namespace bicache

@@ -52,7 +52,7 @@ struct Item {
   int tile_begin, tile_end, rows;         // row tiles; packed rows of the group
   int split, g;
 };
-__device__ __forceinline__ Item read_item(const WeightArgs& a, const ParamList& list, int index) {
+__device__ __forceinline__ Item read_item(const WeightArgs& a, const int* list, int index) {
   Item it;
   it.g = weight_group_of(a, list, index);
   const WeightGroup& g = weight_group(list, it.g);
@@ -88,10 +88,12 @@ struct Sum2 {
 
 }  // namespace wts
 
+template <int kWords>
 __global__ void __launch_bounds__(wts::kWtsThreads, 1)
-tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ ParamList list, int* status,
+tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ ParamList<kWords> params, int* status,
                   long long wait_cycles) {
   using namespace wts;
+  const int* const list = params.w;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Sync* sy = reinterpret_cast<Sync*>(smem + (kKSlots + kQSlots) * kTileBytes);
@@ -275,7 +277,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
         if (lane < npages)
           bulk_copy_g2s(k_ring + slot * kTileBytes + lane * kPageBytes,
-                        a.pool_k + ((long long)list.w[g.page_word + (it.key0 + k0) / kPageSize + lane] * a.Hkv + it.hk) * kPageBytes,
+                        a.pool_k + ((long long)list[g.page_word + (it.key0 + k0) / kPageSize + lane] * a.Hkv + it.hk) * kPageBytes,
                         kPageBytes, full);
         if (lane == 0)
           mbar_arrive_expect_tx(full, (unsigned)(npages * kPageBytes));
@@ -359,14 +361,19 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 }
 
 inline cudaError_t configure_tc_weights() {
-  return cudaFuncSetAttribute(tc_weights_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wts::kSmemBytes);
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsSmall>, attr, wts::kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsMid>, attr, wts::kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWords>, attr, wts::kSmemBytes);
+  return e;
 }
 
-inline cudaError_t launch_tc_weights(const WeightArgs& a, const ParamList& list, int* status, int sm_count,
-                                     long long wait_cycles, cudaStream_t stream) {
+template <int kWords>
+cudaError_t launch_tc_weights(const WeightArgs& a, const ParamList<kWords>& list, int* status, int sm_count,
+                              long long wait_cycles, cudaStream_t stream) {
   if (a.num_items <= 0) return cudaSuccess;
   const int grid = a.num_items < sm_count ? a.num_items : sm_count;
-  tc_weights_kernel<<<grid, wts::kWtsThreads, wts::kSmemBytes, stream>>>(
+  tc_weights_kernel<kWords><<<grid, wts::kWtsThreads, wts::kSmemBytes, stream>>>(
       a, list, status, wait_cycles > 0 ? wait_cycles : tc::kWaitCycles);
   return cudaGetLastError();
 }

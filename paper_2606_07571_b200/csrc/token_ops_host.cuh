@@ -58,7 +58,7 @@ class WeightLaunches {
     g.m = std::min(e.m - g.key0, num_pages * kPageSize);
     back_ -= (num_pages + 1) & ~1;                       // keeps the row runs, which follow, 8-byte aligned
     g.page_word = back_;
-    std::memcpy(&list_.w[back_], pages.data() + page0, sizeof(int32_t) * num_pages);
+    std::memcpy(&list_[back_], pages.data() + page0, sizeof(int32_t) * num_pages);
     back_ -= num_segs * kSegWords;
     g.seg_word = back_;
     g.num_segs = num_segs;
@@ -66,11 +66,11 @@ class WeightLaunches {
     for (int i = 0; i < num_segs; ++i) {
       WeightSeg s = segs[i];
       s.token -= tok0;
-      std::memcpy(&list_.w[back_ + i * kSegWords], &s, sizeof(s));
+      std::memcpy(&list_[back_ + i * kSegWords], &s, sizeof(s));
     }
     g.tokens = tokens;
     g.score_off = score_off;
-    std::memcpy(&list_.w[groups_ * kGroupWords], &g, sizeof(g));
+    std::memcpy(&list_[groups_ * kGroupWords], &g, sizeof(g));
     ++groups_;
     return BICACHE_OK;
   }
@@ -84,7 +84,7 @@ class WeightLaunches {
     }
     const int G = a.Hq / a.Hkv;
     const int block_keys = tensor_ ? wts::kItemKeys : kWsKeys, tile_rows = tensor_ ? wts::kRowTile : kWsRows;
-    WeightGroup* g = reinterpret_cast<WeightGroup*>(list_.w);
+    WeightGroup* g = reinterpret_cast<WeightGroup*>(list_);
     int max_tiles = 1, max_m = 1;
     long long base_items = 0;
     for (int i = 0; i < groups_; ++i) {
@@ -132,25 +132,35 @@ class WeightLaunches {
     }
     a.num_groups = groups_;
     a.num_items = (int)item;
-    cudaError_t e;
-    if (tensor_) {
-      e = launch_tc_weights(a, list_, ctx_->d_status, ctx_->sm_count, ctx_->wait_cycles, stream_);
-    } else {
-      const size_t smem = weights_simt_smem(a.D);
-      if (ctx_->cfg.dtype == BICACHE_F32)
-        weights_simt_kernel<float><<<a.num_items, kWsThreads, smem, stream_>>>(a, list_);
-      else
-        weights_simt_kernel<__nv_bfloat16><<<a.num_items, kWsThreads, smem, stream_>>>(a, list_);
-      e = cudaGetLastError();
+    // the records from the end follow the groups: the list is as short as what it holds
+    const int gap = back_ - front();
+    for (int i = 0; i < groups_; ++i) {
+      g[i].page_word -= gap;
+      g[i].seg_word -= gap;
     }
-    ctx_->launches++;
-    if (e == cudaSuccess && split) {
-      const long long per_group = (long long)a.Hkv * max_m;
-      weights_sum_kernel<<<dim3((unsigned)std::min<long long>((per_group + 255) / 256, 4LL * ctx_->sm_count), groups_), 256, 0,
-                           stream_>>>(a, list_);
+    std::memmove(&list_[front()], &list_[back_], sizeof(int) * (kParamWords - back_));
+    cudaError_t e = cudaSuccess;
+    with_param_list(list_, kParamWords - gap, [&](const auto& list) {
+      constexpr int kWords = sizeof(list.w) / sizeof(int);
+      if (tensor_) {
+        e = launch_tc_weights(a, list, ctx_->d_status, ctx_->sm_count, ctx_->wait_cycles, stream_);
+      } else {
+        const size_t smem = weights_simt_smem(a.D);
+        if (ctx_->cfg.dtype == BICACHE_F32)
+          weights_simt_kernel<float, kWords><<<a.num_items, kWsThreads, smem, stream_>>>(a, list);
+        else
+          weights_simt_kernel<__nv_bfloat16, kWords><<<a.num_items, kWsThreads, smem, stream_>>>(a, list);
+        e = cudaGetLastError();
+      }
       ctx_->launches++;
-      e = cudaGetLastError();
-    }
+      if (e == cudaSuccess && split) {
+        const long long per_group = (long long)a.Hkv * max_m;
+        const unsigned blocks = (unsigned)std::min<long long>((per_group + 255) / 256, 4LL * ctx_->sm_count);
+        weights_sum_kernel<kWords><<<dim3(blocks, groups_), 256, 0, stream_>>>(a, list);
+        ctx_->launches++;
+        e = cudaGetLastError();
+      }
+    });
     groups_ = 0;
     back_ = kParamWords;
     return cuda_status(ctx_, e, "prefix_weights");
@@ -167,7 +177,7 @@ class WeightLaunches {
   bool tensor_, first_ = true;
   cudaStream_t stream_;
   int groups_ = 0, back_ = kParamWords;
-  ParamList list_;
+  alignas(8) int list_[kParamWords];
 };
 static_assert(kParamWords % 2 == 0 && kGroupWords % 2 == 0 && kSegWords % 2 == 0, "8-byte aligned records");
 // what one launch takes of a batch that does not fit: together less than the list
@@ -311,7 +321,7 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
   // one launch for all layers if they share page lists and places, else one per layer
   const bool together = src.uniform && dst.uniform && ctx->uniform_caps;
   const int step = together ? num_layers : 1;
-  ParamList list;
+  int list[kParamWords];
   for (int l = first_layer; l < first_layer + num_layers; l += step) {
     const std::vector<int32_t>&sp = pages_of(src, l), &dp = pages_of(dst, l);
     const int ns = (int)sp.size(), nd = (int)dp.size();
@@ -327,11 +337,13 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
         a.src_pages = std::min(s_step, ns - s0);
         a.dst_first = d0;
         a.dst_pages = std::min(d_step, nd - d0);
-        std::memcpy(list.w, sp.data() + s0, sizeof(int) * a.src_pages);
-        std::memcpy(list.w + a.src_pages, dp.data() + d0, sizeof(int) * a.dst_pages);
+        std::memcpy(list, sp.data() + s0, sizeof(int) * a.src_pages);
+        std::memcpy(list + a.src_pages, dp.data() + d0, sizeof(int) * a.dst_pages);
         const long long chunks = (long long)step * a.dst_pages * kPageSize * cfg.num_kv_heads * a.chunks_per_row;
         const int blocks = (int)std::min<long long>((chunks + kCompactThreads - 1) / kCompactThreads, (long long)ctx->sm_count * 16);
-        compact_prefix_kernel<<<blocks, kCompactThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, list);
+        with_param_list(list, a.src_pages + a.dst_pages, [&](const auto& params) {
+          compact_prefix_kernel<<<blocks, kCompactThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, params);
+        });
         ctx->launches++;
         const int st = cuda_status(ctx, cudaGetLastError(), "compact_prefix");
         if (st != BICACHE_OK) return st;
@@ -349,11 +361,14 @@ bool rope_angles(RopeAngles* a, int32_t rot_dim, const double* inv_freq, const i
   *a = RopeAngles();
   a->pairs = rot_dim / 2;
   for (int i = 0; i < a->pairs; ++i) {
-    if (!std::isfinite(inv_freq[i])) return false;
-    const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
-    long double part = turns - std::floor(turns);                 // whole turns per position change nothing
-    part = std::floor(part * 18446744073709551616.0L + 0.5L);
-    a->turn[i] = part >= 18446744073709551616.0L ? 0ull : (unsigned long long)part;
+    if (!(std::fabs(inv_freq[i]) <= 1048576.0)) return false;
+    // inv_freq / (2 pi) to 2^-64 and better: the product with the leading part of 1 / (2 pi) as a sum of two
+    // doubles, and the product with the rest of the constant
+    const double f = inv_freq[i], high = f * 0.15915494309189535;
+    const double low = std::fma(f, 0.15915494309189535, -high) + f * -9.839338337591243e-18;
+    const double part = high - std::floor(high);                  // whole turns per position change nothing
+    a->turn[i] = (part < 1.0 ? (unsigned long long)(part * 18446744073709551616.0) : 0ull) +
+                 (unsigned long long)(long long)std::nearbyint(low * 18446744073709551616.0);
   }
   a->positions = positions;
   a->position0 = position0;
@@ -375,7 +390,7 @@ int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t 
   if (!aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "misaligned positions");
   RopeAngles a;
   if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, inverse != 0))
-    return fail(ctx, BICACHE_ERR_INVALID, "frequencies and scale must be finite, the scale not 0");
+    return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
   RopeRows r = RopeRows();
   r.rows = rows;
   r.head_bytes = cfg.head_dim * ctx->esize;
@@ -407,13 +422,11 @@ int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t 
   if (rows == 0) return BICACHE_OK;
   DeviceGuard guard(cfg.device);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const int blocks = (int)std::min<int64_t>(rows, 16LL * ctx->sm_count);
-  if (cfg.dtype == BICACHE_F32)
-    rope_rows_kernel<float><<<blocks, kRopeThreads, 0, stream>>>(a, r, interleaved != 0);
-  else
-    rope_rows_kernel<__nv_bfloat16><<<blocks, kRopeThreads, 0, stream>>>(a, r, interleaved != 0);
+  const cudaError_t e = cfg.dtype == BICACHE_F32
+                            ? launch_rope<float>(a, r, interleaved != 0, ctx->sm_count, stream)
+                            : launch_rope<__nv_bfloat16>(a, r, interleaved != 0, ctx->sm_count, stream);
   ctx->launches++;
-  return cuda_status(ctx, cudaGetLastError(), "rope");
+  return cuda_status(ctx, e, "rope");
 }
 
 int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
@@ -426,22 +439,29 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
   if ((rows > 0 && !table) || !aligned16(table) || !aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "bad pointer");
   RopeAngles a;
   if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, false))
-    return fail(ctx, BICACHE_ERR_INVALID, "frequencies and scale must be finite, the scale not 0");
+    return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
   if (ctx->host_only) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "host-only context has no device path");
   if (rows == 0) return BICACHE_OK;
   DeviceGuard guard(ctx->cfg.device);
-  const long long total = (long long)rows * a.pairs;
-  const int blocks = (int)std::min<long long>((total + kRopeThreads - 1) / kRopeThreads, 16LL * ctx->sm_count);
+  const int per_block = kRopeThreads / a.pairs;
+  const int blocks = (int)std::min<long long>((rows + per_block - 1) / per_block, 8LL * ctx->sm_count);
   rope_table_kernel<<<blocks, kRopeThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, rows, reinterpret_cast<float2*>(table));
   ctx->launches++;
   return cuda_status(ctx, cudaGetLastError(), "rope_table");
 }
 
 cudaError_t configure_token_ops(bool tensor_ok) {
-  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
+  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4 + kSelStaged / 32 * 8);
   const int ws = (int)weights_simt_smem(kSimtMaxD);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, ws);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, ws);
+  auto simt = [&](auto words) {
+    constexpr int kWords = decltype(words)::value;
+    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<float, kWords>, attr, ws);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<__nv_bfloat16, kWords>, attr, ws);
+  };
+  simt(std::integral_constant<int, kParamWordsSmall>());
+  simt(std::integral_constant<int, kParamWordsMid>());
+  simt(std::integral_constant<int, kParamWords>());
   if (e == cudaSuccess && tensor_ok) e = configure_tc_weights();
   return e;
 }
@@ -485,9 +505,9 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
     a.n = n;
     a.keep = keep;
     DeviceGuard guard(ctx->cfg.device);
-    select_tokens_kernel<<<(unsigned)rows, kSelThreads, n <= kSelStaged ? (size_t)n * 4 : 0, static_cast<cudaStream_t>(stream)>>>(a);
+    const cudaError_t e = launch_select(a, rows, ctx->sm_count, static_cast<cudaStream_t>(stream));
     ctx->launches++;
-    return cuda_status(ctx, cudaGetLastError(), "select_tokens");
+    return cuda_status(ctx, e, "select_tokens");
   });
 }
 

@@ -122,7 +122,7 @@ def test_rope_refusals(lib, ctx):
     assert call() == b.ERR_UNSUPPORTED
     assert call(k=None, ko=None, pos=None) == b.ERR_UNSUPPORTED
     assert call(q=None, qo=None, rows=0) == b.ERR_UNSUPPORTED
-    for bad in (dict(rows=-1), dict(rot=0), dict(rot=7), dict(rot=130), dict(f=None), dict(f=(float("inf"),) * 64),
+    for bad in (dict(rows=-1), dict(rot=0), dict(rot=7), dict(rot=130), dict(f=None), dict(f=(float("inf"),) * 64), dict(f=(-2.0 ** 21,) * 64),
                 dict(scale=0.0), dict(scale=float("nan")), dict(pos=ODD), dict(q=None), dict(qo=None), dict(k=None),
                 dict(q=None, qo=None, k=None, ko=None), dict(q=A4), dict(ko=A4), dict(qs=504), dict(kos=255),
                 dict(qs=516), dict(qs=520), dict(c=None)):
