@@ -31,27 +31,29 @@ inline void with_param_list(const int* w, int used, F&& f) {
 
 // ---------------------------------------------------------------------------------------------
 // bicache_select_tokens: per row of scores the `keep` largest, protected ends first, ties to the lowest
-// index, as ascending indices.  Scores become unsigned integers in the same order; the keep-th largest is
-// found digit by digit (11 bits each, largest digit first, over the bits in which the row's scores differ
-// at all: narrow rows spread over the bins as wide ones do) until its bin holds few enough scores to be
-// ranked against one another.  Then every score becomes a bit "kept" (or, if only some of the scores equal to
-// the last one are kept, two bits), a scan over the words of bits gives each its place, and the indices are
-// put in order in shared memory and written out.
+// index, as ascending indices.  Scores become unsigned integers in the same order.  The keep-th largest is
+// found digit by digit: 11 bits each, largest digit first, over the bits in which the row's scores differ
+// at all (narrow rows spread over the bins as wide ones do); the scores of the first digit's bin are gathered, the
+// further digits touch these only, and once they are few they are ranked against one another.  Then every
+// thread takes a run of scores into registers, counts what stays, learns its place from a scan, and puts the indices
+// into a list that leaves in order.
 //
-// A row is served by a cluster of 1 to 8 blocks, each with a part of it, which read one another's counts through
-// distributed shared memory: several blocks make a few rows fast and let two blocks share an SM, so
-// that one loads while the other counts.  Scores are read from memory once, in 16-byte loads, and stay in shared
-// memory; a row too long for that is read again (from L2, as a rule) by every pass, by one block.
+// Scores are read from memory once, in 16-byte loads, and stay in shared memory: one block per row, and a
+// cluster of up to 8 blocks, which read one another's counts through distributed shared memory, for rows that one
+// block cannot hold.  (Clusters for shorter rows were slower, for few rows as for many: a cluster barrier costs
+// about 1 us.)  A row too long for that is read again, from L2 as a rule, by every pass.
 // The bound for many rows is the instructions per score (about 1 us for each, for 36 M scores), then memory.
 // ---------------------------------------------------------------------------------------------
-constexpr int kSelThreads = 512;
+constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelDigitBits = 11;
 constexpr int kSelBins = 1 << kSelDigitBits;
-constexpr int kSelRanked = 256;                 // a bin of at most this many scores is ranked directly
+constexpr int kSelGathered = kSelBins;          // scores of the first digit's bin that are kept apart
+constexpr int kSelRanked = 256;                 // at most so many are ranked directly
 constexpr int kSelStaged = 49152;               // scores of a block's part kept in shared memory (192 KB)
-constexpr int kSelWords = kSelStaged / 32;      // bit words kept at a time
+constexpr int kSelRunQuads = 5;                 // scores / 4 of a thread's run: odd, so that runs start on different banks
 constexpr int kSelMaxCluster = 8;
+static_assert(kSelBins == 2 * kSelThreads && kSelWarps == 32, "two bins to a thread, a warp over the warps' results");
 
 // NaN counts as -inf; -0 as +0; larger score <=> larger integer.  Never 0 nor 0xffffffff.
 __device__ __forceinline__ unsigned select_key(float x) {
@@ -78,11 +80,19 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  const int w = lane < kSelWarps ? warp_sums[lane] : 0;
+  const int w = warp_sums[lane];
   const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
   *total = __reduce_add_sync(0xffffffffu, w);
   __syncthreads();                              // warp_sums may be written again
   return before + incl - v;
+}
+
+// smallest v of the block.  One barrier; warp_mins may be written again after the next.
+__device__ __forceinline__ unsigned block_min(unsigned v, unsigned* warp_mins) {
+  v = __reduce_min_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0) warp_mins[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return __reduce_min_sync(0xffffffffu, warp_mins[threadIdx.x & 31]);
 }
 
 template <bool kStaged>
@@ -90,20 +100,19 @@ __global__ void __launch_bounds__(kSelThreads)
 select_tokens_kernel(SelectArgs a) {
   namespace cg = cooperative_groups;
   struct Shared {                               // what the cluster's blocks read of one another
-    int hist[2][kSelBins];                      // digits in turn
-    unsigned lo, hi;                            // smallest and largest competing score of the part
-    unsigned ranked[kSelRanked];                // scores of the last bin found in the part ...
-    int num_ranked;                             // ... and how many
+    int hist[2][kSelBins];                      // digits in turn; the second also holds the gathered scores at first
+    unsigned range[2][2];                       // smallest and largest competing score inside the range, in turn
+    int num_gathered;
     int above, equal;                           // kept for sure / tied, in the part
   };
   extern __shared__ __align__(16) unsigned staged[];
   __shared__ __align__(16) Shared sh;
-  __shared__ __align__(16) unsigned candidates[kSelRanked];
+  __shared__ __align__(16) unsigned gathered[kSelGathered];           // all parts' scores inside the range
   __shared__ int warp_sums[kSelWarps];
   __shared__ unsigned warp_lo[kSelWarps], warp_hi[kSelWarps];
   __shared__ int found_bin, found_above, found_count;
   __shared__ unsigned found_key;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
   const cg::cluster_group cluster = cg::this_cluster();
   const int parts = kStaged ? (int)cluster.num_blocks() : 1, part = kStaged ? (int)cluster.block_rank() : 0;
   auto sync_parts = [&]() {
@@ -113,14 +122,13 @@ select_tokens_kernel(SelectArgs a) {
   const long long row_index = blockIdx.x / parts;
   const float* __restrict__ row = a.scores + row_index * a.score_stride;
   int* out = a.idx + row_index * a.idx_stride;
-  const int n = a.n, free_begin = a.first, free_end = n - a.last;      // the tokens that compete
+  const int n = a.n;
   // The row starts `shift` scores past a 16-byte boundary.  Slot s holds token s - shift, so that 16-byte loads
   // and 16-byte shared-memory words line up; slots below `shift` and past the end are no tokens.
   const int shift = (int)((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
   const int slots = n + shift, quads = (slots + 3) >> 2;
-  // this block's part: whole words of 32 slots
-  const int all_words = (slots + 31) >> 5, part_words = (all_words + parts - 1) / parts;
-  const int quad_begin = min(quads, part * part_words * 8), quad_end = min(quads, quad_begin + part_words * 8);
+  const int part_quads = (quads + parts - 1) / parts;
+  const int quad_begin = min(quads, part * part_quads), quad_end = min(quads, quad_begin + part_quads);
   auto load_quad = [&](int v) {                                        // slots 4 v .. 4 v + 3, from memory
     float4 f;
     if (4 * v >= shift && 4 * v + 3 < slots) {
@@ -136,18 +144,24 @@ select_tokens_kernel(SelectArgs a) {
     return make_uint4(select_key(f.x), select_key(f.y), select_key(f.z), select_key(f.w));
   };
   auto quad_at = [&](int v) { return kStaged ? reinterpret_cast<const uint4*>(staged)[v - quad_begin] : load_quad(v); };
-  // competing slots; the quads that lie wholly inside take the short path
-  const int slot_begin = free_begin + shift, slot_end = free_end + shift;
-  auto inside = [&](int v) { return 4 * v >= slot_begin && 4 * v + 4 <= slot_end; };
-  auto competes = [&](int s) { return s >= slot_begin && s < slot_end; };
+  // The part's competing slots [slot_begin, slot_end): whole quads [qa, qb), and up to three slots on each side,
+  // one to a thread.
+  const int slot_begin = max(a.first + shift, quad_begin * 4), slot_end = min(n - a.last + shift, quad_end * 4);
+  const int qa = (slot_begin + 3) >> 2, qb = max(qa, slot_end >> 2);
+  int edge = -1;
+  if (tid < 4 && slot_begin + tid < min(qa * 4, slot_end)) edge = slot_begin + tid;
+  if (tid >= 4 && tid < 8 && slot_begin < slot_end && qb * 4 + tid - 4 < slot_end) edge = qb * 4 + tid - 4;
+  const unsigned edge_key = edge >= 0 ? select_key(row[edge - shift]) : 0u;
 
-  // behind the scores: the bit words
-  unsigned* const bits_above = staged + (kStaged ? part_words * 32 : 0);
-  unsigned* const bits_equal = bits_above + (kStaged ? part_words : kSelWords);
+  // a slot that does not compete is marked: protected tokens stay (largest key), other slots never do
+  auto marked = [&](uint4 q, int v) {
+    auto mark = [&](unsigned key, int s) {
+      return s >= slot_begin && s < slot_end ? key : (s >= shift && s < slots ? 0xffffffffu : 0u);
+    };
+    return make_uint4(mark(q.x, 4 * v), mark(q.y, 4 * v + 1), mark(q.z, 4 * v + 2), mark(q.w, 4 * v + 3));
+  };
 
-  for (int b = tid; b < 2 * kSelBins; b += kSelThreads) (&sh.hist[0][0])[b] = 0;
-  if (tid == 0) sh.num_ranked = 0;
-  unsigned lo = 0xffffffffu, hi = 0u;
+  unsigned lo = edge >= 0 ? edge_key : 0xffffffffu, hi = edge_key;
   constexpr int kAhead = 4;                                            // loads in flight per thread
   for (int v0 = quad_begin + tid; v0 < quad_end; v0 += kAhead * kSelThreads) {
     uint4 k[kAhead];
@@ -158,259 +172,283 @@ select_tokens_kernel(SelectArgs a) {
     for (int j = 0; j < kAhead; ++j) {
       const int v = v0 + j * kSelThreads;
       if (v >= quad_end) break;
-      if (kStaged) reinterpret_cast<uint4*>(staged)[v - quad_begin] = k[j];
-      if (inside(v)) {
+      const bool whole = v >= qa && v < qb;
+      if (kStaged) reinterpret_cast<uint4*>(staged)[v - quad_begin] = whole ? k[j] : marked(k[j], v);
+      if (whole) {
         lo = min(min(min(lo, k[j].x), k[j].y), min(k[j].z, k[j].w));
         hi = max(max(max(hi, k[j].x), k[j].y), max(k[j].z, k[j].w));
-      } else {
-        const unsigned e[4] = {k[j].x, k[j].y, k[j].z, k[j].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (competes(4 * v + i)) {
-            lo = min(lo, e[i]);
-            hi = max(hi, e[i]);
-          }
       }
     }
   }
-  lo = __reduce_min_sync(0xffffffffu, lo);
-  hi = __reduce_max_sync(0xffffffffu, hi);
-  if (lane == 0) {
-    warp_lo[warp] = lo;
-    warp_hi[warp] = hi;
-  }
-  __syncthreads();
-  lo = __reduce_min_sync(0xffffffffu, warp_lo[lane % kSelWarps]);
-  hi = __reduce_max_sync(0xffffffffu, warp_hi[lane % kSelWarps]);
+  reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);    // both digits: 4 * 1024 bins
+  if (tid == 0) sh.num_gathered = 0;
+  lo = block_min(lo, warp_lo);
+  hi = ~block_min(~hi, warp_hi);
   if (parts > 1) {
     if (tid == 0) {
-      sh.lo = lo;
-      sh.hi = hi;
+      sh.range[0][0] = lo;
+      sh.range[0][1] = hi;
     }
     cluster.sync();
-    for (int p = 0; p < parts; ++p) {
-      lo = min(lo, other(p)->lo);
-      hi = max(hi, other(p)->hi);
-    }
+    const Shared* o = other(lane % parts);                             // lane p asks part p: one trip for all
+    lo = __reduce_min_sync(0xffffffffu, o->range[0][0]);
+    hi = __reduce_max_sync(0xffffffffu, o->range[0][1]);
   }
 
-  // `threshold`: the k-th largest of the competing scores; `ties` of the `equals` scores equal to it are kept
-  int k = a.keep - a.first - a.last;
-  unsigned threshold = 0;                                              // below every key: all of them are kept
-  int ties = 0, equals = 0;
-  if (k <= 0) {
-    threshold = 0xffffffffu;
-  } else if (k < free_end - free_begin) {
-    unsigned base = lo, span = hi - lo;                                // the k-th largest is in [base, base + span]
-    int digit = max(0, (32 - __clz(span)) - kSelDigitBits);
-    for (int pass = 0;; ++pass) {
-      int* const hist = sh.hist[pass & 1];
-      for (int v = quad_begin + tid; v < quad_end; v += kSelThreads) {
-        const uint4 q = quad_at(v);
-        const unsigned d[4] = {q.x - base, q.y - base, q.z - base, q.w - base};   // below base: wraps to a large value
-        if (inside(v)) {
-          if (pass == 0) {                                             // all of them are inside the range
+  // The k-th largest of the competing scores is in [base, base + span], where `inside` of them are and it is the
+  // k-th from the top.  narrow(): the digit's histogram, summed over `among` parts, shortens the range.
+  int k = a.keep - a.first - a.last, inside = 0, pass = 0, digit = 0;
+  unsigned base = 0, span = 0;                                         // below every competing key: all are kept
+  auto narrow = [&](int among, int buffer) {
+    // counts from the top: thread t holds bins 2046 - 2 t and 2047 - 2 t
+    const int bin0 = kSelBins - 2 - 2 * tid;
+    int2 h = *reinterpret_cast<const int2*>(&sh.hist[buffer][bin0]);
+    int c0 = h.x, c1 = h.y;
+    if (among > 1) {
+      int2 g[kSelMaxCluster];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) atomicAdd(&hist[d[j] >> digit], 1);
-          } else if (min(min(d[0], d[1]), min(d[2], d[3])) <= span) {
+      for (int p = 0; p < kSelMaxCluster; ++p)
+        if (p < among && p != part) g[p] = *reinterpret_cast<const int2*>(&other(p)->hist[buffer][bin0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (d[j] <= span) atomicAdd(&hist[d[j] >> digit], 1);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (competes(4 * v + j) && d[j] <= span) atomicAdd(&hist[d[j] >> digit], 1);
+      for (int p = 0; p < kSelMaxCluster; ++p)
+        if (p < among && p != part) {
+          c0 += g[p].x;
+          c1 += g[p].y;
         }
-      }
-      sync_parts();
-      // every part has read the digit before this one: its bins are cleared for the next
-      for (int b = tid; b < kSelBins && pass > 0; b += kSelThreads) sh.hist[(pass + 1) & 1][b] = 0;
-      // counts from the top: thread t holds bins 2044 - 4 t .. 2047 - 4 t
-      const int bin0 = kSelBins - 4 - 4 * tid;
-      int c[4] = {0, 0, 0, 0};
-      for (int p = 0; p < parts; ++p) {
-        const int4 h = *reinterpret_cast<const int4*>(&other(p)->hist[pass & 1][bin0]);
-        c[0] += h.x;
-        c[1] += h.y;
-        c[2] += h.z;
-        c[3] += h.w;
-      }
-      int total;
-      int above = block_scan(c[0] + c[1] + c[2] + c[3], warp_sums, &total);
-#pragma unroll
-      for (int j = 3; j >= 0; --j) {
-        if (above < k && k <= above + c[j]) {
-          found_bin = bin0 + j;
-          found_above = above;
-          found_count = c[j];
-        }
-        above += c[j];
-      }
-      __syncthreads();
-      k -= found_above;
-      equals = found_count;
-      base += (unsigned)found_bin << digit;
-      span = min(span - ((unsigned)found_bin << digit), (1u << digit) - 1u);
-      if (digit == 0) {
-        threshold = base;
-        break;
-      }
-      if (equals <= kSelRanked) {
-        // gather the bin's scores of all parts and rank them against one another
-        for (int v = quad_begin + tid; v < quad_end; v += kSelThreads) {
-          const uint4 q = quad_at(v);
-          const unsigned e[4] = {q.x, q.y, q.z, q.w};
-          if (min(min(q.x - base, q.y - base), min(q.z - base, q.w - base)) <= span) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (e[j] - base <= span && competes(4 * v + j)) sh.ranked[atomicAdd(&sh.num_ranked, 1)] = e[j];
-          }
-        }
-        sync_parts();
-        for (int p = 0, at = 0; p < parts; ++p) {
-          const Shared* o = other(p);
-          const int m = o->num_ranked;
-          if (tid < m) candidates[at + tid] = o->ranked[tid];
-          at += m;
-        }
-        __syncthreads();
-        if (tid < equals) {
-          const unsigned mine = candidates[tid];
-          int greater = 0, same = 0;
-          for (int i = 0; i < equals; ++i) {
-            greater += candidates[i] > mine ? 1 : 0;
-            same += candidates[i] == mine ? 1 : 0;
-          }
-          if (greater < k && k <= greater + same) {                    // by every thread with that score, alike
-            found_key = mine;
-            found_above = greater;
-            found_count = same;
-          }
-        }
-        __syncthreads();
-        threshold = found_key;
-        k -= found_above;
-        equals = found_count;
-        break;
-      }
-      digit = max(0, digit - kSelDigitBits);
     }
-    ties = k;
-  }
-  const bool split = ties < equals;                                    // some of the equal scores stay, some go
-
-  // Ordered output, at most kSelWords words at a time (one round for a staged row).  A thread turns 8 slots into
-  // a byte.  Where ties are not split, "above" is all that is kept.
-  int above_before = 0, equal_before = 0;                              // earlier rounds
-  for (int round = quad_begin; round < quad_end || (parts > 1 && round == quad_begin); round += kSelWords * 8) {
-    const int words = min(kSelWords, (quad_end - round + 7) >> 3);
-    const int word_slot = round * 4;                                   // first slot of the round
-    for (int byte = tid; byte < words * 4; byte += kSelThreads) {
-      unsigned above = 0, equal = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int v = round + byte * 2 + i;
-        if (v >= quad_end) break;
-        const uint4 q = quad_at(v);
-        const unsigned e[4] = {q.x, q.y, q.z, q.w};
-        if (inside(v)) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            above |= e[j] > threshold ? 1u << (4 * i + j) : 0u;
-            equal |= e[j] == threshold ? 1u << (4 * i + j) : 0u;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int s = 4 * v + j;
-            const bool held = s >= shift && s < slots && !competes(s);          // a protected token
-            above |= held || (competes(s) && e[j] > threshold) ? 1u << (4 * i + j) : 0u;
-            equal |= competes(s) && e[j] == threshold ? 1u << (4 * i + j) : 0u;
-          }
-        }
-      }
-      reinterpret_cast<unsigned char*>(bits_above)[byte] = (unsigned char)(split ? above : above | equal);
-      if (split) reinterpret_cast<unsigned char*>(bits_equal)[byte] = (unsigned char)equal;
+    int total;
+    const int above1 = block_scan(c0 + c1, warp_sums, &total), above0 = above1 + c1;
+    const bool in1 = above1 < k && k <= above0, in0 = above0 < k && k <= above0 + c0;
+    if (in0 || in1) {
+      found_bin = in1 ? bin0 + 1 : bin0;
+      found_above = in1 ? above1 : above0;
+      found_count = in1 ? c1 : c0;
     }
     __syncthreads();
-    // every thread takes a run of words: where the run starts, then token by token
-    const int run = (words + kSelThreads - 1) / kSelThreads;
-    const int w0 = min(words, tid * run), w1 = min(words, w0 + run);
+    k -= found_above;
+    inside = found_count;
+    base += (unsigned)found_bin << digit;
+    span = min(span - ((unsigned)found_bin << digit), (1u << digit) - 1u);
+    digit = max(0, digit - kSelDigitBits);
+  };
+  // f(score) for every competing score inside the range
+  auto each_inside = [&](auto&& f) {
+#pragma unroll 2
+    for (int v = qa + tid; v < qb; v += kSelThreads) {
+      const uint4 q = quad_at(v);
+      const unsigned d[4] = {q.x - base, q.y - base, q.z - base, q.w - base};   // below base: wraps to a large value
+      if (min(min(d[0], d[1]), min(d[2], d[3])) <= span) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (d[j] <= span) f(d[j] + base);
+      }
+    }
+    if (edge >= 0 && edge_key - base <= span) f(edge_key);
+  };
+  if (k <= 0) {
+    base = 0xffffffffu;
+    k = 0;
+  } else if (k < n - a.first - a.last) {
+    base = lo;
+    span = hi - lo;
+    digit = max(0, (32 - __clz(span)) - kSelDigitBits);
+#pragma unroll 2
+    for (int v = qa + tid; v < qb; v += kSelThreads) {                 // every score is inside the range
+      const uint4 q = quad_at(v);
+      atomicAdd(&sh.hist[0][(q.x - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.y - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.z - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.w - base) >> digit], 1);
+    }
+    if (edge >= 0) atomicAdd(&sh.hist[0][(edge_key - base) >> digit], 1);
+    sync_parts();
+    narrow(parts, 0);
+    // A bin of many scores is often one of many equal ones: their smallest and largest say so, and else where
+    // the next digit begins.  A bin too full to be gathered takes further digits over the whole row.
+    while (span > 0 && inside > k && inside > kSelRanked) {
+      ++pass;
+      unsigned least = 0xffffffffu, most = 0u;
+      each_inside([&](unsigned e) {
+        least = min(least, e);
+        most = max(most, e);
+      });
+      least = block_min(least, warp_lo);
+      most = ~block_min(~most, warp_hi);
+      if (parts > 1) {
+        if (tid == 0) {
+          sh.range[pass & 1][0] = least;
+          sh.range[pass & 1][1] = most;
+        }
+        cluster.sync();
+        const Shared* o = other(lane % parts);
+        least = __reduce_min_sync(0xffffffffu, o->range[pass & 1][0]);
+        most = __reduce_max_sync(0xffffffffu, o->range[pass & 1][1]);
+      }
+      base = least;
+      span = most - least;
+      digit = max(0, (32 - __clz(span)) - kSelDigitBits);
+      if (span == 0 || inside <= kSelGathered) break;
+      each_inside([&](unsigned e) { atomicAdd(&sh.hist[pass & 1][(e - base) >> digit], 1); });
+      sync_parts();
+      // every part has read the digit before this one: its bins are cleared for the next
+      reinterpret_cast<int2*>(sh.hist[(pass + 1) & 1])[tid] = make_int2(0, 0);
+      narrow(parts, pass & 1);
+    }
+    if (span > 0 && inside > k) {
+      // gather the scores inside; from here on every part of the cluster does the same work on the same list
+      const int lists = (pass + 1) & 1, bins = pass & 1;               // one digit's bins hold the part's list
+      unsigned* const mine = reinterpret_cast<unsigned*>(sh.hist[lists]);
+      each_inside([&](unsigned e) { mine[atomicAdd(&sh.num_gathered, 1)] = e; });
+      if (parts == 1 && tid < 4 && inside + tid < kSelGathered) mine[inside + tid] = 0u;      // read in fours below
+      sync_parts();
+      unsigned* list = mine;
+      if (parts > 1) {
+        const int theirs = lane < parts ? other(lane)->num_gathered : 0;
+        for (int i = tid; i < kSelGathered; i += kSelThreads) {        // thread i takes the i-th of all parts' scores
+          int from = -1, at = i;
+#pragma unroll
+          for (int p = 0; p < kSelMaxCluster; ++p) {
+            const int m = __shfl_sync(0xffffffffu, theirs, p);
+            if (from < 0 && at < m) from = p;
+            if (from < 0) at -= m;
+          }
+          gathered[i] = from >= 0 ? (unsigned)other(from)->hist[lists][at] : 0u;       // past the end: below any score
+        }
+        list = gathered;
+        __syncthreads();
+      }
+      const int all = inside;
+      while (span > 0 && inside > k) {
+        if (all <= kSelRanked) {
+          if (tid < all) {
+            const unsigned key = list[tid];
+            int greater = 0, same = 0;
+            for (int i = 0; i < all; i += 4) {
+              const uint4 c = *reinterpret_cast<const uint4*>(&list[i]);
+              greater += (c.x > key) + (c.y > key) + (c.z > key) + (c.w > key);
+              same += (c.x == key) + (c.y == key) + (c.z == key) + (c.w == key);
+            }
+            if (greater < k && k <= greater + same) {                  // by every thread with that score, alike
+              found_key = key;
+              found_above = greater;
+              found_count = same;
+            }
+          }
+          __syncthreads();
+          base = found_key;
+          k -= found_above;
+          inside = found_count;
+          span = 0;
+        } else {
+          reinterpret_cast<int2*>(sh.hist[bins])[tid] = make_int2(0, 0);
+          __syncthreads();
+          for (int i = tid; i < all; i += kSelThreads) {
+            const unsigned d = list[i] - base;
+            if (d <= span) atomicAdd(&sh.hist[bins][d >> digit], 1);
+          }
+          __syncthreads();
+          narrow(1, bins);
+        }
+      }
+    }
+  }
+  // Kept: scores above `base`, and the first k of those equal to it; where all of these are kept (or none competes),
+  // scores from `base` on.  (With inside == k the range may still be wider than one value.)
+  const bool split = inside > k;
+  const unsigned least = split ? base + 1u : base;
+
+  const unsigned from = max(least, 1u);                                // key 0 is no token
+  auto keys_at = [&](int v) {                                          // with marks in the slots that do not compete
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (v < quad_end) q = quad_at(v);
+    if (!kStaged && (v < qa || v >= qb)) q = marked(q, v);
+    return q;
+  };
+  // Where the part's list starts: behind what the parts before it keep, which the cluster has to count first.
+  int at_above = 0, at_equal = 0;
+  if (parts > 1) {
     int n_above = 0, n_equal = 0;
-    for (int i = w0; i < w1; ++i) {
-      n_above += __popc(bits_above[i]);
-      if (split) n_equal += __popc(bits_equal[i]);
+    for (int v = quad_begin + tid; v < quad_end; v += kSelThreads) {
+      const uint4 q = keys_at(v);
+      n_above += (q.x >= from) + (q.y >= from) + (q.z >= from) + (q.w >= from);
+      n_equal += (q.x == base) + (q.y == base) + (q.z == base) + (q.w == base);
     }
-    int total_above, total_equal = 0;
-    int at_above = above_before + block_scan(n_above, warp_sums, &total_above), at_equal = equal_before;
-    if (split) at_equal += block_scan(n_equal, warp_sums, &total_equal);
-    int part_above = 0, part_equal = 0;                                // in the parts before this one
-    if (parts > 1) {
-      if (tid == 0) {
-        sh.above = total_above;
-        sh.equal = total_equal;
-      }
-      cluster.sync();
-      for (int p = 0; p < part; ++p) {
-        part_above += other(p)->above;
-        part_equal += other(p)->equal;
-      }
-      at_above += part_above;
-      at_equal += part_equal;
+    int total_above, total_equal;
+    block_scan(n_above, warp_sums, &total_above);
+    block_scan(n_equal, warp_sums, &total_equal);
+    if (tid == 0) {
+      sh.above = total_above;
+      sh.equal = total_equal;
     }
-    // A staged row's list is put together where its scores were (they have been used) and written in order.
-    const int out0 = above_before + part_above + min(equal_before + part_equal, ties);
-    for (int i = w0; i < w1; ++i) {
-      unsigned kept = bits_above[i];
-      int at = at_above + min(at_equal, ties) - (kStaged ? out0 : 0);
-      at_above += __popc(kept);
-      if (split) {
-        unsigned equal = bits_equal[i];
-        const int here = __popc(equal);
-        for (int room = max(0, ties - at_equal); here > room && __popc(equal) > room;)
-          equal &= ~(0x80000000u >> __clz(equal));                     // the highest of them go
-        kept |= equal;
-        at_equal += here;
-      }
-      const int token = word_slot + i * 32 - shift;
-      while (kept) {
-        (kStaged ? reinterpret_cast<int*>(staged) : out)[at++] = token + __ffs(kept) - 1;
-        kept &= kept - 1;
-      }
+    cluster.sync();
+    const Shared* o = other(lane % parts);
+    at_above = __reduce_add_sync(0xffffffffu, lane < part ? o->above : 0);
+    at_equal = __reduce_add_sync(0xffffffffu, lane < part ? o->equal : 0);
+  }
+  const int list_begin = at_above + (split ? min(at_equal, k) : 0);
+  // A staged row's list is put together where its scores were: what is kept of the slots so far needs no more
+  // room than they did, and they are in registers.
+  int* const list = kStaged ? reinterpret_cast<int*>(staged) : out;
+  for (int round = quad_begin; round < quad_end; round += kSelRunQuads * kSelThreads) {
+    unsigned e[4 * kSelRunQuads];                                      // this thread's run
+    const int v0 = round + tid * kSelRunQuads;
+#pragma unroll
+    for (int i = 0; i < kSelRunQuads; ++i) {
+      const uint4 q = keys_at(v0 + i);
+      e[4 * i] = q.x;
+      e[4 * i + 1] = q.y;
+      e[4 * i + 2] = q.z;
+      e[4 * i + 3] = q.w;
     }
-    above_before += total_above;
-    equal_before += total_equal;
-    if (kStaged) {
-      __syncthreads();
-      const int count = above_before + part_above + min(equal_before + part_equal, ties) - out0;
-      for (int i = tid; i < count; i += kSelThreads) out[out0 + i] = (int)staged[i];
+    int n_above = 0, n_equal = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * kSelRunQuads; ++i) n_above += e[i] >= from ? 1 : 0;
+    int total_above, total_equal = 0, equal = at_equal;
+    const int above = at_above + block_scan(n_above, warp_sums, &total_above);
+    int at = above - (kStaged ? list_begin : 0);
+    const int token = v0 * 4 - shift;
+    if (split) {
+#pragma unroll
+      for (int i = 0; i < 4 * kSelRunQuads; ++i) n_equal += e[i] == base ? 1 : 0;
+      equal += block_scan(n_equal, warp_sums, &total_equal);
+      at += min(equal, k);
     }
-    __syncthreads();                                                   // the words may be written again
+    // the run's equal scores all stay or all go, but for one run of the row
+    if (equal < k && equal + n_equal > k) {
+#pragma unroll
+      for (int i = 0; i < 4 * kSelRunQuads; ++i)
+        if (e[i] >= from || (e[i] == base && equal++ < k)) list[at++] = token + i;
+    } else {
+      const unsigned cut = n_equal > 0 && equal < k ? base : from;
+#pragma unroll
+      for (int i = 0; i < 4 * kSelRunQuads; ++i)
+        if (e[i] >= cut) list[at++] = token + i;
+    }
+    at_above += total_above;
+    at_equal += total_equal;
+  }
+  if (kStaged) {
+    __syncthreads();
+    const int count = at_above + (split ? min(at_equal, k) : 0) - list_begin;
+    for (int i = tid; i < count; i += kSelThreads) out[list_begin + i] = list[i];
   }
   if (parts > 1) cluster.sync();                                       // the others have read this block's counts
 }
 
-// Blocks per row.  More than one where a part would not leave room for a second block on the SM (20,480
-// scores), and where the rows alone do not fill the GPU (down to 2048 scores a block).
-inline int select_parts(long long rows, int n, int sm_count) {
+// Blocks per row: as few as hold it.
+inline cudaError_t launch_select(const SelectArgs& a, long long rows, cudaStream_t stream) {
+  const int quads = (a.n + 3 + 3) / 4;                                 // up to three slots before the first token
   int parts = 1;
-  while (parts < kSelMaxCluster && (n / parts > 20480 || (rows * parts <= sm_count && n / parts > 2048))) parts *= 2;
-  return parts;
-}
-
-inline cudaError_t launch_select(const SelectArgs& a, long long rows, int sm_count, cudaStream_t stream) {
-  const int parts = select_parts(rows, a.n, sm_count);
-  // slots of the largest part (up to three slots before the first token, whole words)
-  const int part_slots = (((a.n + 3 + 31) / 32 + parts - 1) / parts) * 32;
-  if (part_slots > kSelStaged || rows * parts > 0x7fffffffLL) {
-    select_tokens_kernel<false><<<(unsigned)rows, kSelThreads, 2 * kSelWords * 4, stream>>>(a);
+  while (parts < kSelMaxCluster && (quads + parts - 1) / parts * 4 > kSelStaged) parts *= 2;
+  const int part_quads = (quads + parts - 1) / parts;
+  if (part_quads * 4 > kSelStaged || rows * parts > 0x7fffffffLL) {
+    select_tokens_kernel<false><<<(unsigned)rows, kSelThreads, 0, stream>>>(a);
     return cudaGetLastError();
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * parts), 1, 1);
   cfg.blockDim = dim3(kSelThreads, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)part_slots * 4 + part_slots / 32 * 8;
+  cfg.dynamicSmemBytes = (size_t)part_quads * 16;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -418,7 +456,7 @@ inline cudaError_t launch_select(const SelectArgs& a, long long rows, int sm_cou
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = parts > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, select_tokens_kernel<true>, a);
 }
 

@@ -451,7 +451,7 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
 }
 
 cudaError_t configure_token_ops(bool tensor_ok) {
-  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4 + kSelStaged / 32 * 8);
+  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
   const int ws = (int)weights_simt_smem(kSimtMaxD);
   auto simt = [&](auto words) {
     constexpr int kWords = decltype(words)::value;
@@ -505,7 +505,7 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
     a.n = n;
     a.keep = keep;
     DeviceGuard guard(ctx->cfg.device);
-    const cudaError_t e = launch_select(a, rows, ctx->sm_count, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_select(a, rows, static_cast<cudaStream_t>(stream));
     ctx->launches++;
     return cuda_status(ctx, e, "select_tokens");
   });

@@ -333,7 +333,7 @@ def test_select_special_values(bc):
     assert select(bc, x[:0], 5) == [] and select(bc, x, 0) == [[]] * 6
 
 
-@pytest.mark.parametrize("n", [16384, 40001, 49152, 49153, 131072, 300007])
+@pytest.mark.parametrize("n", [16384, 40001, 49149, 49150, 49153, 131072, 300007, 393300])
 def test_select_long_rows(bc, n):
     x = torch.exp(torch.randn((3, n), generator=gen(n), device="cuda") * 2 - 5)
     x[1] = (x[1] * 64).round()
