@@ -530,7 +530,8 @@ compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_consta
 //                  exp(scale q[a][h] . k[t][j] - lse[a][h]);
 // rows with an infinite lse add nothing.  The batch: groups (one per prefix), the runs of query rows that
 // belong to each, and their page lists, all in the parameter list.  Row space of a group: the tokens of its
-// requests one after the other, packed row p = token * G + head in the KV group, cut into row tiles.  A
+// requests one after the other, packed row p = token * G + head in the KV group, cut into row tiles (of 64 rows in
+// the CUDA-core form, of whole tokens in the other).  A
 // work item is one block of keys against a range of row tiles; with several ranges (splits) the items
 // write partial sums and a second kernel adds them in a fixed order.
 // ---------------------------------------------------------------------------------------------
@@ -568,6 +569,8 @@ struct WeightArgs {
   int page_bytes, swizzled;
   int Hq, Hkv, D;
   int num_groups, num_items;
+  int tile_tokens;              // tensor-core form: tokens of a row tile (as many as give at most 128 rows)
+  int boxes;                    // tensor-core form: the tensor map of q is valid
 };
 
 __device__ __forceinline__ const WeightGroup& weight_group(const int* list, int g) {

@@ -1,20 +1,27 @@
 // Accumulated attention weights on the tensor cores (bf16, head_dim 128): for every cached key the sum over
 // all query rows of exp(scale q.k - lse), see WeightGroup in evict.cuh for the batch.
 //
-// S^T = K Q^T: the keys are the M dimension, so a TMEM lane is one key and a thread that owns the lane sums
-// over the columns (rows of queries) on its own - no shuffles, no atomics, one running sum in a register.  Two
-// key tiles of 128 stay in shared memory while the row tiles of 128 stream past them; every row tile is
-// gathered once per 256 keys.
+// S = Q K^T with 128 query rows on the TMEM lanes and 256 keys along the columns.  The keys of an item stay in
+// shared memory while the row tiles stream past them.  A thread owns a row (its log-sum-exp is one register) and
+// 64 of the keys, for each of which it keeps a running sum in a register; the sum over the rows of a tile, across
+// the lanes, is put off until up to 48 tiles have been added, and then costs 62 shuffles for 64 keys.  (With the
+// keys on the lanes the sum over rows needs no shuffles, but every log-sum-exp is a shared-memory operand of
+// every thread: that form ran at 4.6 ms where this one takes 4.1, 32 requests of 1024 rows and 28 heads over 16,384 keys.)
 //
 // What bounds it: one exponential per (row, key) against 256 flops of the product.  An SM computes 16
-// exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a 128 x 128
-// tile takes 1024 cycles of the one and 512 of the other.  With few rows it is bound by reading the keys.
+// exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a tile of 128 x
+// 256 takes 2048 cycles of the one and 1024 of the other.  A thread's 64 sums leave no registers to
+// hide a polynomial's constants and latency behind: sending two of every eight pairs to the FMA pipe, which is
+// faster on its own (116 cycles against 135 for 16 keys of four warps), made the kernel 8 % slower.
+// With few rows the kernel is bound by reading the keys.
 //
-// Roles: warps 0-3 sum key tile 0, warps 4-7 key tile 1, warp 8 issues the MMAs and owns TMEM, warp 9 stages
-// key tiles (pages, 4 KB bulk copies: a page already is the operand image), warps 10-13 gather the query rows
-// (16-byte copies, any head grouping and row stride) with their log-sum-exps.  Key tiles have a ring of four
-// slots (the next item's are fetched while this one's are used), row tiles a ring of three, S two buffers
-// per key tile.  All waits are bounded as in the attention kernels.
+// Roles: warps 0-15 exponentials and sums (warp w: lanes 32 (w & 3) .., keys 64 (w >> 2) ..), warp 16 issues the MMAs
+// and owns TMEM (two S buffers of 256 columns), warp 17 stages keys (pages, 4 KB bulk copies: a page already is the
+// operand image), warps 18 and 19 fetch the query rows with their log-sum-exps.  A row tile is the G query heads
+// of as many tokens as fit 128 rows: if its tokens are one run of rows, two TMA boxes (64 dims, G heads, the
+// tokens) are the tile; a tile that spans the end of one request and the start of the next is gathered with
+// 16-byte copies.  Keys have two slots of 256 (the next item's are fetched while this one's are used), row tiles a
+// ring of three.  All waits are bounded as in the attention kernels.
 #pragma once
 #include "evict.cuh"
 #include "tc_attention.cuh"
@@ -26,30 +33,45 @@ using namespace tc;
 
 constexpr int kItemKeys = 256;
 constexpr int kRowTile = 128;
-constexpr int kKSlots = 4, kQSlots = 3;
-constexpr int kSumWarps = 8;
-constexpr int kWtsThreads = 448;
+constexpr int kKeyBytes = kItemKeys * 128 * 2;   // 64 KB
+constexpr int kKSlots = 2, kQSlots = 3;
+constexpr int kSumWarps = 16;
+constexpr int kMmaWarpW = 16, kKeyWarp = 17, kRowWarp = 18;
+constexpr int kWtsThreads = 640;             // 20 warps: five to a scheduler
+constexpr int kLaunchRegs = 96;              // what the compiler gives 640 threads
+constexpr int kSumRegs = 104, kFetchRegs = 64;   // after the split, per thread
+static_assert(32 * kSumWarps * kSumRegs + 128 * kFetchRegs <= kWtsThreads * kLaunchRegs, "register split within the block's share");
+constexpr int kGroupKeys = 4 * kItemKeys / kSumWarps;      // keys of a sum warp
+constexpr int kLaneKeys = kGroupKeys / 32;                 // whose sums end in a lane
+constexpr int kMaxTerms = 48;                // row tiles a thread adds before the lanes are put together
 constexpr unsigned kIdescNoN = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // as kIdescQK, N to be added
 
 struct alignas(16) Sync {
   float neg_lse2[kQSlots][kRowTile];      // -lse log2(e) per row of the tile; -inf: the row adds nothing
-  int masked[kQSlots][4];                 // per gather warp: some row of its 32 adds nothing
+  float hop_sum[kItemKeys];               // sums on their way from one lane group to the next
   unsigned long long k_full[kKSlots], k_free[kKSlots];
   unsigned long long q_full[kQSlots], q_free[kQSlots];
-  unsigned long long s_full[2][2], s_free[2][2];      // [key tile][buffer]
+  unsigned long long s_full[2], s_free[2];
+  unsigned long long hop[kSumWarps / 4][4];   // [key group][lane group]: hop_sum holds the sums of lane groups >= it; 0: read
   unsigned long long drain;
   long long wait_cycles;                  // directly before abort_flag (mbar_wait reads it)
   int abort_flag;
   unsigned tmem_base;
   int dead;
 };
-constexpr int kSmemBytes = 1024 + (kKSlots + kQSlots) * kTileBytes + (int)sizeof(Sync);
+constexpr int kSmemBytes = kKSlots * kKeyBytes + kQSlots * kTileBytes + (int)sizeof(Sync);
 static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
+
+// byte offset of 16-byte chunk c16 (0..15) of row r (0..127) of a row tile: two blocks of 128 rows x 64 dims, as the TMA
+// boxes write them (8-row groups 1024 bytes apart), 128-byte swizzle
+__device__ __forceinline__ unsigned row_chunk_offset(int r, int c16) {
+  return (unsigned)((c16 >> 3) * 16384 + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
+}
 
 // One work item as every role derives it from the parameter list.
 struct Item {
   int hk, key0, keys;                     // KV head, first key of the launch's key range, keys (1 .. 256)
-  int tile_begin, tile_end, rows;         // row tiles; packed rows of the group
+  int tile_begin, tile_end, tokens;       // row tiles; tokens of the group
   int split, g;
 };
 __device__ __forceinline__ Item read_item(const WeightArgs& a, const int* list, int index) {
@@ -63,15 +85,11 @@ __device__ __forceinline__ Item read_item(const WeightArgs& a, const int* list, 
   it.hk = rem / g.splits;
   it.key0 = kb * kItemKeys;
   it.keys = min(kItemKeys, g.m - it.key0);
-  it.rows = g.tokens * (a.Hq / a.Hkv);
-  const int tiles = (it.rows + kRowTile - 1) / kRowTile;
+  it.tokens = g.tokens;
+  const int tiles = (it.tokens + a.tile_tokens - 1) / a.tile_tokens;
   it.tile_begin = min(tiles, it.split * g.tiles_per_split);
   it.tile_end = min(tiles, it.tile_begin + g.tiles_per_split);
   return it;
-}
-// columns of a row tile that are computed: its rows, to a multiple of 32
-__device__ __forceinline__ int tile_cols(const Item& it, int tile) {
-  return min(kRowTile, (it.rows - tile * kRowTile + 31) & ~31);
 }
 
 // A running sum with its rounding error carried along (the sums run over up to millions of rows).
@@ -86,23 +104,46 @@ struct Sum2 {
   __device__ __forceinline__ double value() const { return (double)s + (isinf(s) ? 0.0 : (double)c); }
 };
 
+// Has the phase completed?  Unlike try_wait this does not suspend the thread.
+__device__ __forceinline__ bool mbar_test(unsigned bar, unsigned parity) {
+  unsigned ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
 }  // namespace wts
 
 template <int kWords>
 __global__ void __launch_bounds__(wts::kWtsThreads, 1)
-tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ ParamList<kWords> params, int* status,
-                  long long wait_cycles) {
+tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap q_map, int* status,
+                  long long wait_cycles, const __grid_constant__ ParamList<kWords> params) {
   using namespace wts;
   const int* const list = params.w;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Sync* sy = reinterpret_cast<Sync*>(smem + (kKSlots + kQSlots) * kTileBytes);
+  // No room for alignment slack: the kernel has no static shared memory, the dynamic window starts 1024-byte
+  // aligned (the swizzled tiles need that), and a CTA that finds otherwise reports an error instead of computing.
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Sync* sy = reinterpret_cast<Sync*>(smem + kKSlots * kKeyBytes + kQSlots * kTileBytes);
   volatile int* abort_flag = &sy->abort_flag;
-  const unsigned k_ring = smem_u32(smem), q_ring = k_ring + kKSlots * kTileBytes;
+  const unsigned k_ring = smem_u32(smem), q_ring = k_ring + kKSlots * kKeyBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
     sy->wait_cycles = wait_cycles;
+    if ((smem_u32(smem) & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
     sy->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
     sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
     for (int i = 0; i < kKSlots; ++i) {
@@ -110,18 +151,18 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       mbar_init(smem_u32(&sy->k_free[i]), 1);
     }
     for (int i = 0; i < kQSlots; ++i) {
-      mbar_init(smem_u32(&sy->q_full[i]), 128);
-      mbar_init(smem_u32(&sy->q_free[i]), 1 + kSumWarps);
+      mbar_init(smem_u32(&sy->q_full[i]), 64);
+      mbar_init(smem_u32(&sy->q_free[i]), 1 + kSumWarps);     // the MMAs; the warps that read the log-sum-exps
     }
-    for (int x = 0; x < 2; ++x)
-      for (int b = 0; b < 2; ++b) {
-        mbar_init(smem_u32(&sy->s_full[x][b]), 1);
-        mbar_init(smem_u32(&sy->s_free[x][b]), 4);
-      }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&sy->s_full[b]), 1);
+      mbar_init(smem_u32(&sy->s_free[b]), kSumWarps);
+    }
+    for (int i = 0; i < kSumWarps; ++i) mbar_init(smem_u32(&sy->hop[i >> 2][i & 3]), 1);
     mbar_init(smem_u32(&sy->drain), 1);
     fence_barrier_init();
   }
-  if (warp == 8) {
+  if (warp == kMmaWarpW) {
     tmem_alloc(smem_u32(&sy->tmem_base), kTmemCols);
     tmem_relinquish();
   }
@@ -133,211 +174,341 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 
   if (warp < kSumWarps) {
     // ================================ exponentials and sums ================================
-    const int x = warp >> 2;                                  // key tile
-    const unsigned lane_base = (unsigned)((warp & 3) * 32) << 16;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
+    const int lg = warp & 3, kg = warp >> 2;                  // lane group, key group
+    const unsigned s_addr = tmem + kg * kGroupKeys + ((unsigned)(lg * 32) << 16);
     const float sl2 = a.scale * 1.4426950408889634f;
     const unsigned long long sl2_2 = pack2(sl2, sl2);
     bool ok = !dead;
-    unsigned qt = 0, st = 0;                                  // row tiles seen; S buffers of this key tile used
+    unsigned slot = 0, slot_parity = 0, b = 0, b_parity = 0;  // row tile ring and S buffer of the next tile
+    unsigned handed = 0;                                      // items whose sums went from group to group
+    const unsigned q_full0 = smem_u32(&sy->q_full[0]), q_free0 = smem_u32(&sy->q_free[0]);
+    const unsigned s_full0 = smem_u32(&sy->s_full[0]), s_free0 = smem_u32(&sy->s_free[0]);
     for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
       const Item it = read_item(a, list, item);
-      const bool active = it.keys > x * 128;
-      Sum2 total = {0.f, 0.f};
-      for (int tile = it.tile_begin; tile < it.tile_end && ok; ++tile, ++qt) {
-        const unsigned slot = qt % kQSlots;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->q_full[slot]), (qt / kQSlots) & 1, abort_flag));
-        if (!ok) break;
-        if (active) {
-          const unsigned b = st & 1;
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->s_full[x][b]), (st >> 1) & 1, abort_flag));
+      const bool active = it.keys > kg * kGroupKeys;
+      Sum2 total[kLaneKeys];                                  // keys kLaneKeys * lane .., over this lane group
+#pragma unroll
+      for (int i = 0; i < kLaneKeys; ++i) total[i] = Sum2{0.f, 0.f};
+      for (int left = it.tile_end - it.tile_begin; left > 0 && ok; left -= kMaxTerms) {
+        unsigned long long acc[kGroupKeys / 2];                 // keys 2 p, 2 p + 1 of the warp's
+#pragma unroll
+        for (int p = 0; p < kGroupKeys / 2; ++p) acc[p] = 0ull;
+#pragma unroll 1
+        for (int n = min(left, kMaxTerms); n > 0; --n) {
+          // one vote for both waits: after a give-up the log-sum-exp read in between is any number
+          bool good = mbar_wait(q_full0 + slot * 8, slot_parity, abort_flag);
+          const float nl = sy->neg_lse2[slot][lg * 32 + lane];
+          good = mbar_wait(s_full0 + b * 8, b_parity, abort_flag) && good;
+          ok = __all_sync(0xffffffffu, good);
           if (!ok) break;
+          if (lane == 0) mbar_arrive(q_free0 + slot * 8);       // the vote is behind every lane's read
           tc_fence_after();
-          const int cols = tile_cols(it, tile);
-          const unsigned s_addr = tmem + (x * 2 + b) * kRowTile + lane_base;
-          const float* nl = sy->neg_lse2[slot];
-          unsigned long long acc_a = pack2(0.f, 0.f), acc_b = acc_a;
-          for (int c = 0; c < cols; c += 32) {
-            unsigned r[32];
-            tmem_ld32(s_addr + c, r);
-            tmem_wait_ld();
-            if (sy->masked[slot][c >> 5]) {
-              // some rows add nothing: selected out, because a product with a key that is not finite is NaN
-              float sum = 0.f;
+          const bool adds = nl != -INFINITY;
+          const unsigned live = __ballot_sync(0xffffffffu, adds);
+          const bool computes = active && live != 0u;
+          if (computes) {
+            const unsigned long long nl2 = pack2(nl, nl);
+            const unsigned s_tile = s_addr + b * kItemKeys;
+            // without branches inside: the compiler overlaps the end of one run of 16 keys with the start of the next
+            auto sum_tile = [&](auto holes) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float l = nl[c + i];
-                const float e = ex2(fmaf(__uint_as_float(r[i]), sl2, l));
-                sum += l == -INFINITY ? 0.f : e;
-              }
-              acc_a = add2(acc_a, pack2(sum, 0.f));
-            } else {
+              for (int c = 0; c < kGroupKeys / 16; ++c) {
+                unsigned r[16];
+                tmem_ld16(s_tile + c * 16, r);
+                tmem_wait_ld();
+                if (decltype(holes)::value) {
+                  // a row that adds nothing: whatever its product is (with a key that is not finite, or from memory behind
+                  // the last request), 2^-inf is 0
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 l = *reinterpret_cast<const float4*>(nl + c + i);
-                const unsigned long long xa =
-                    fma2(pack2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sl2_2, pack2(l.x, l.y));
-                const unsigned long long xb =
-                    fma2(pack2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), sl2_2, pack2(l.z, l.w));
-                float x0, x1, x2, x3;
-                unpack2(xa, x0, x1);
-                unpack2(xb, x2, x3);
-                acc_a = add2(acc_a, pack2(ex2(x0), ex2(x1)));
-                acc_b = add2(acc_b, pack2(ex2(x2), ex2(x3)));
+                  for (int i = 0; i < 16; ++i) r[i] = adds ? r[i] : 0u;
+                }
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                  float x0, x1;
+                  unpack2(fma2(pack2(__uint_as_float(r[2 * p]), __uint_as_float(r[2 * p + 1])), sl2_2, nl2), x0, x1);
+                  acc[c * 8 + p] = add2(acc[c * 8 + p], pack2(ex2(x0), ex2(x1)));
+                }
               }
-            }
+            };
+            if (live == 0xffffffffu) sum_tile(std::false_type()); else sum_tile(std::true_type());
           }
           tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&sy->s_free[x][b]));
-          float s0, s1, s2, s3;
-          unpack2(acc_a, s0, s1);
-          unpack2(acc_b, s2, s3);
-          total.add((s0 + s1) + (s2 + s3));
-          ++st;
+          if (lane == 0) mbar_arrive(s_free0 + b * 8);
+          if (++slot == kQSlots) {
+            slot = 0;
+            slot_parity ^= 1;
+          }
+          b ^= 1;
+          b_parity ^= b ^ 1;                                    // the phase changes when both buffers have been used
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sy->q_free[slot]));
+        if (active) {
+          // The lanes' sums put together: in each step a lane passes half of its keys to its partner and takes the other
+          // half; lane l ends with the keys from kLaneKeys * l on.
+          float v[kGroupKeys];
+#pragma unroll
+          for (int p = 0; p < kGroupKeys / 2; ++p) unpack2(acc[p], v[2 * p], v[2 * p + 1]);
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+            const bool upper = (lane & o) != 0;
+#pragma unroll
+            for (int i = 0; i < kLaneKeys * o; ++i) {
+              const float send = upper ? v[i] : v[i + kLaneKeys * o], keep = upper ? v[i + kLaneKeys * o] : v[i];
+              v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kLaneKeys; ++i) total[i].add(v[i]);
+        }
       }
       if (!ok) break;
-      const WeightGroup& g = weight_group(list, it.g);
-      const int t = it.key0 + x * 128 + (warp & 3) * 32 + lane;
-      if (t < g.m) {
-        if (g.splits > 1) {
-          a.part[g.part_off + ((long long)it.split * a.Hkv + it.hk) * g.m + t] = (float)total.value();
-        } else {
-          const long long o = g.score_off + it.hk * a.head_stride + g.key0 + t;
-          const double before = a.decay != 0.f ? (double)a.decay * (double)a.in[o] : 0.0;
-          a.out[o] = (float)(before + total.value());
+      // Lane groups 3, 2, 1, 0 add their sums in turn; group 0 writes the result.
+      if (active) {
+        const int first = kg * kGroupKeys + kLaneKeys * lane;
+        double sum[kLaneKeys];
+#pragma unroll
+        for (int i = 0; i < kLaneKeys; ++i) sum[i] = total[i].value();
+        if (it.tile_begin < it.tile_end) {
+          // group 3 waits for group 0 to have read the item before
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->hop[kg][(lg + 1) & 3]), (handed & 1) ^ (lg == 3 ? 1 : 0), abort_flag));
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < kLaneKeys; ++i) {
+            if (lg < 3) sum[i] += (double)sy->hop_sum[first + i];
+            if (lg > 0) sy->hop_sum[first + i] = (float)sum[i];
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sy->hop[kg][lg]));
+          ++handed;
+        }
+        if (lg == 0) {
+          const WeightGroup& g = weight_group(list, it.g);
+#pragma unroll
+          for (int i = 0; i < kLaneKeys; ++i) {
+            const int t = it.key0 + first + i;
+            if (t >= g.m) break;
+            if (g.splits > 1) {
+              a.part[g.part_off + ((long long)it.split * a.Hkv + it.hk) * g.m + t] = (float)sum[i];
+            } else {
+              const long long o = g.score_off + it.hk * a.head_stride + g.key0 + t;
+              a.out[o] = (float)((a.decay != 0.f ? (double)a.decay * (double)a.in[o] : 0.0) + sum[i]);
+            }
+          }
         }
       }
     }
     tc_fence_before();
-  } else if (warp == 8) {
-    // ====================================== MMA issue ======================================
-    bool ok = !dead;
-    unsigned qt = 0, kt = 0;                                  // row tiles and key tiles consumed
-    unsigned st[2] = {0, 0};                                  // S buffers filled, per key tile
-    const unsigned el = elect_one() ? 1u : 0u;
-    auto kstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 64); };
-    for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-      const Item it = read_item(a, list, item);
-      const int ktiles = it.keys > 128 ? 2 : 1;
-      if (it.tile_begin >= it.tile_end) continue;             // no rows: no keys are staged either
-      for (int x = 0; x < ktiles && ok; ++x)
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_full[(kt + x) % kKSlots]), ((kt + x) / kKSlots) & 1, abort_flag));
-      for (int tile = it.tile_begin; tile < it.tile_end && ok; ++tile, ++qt) {
-        const unsigned slot = qt % kQSlots;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->q_full[slot]), (qt / kQSlots) & 1, abort_flag));
-        const unsigned idesc = kIdescNoN | ((unsigned)(tile_cols(it, tile) >> 3) << 17);
-        const unsigned long long q_desc = make_desc(q_ring + slot * kTileBytes, 16, 2048);
-        for (int x = 0; x < ktiles && ok; ++x) {
-          const unsigned b = st[x] & 1;
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->s_free[x][b]), ((st[x] >> 1) & 1) ^ 1, abort_flag));
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFetchRegs));
+    if (warp == kMmaWarpW) {
+      // ====================================== MMA issue ======================================
+      bool ok = !dead;
+      unsigned qt = 0, kt = 0;                                // row tiles and key blocks consumed
+      const unsigned el = elect_one() ? 1u : 0u;
+      // a K step of 16 dims: 32 bytes inside the swizzled row; dims 64.. sit 1024 bytes further in the keys, 16 KB
+      // further in a row tile
+      auto kstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 64); };
+      auto qstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 1024); };
+      for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
+        const Item it = read_item(a, list, item);
+        if (it.tile_begin >= it.tile_end) continue;           // no rows: no keys are staged either
+        const unsigned ks = kt % kKSlots;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_full[ks]), (kt / kKSlots) & 1, abort_flag));
+        const unsigned idesc = kIdescNoN | ((unsigned)((it.keys + 15) >> 4) << 18);       // N: keys to a multiple of 16
+        const unsigned long long k_desc = make_desc(k_ring + ks * kKeyBytes, 16, 2048);
+        for (int tile = it.tile_begin; tile < it.tile_end && ok; ++tile, ++qt) {
+          const unsigned slot = qt % kQSlots, b = qt & 1;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->q_full[slot]), (qt / kQSlots) & 1, abort_flag));
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->s_free[b]), ((qt >> 1) & 1) ^ 1, abort_flag));
           if (!ok) break;
           tc_fence_after();
-          const unsigned long long k_desc = make_desc(k_ring + ((kt + x) % kKSlots) * kTileBytes, 16, 2048);
-          unsigned long long ka[8], qb[8];
+          const unsigned long long q_desc = make_desc(q_ring + slot * kTileBytes, 16, 1024);
+          unsigned long long qa[8], kb[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            ka[k] = k_desc + kstep(k);
-            qb[k] = q_desc + kstep(k);
+            qa[k] = q_desc + qstep(k);
+            kb[k] = k_desc + kstep(k);
           }
-          mma_ss_batch8(el, tmem + (x * 2 + b) * kRowTile, ka, qb, idesc);
-          mma_commit_pred(el, smem_u32(&sy->s_full[x][b]));
-          ++st[x];
+          mma_ss_batch8(el, tmem + b * kItemKeys, qa, kb, idesc);
+          mma_commit_pred(el, smem_u32(&sy->s_full[b]));
+          mma_commit_pred(el, smem_u32(&sy->q_free[slot]));
         }
-        if (ok) mma_commit_pred(el, smem_u32(&sy->q_free[slot]));
+        if (ok) mma_commit_pred(el, smem_u32(&sy->k_free[ks]));
+        ++kt;
       }
-      if (ok)
-        for (int x = 0; x < ktiles; ++x) mma_commit_pred(el, smem_u32(&sy->k_free[(kt + x) % kKSlots]));
-      kt += ktiles;
-    }
-    // Whatever happened, let every MMA issued so far finish before TMEM is released.
-    __syncwarp();
-    if (!dead) {
-      mma_commit_elect(smem_u32(&sy->drain));
-      mbar_wait_issued(smem_u32(&sy->drain), 0);
-    }
-    __syncwarp();
-  } else if (warp == 9) {
-    // ====================================== key tiles ======================================
-    bool ok = !dead;
-    unsigned kt = 0;
-    int armed[kKSlots] = {-1, -1, -1, -1};                    // the last phase armed with copies, per slot
-    for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-      const Item it = read_item(a, list, item);
-      if (it.tile_begin >= it.tile_end) continue;
-      const WeightGroup& g = weight_group(list, it.g);
-      for (int k0 = 0; k0 < it.keys && ok; k0 += 128, ++kt) {
-        const unsigned slot = kt % kKSlots;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[slot]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
+      // Whatever happened, let every MMA issued so far finish before TMEM is released.
+      __syncwarp();
+      if (!dead) {
+        mma_commit_elect(smem_u32(&sy->drain));
+        mbar_wait_issued(smem_u32(&sy->drain), 0);
+      }
+      __syncwarp();
+    } else if (warp == kKeyWarp) {
+      // ======================================== keys =========================================
+      bool ok = !dead;
+      unsigned kt = 0;
+      int armed[kKSlots] = {-1, -1};                          // the last phase armed with copies, per slot
+      for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
+        const Item it = read_item(a, list, item);
+        if (it.tile_begin >= it.tile_end) continue;
+        const WeightGroup& g = weight_group(list, it.g);
+        const unsigned ks = kt % kKSlots;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[ks]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
         if (!ok) break;
-        const int npages = (min(128, it.keys - k0) + kPageSize - 1) / kPageSize;
-        const unsigned full = smem_u32(&sy->k_full[slot]);
+        const int npages = (it.keys + kPageSize - 1) / kPageSize;          // up to 16
+        const unsigned full = smem_u32(&sy->k_full[ks]);
         // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
         if (lane < npages)
-          bulk_copy_g2s(k_ring + slot * kTileBytes + lane * kPageBytes,
-                        a.pool_k + ((long long)list[g.page_word + (it.key0 + k0) / kPageSize + lane] * a.Hkv + it.hk) * kPageBytes,
+          bulk_copy_g2s(k_ring + ks * kKeyBytes + lane * kPageBytes,
+                        a.pool_k + ((long long)list[g.page_word + it.key0 / kPageSize + lane] * a.Hkv + it.hk) * kPageBytes,
                         kPageBytes, full);
         if (lane == 0)
           mbar_arrive_expect_tx(full, (unsigned)(npages * kPageBytes));
         else
           mbar_arrive(full);
-        armed[slot] = (int)((kt / kKSlots) & 1);
+        armed[ks] = (int)((kt / kKSlots) & 1);
+        ++kt;
       }
-    }
-    // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
-      for (int s = 0; s < kKSlots; ++s)
-        if (armed[s] >= 0)
-          for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->k_full[s]), (unsigned)armed[s]); ++n) __nanosleep(256);
-    }
-  } else {
-    // ====================================== query rows ======================================
-    const int w = warp - 10;                                  // rows 32 w .. 32 w + 31 of every tile
-    const int G = a.Hq / a.Hkv;
-    const int c16 = lane & 15;
-    bool ok = !dead;
-    unsigned qt = 0;
-    int pending = -1;                                         // slot whose copies have not been announced yet
-    auto announce = [&]() {
-      fence_proxy_async();
-      mbar_arrive(smem_u32(&sy->q_full[pending]));
-      pending = -1;
-    };
-    for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-      const Item it = read_item(a, list, item);
-      const WeightGroup& g = weight_group(list, it.g);
-      for (int tile = it.tile_begin; tile < it.tile_end && ok; ++tile, ++qt) {
-        const unsigned slot = qt % kQSlots;
-        // where this lane's row is, and its log-sum-exp
-        const int p = tile * kRowTile + w * 32 + lane;
-        long long src = 0;
-        float nl = -INFINITY;
-        if (p < it.rows) {
-          const int tok = p / G, h = it.hk * G + (p - tok * G);
-          const long long row = weight_row(list, g, tok);
-          const float l = a.lse[row * a.Hq + h];
-          src = (row * a.q_stride + (long long)h * 128) * 2;
-          if (!isinf(l)) nl = l * -1.4426950408889634f;
+      // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
+      if (!dead && (!ok || *abort_flag) && lane == 0) {
+        for (int s = 0; s < kKSlots; ++s)
+          if (armed[s] >= 0)
+            for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->k_full[s]), (unsigned)armed[s]); ++n) __nanosleep(256);
+      }
+    } else {
+      // ====================================== query rows ======================================
+      // One tile ahead of the copies, every lane looks up where its rows of the tile are and requests their
+      // log-sum-exps, so that neither stands between two tiles' copies.
+      const int w = warp - kRowWarp;                          // rows 64 w .. 64 w + 63 of every tile
+      const int G = a.Hq / a.Hkv, T = a.tile_tokens;
+      const int c16 = lane & 15;
+      // byte offset in the tile of this lane's chunk of rows 2 j + (lane >> 4): repeats every four steps
+      unsigned chunk_off[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) chunk_off[j] = row_chunk_offset(2 * j + (lane >> 4), c16);
+      // token of the tile and head of the group of this lane's rows: the same in every tile
+      int tok_in[2], head_in[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = w * 64 + i * 32 + lane;
+        tok_in[i] = r / G;
+        head_in[i] = r - tok_in[i] * G;
+      }
+      bool ok = !dead;
+      unsigned qt = 0;
+      int boxed[kQSlots] = {-1, -1, -1};                      // the last phase armed with a box, per slot
+      int pending = -1;                                       // slot whose copies have not been announced yet
+      auto announce = [&]() {
+        fence_proxy_async();
+        mbar_arrive(smem_u32(&sy->q_full[pending]));
+        pending = -1;
+      };
+      int item = blockIdx.x, tile = 0, tile_end = 0, tokens = 0, hk = 0, segs = 0;
+      const WeightSeg* seg = nullptr;
+      // the runs of rows the lane's two rows and the tile's first token are in: number, end, row of token 0
+      int run[3], run_end[3];
+      long long run_row[3];
+      auto read_run = [&](int i, int number) {
+        run[i] = number;
+        run_row[i] = seg[number].row - seg[number].token;
+        run_end[i] = number + 1 < segs ? seg[number + 1].token : 0x7fffffff;
+      };
+      auto next_item = [&]() {                                // to the next item that has row tiles
+        for (; item < a.num_items; item += gridDim.x) {
+          const Item it = read_item(a, list, item);
+          if (it.tile_begin >= it.tile_end) continue;
+          const WeightGroup& g = weight_group(list, it.g);
+          tile = it.tile_begin;
+          tile_end = it.tile_end;
+          tokens = it.tokens;
+          hk = it.hk;
+          segs = g.num_segs;
+          seg = reinterpret_cast<const WeightSeg*>(&list[g.seg_word]);
+          int lo = 0, hi = segs - 1;                          // last run that starts at or before the first token
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (seg[mid].token <= tile * T) lo = mid; else hi = mid - 1;
+          }
+#pragma unroll
+          for (int i = 0; i < 3; ++i) read_run(i, lo);
+          return;
         }
-        const unsigned live = __ballot_sync(0xffffffffu, nl != -INFINITY);
+      };
+      long long src[2], box_row = 0;
+      float lse[2];
+      bool one_run = false;                                   // the tile's tokens are consecutive rows
+      auto look_up = [&]() {
+        const int tok0 = tile * T, last = min(tokens, tok0 + T) - 1;
+        while (tok0 >= run_end[2]) read_run(2, run[2] + 1);
+        one_run = a.boxes && last < run_end[2];
+        box_row = run_row[2] + tok0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int tok = tok0 + tok_in[i];
+          src[i] = 0;
+          lse[i] = INFINITY;
+          if (tok_in[i] < T && tok <= last) {
+            while (tok >= run_end[i]) read_run(i, run[i] + 1);
+            const long long row = run_row[i] + tok;
+            const int h = hk * G + head_in[i];
+            src[i] = (row * a.q_stride + (long long)h * 128) * 2;
+            lse[i] = a.lse[row * a.Hq + h];
+          }
+        }
+      };
+      next_item();
+      if (item < a.num_items) look_up();
+      while (item < a.num_items && ok) {
+        const int box_head = hk * G, box_first = (int)box_row;
+        const bool boxes = one_run;
+        float nl[2];
+        unsigned live[2];
+        long long from[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          nl[i] = isinf(lse[i]) ? -INFINITY : lse[i] * -1.4426950408889634f;
+          live[i] = __ballot_sync(0xffffffffu, nl[i] != -INFINITY);
+          from[i] = src[i];
+        }
+        if (++tile >= tile_end) {
+          item += gridDim.x;
+          next_item();
+        }
+        if (item < a.num_items) look_up();
+        const unsigned slot = qt % kQSlots;
         const unsigned q_free = smem_u32(&sy->q_free[slot]), free_parity = ((qt / kQSlots) & 1) ^ 1;
-        if (pending >= 0 && !__all_sync(0xffffffffu, mbar_try_wait(q_free, free_parity))) {
-          cp_async_wait<0>();                                 // the slot is not free yet: hand over what has been fetched
+        const unsigned q_full = smem_u32(&sy->q_full[slot]);
+        ++qt;
+        if (pending >= 0 && (boxes || !__all_sync(0xffffffffu, mbar_test(q_free, free_parity)))) {
+          cp_async_wait<0>();                                 // nothing more to put behind these copies yet: hand them over
           announce();
         }
         ok = __all_sync(0xffffffffu, mbar_wait(q_free, free_parity, abort_flag));
         if (!ok) break;
-        sy->neg_lse2[slot][w * 32 + lane] = nl;
-        if (lane == 0) sy->masked[slot][w] = live != 0xffffffffu;
-        if (w * 32 < tile_cols(it, tile)) {
-          const unsigned dst = q_ring + slot * kTileBytes;
-#pragma unroll 4
-          for (int i = 0; i < 16; ++i) {
-            const int r = 2 * i + (lane >> 4);
-            const long long s = __shfl_sync(0xffffffffu, src, r);
-            cp_async16(dst + tile_chunk_offset(w * 32 + r, c16), a.q + s + c16 * 16, (live >> r) & 1u ? 16u : 0u);
+        const unsigned dst = q_ring + slot * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sy->neg_lse2[slot][w * 64 + i * 32 + lane] = nl[i];
+        if (boxes) {
+          // rows past the tile's last token come along (or as zeros, past the tensor): they add nothing
+          if (lane == 0) {
+            mbar_arrive_expect_tx(q_full, (unsigned)(T * G * 128));         // each warp fetches one half of the dims
+            tma_load_3d(dst + w * 16384, &q_map, w * 64, box_head, box_first, q_full);
+            boxed[slot] = (int)(((qt - 1) / kQSlots) & 1);
+          } else {
+            mbar_arrive(q_full);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (live[i] == 0u) continue;                        // rows that add nothing may hold anything
+          const int r0 = w * 64 + i * 32;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int r = 2 * j + (lane >> 4);
+            const long long s = __shfl_sync(0xffffffffu, from[i], r);
+            cp_async16(dst + r0 * 128 + (j >> 2) * 1024 + chunk_off[j & 3], a.q + s + c16 * 16,
+                       (live[i] >> r) & 1u ? 16u : 0u);
           }
         }
         cp_async_commit();
@@ -347,13 +518,19 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         }
         pending = (int)slot;
       }
+      cp_async_wait<0>();
+      if (pending >= 0) announce();
+      // After a give-up, boxes may still be in flight: wait (bounded) for the barriers armed last.
+      if (!dead && (!ok || *abort_flag) && lane == 0) {
+        for (int s = 0; s < kQSlots; ++s)
+          if (boxed[s] >= 0)
+            for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->q_full[s]), (unsigned)boxed[s]); ++n) __nanosleep(256);
+      }
     }
-    cp_async_wait<0>();
-    if (pending >= 0) announce();
   }
 
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kMmaWarpW) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
@@ -361,20 +538,27 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 }
 
 inline cudaError_t configure_tc_weights() {
-  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsSmall>, attr, wts::kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsMid>, attr, wts::kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWords>, attr, wts::kSmemBytes);
+  auto configure = [](auto* kernel) {
+    cudaFuncAttributes attr;
+    cudaError_t e = cudaFuncGetAttributes(&attr, kernel);
+    // the register split must not ask for more than the block was launched with: it would wait for good
+    if (e == cudaSuccess && attr.numRegs < wts::kLaunchRegs) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wts::kSmemBytes);
+    return e;
+  };
+  cudaError_t e = configure(tc_weights_kernel<kParamWordsSmall>);
+  if (e == cudaSuccess) e = configure(tc_weights_kernel<kParamWordsMid>);
+  if (e == cudaSuccess) e = configure(tc_weights_kernel<kParamWords>);
   return e;
 }
 
 template <int kWords>
-cudaError_t launch_tc_weights(const WeightArgs& a, const ParamList<kWords>& list, int* status, int sm_count,
-                              long long wait_cycles, cudaStream_t stream) {
+cudaError_t launch_tc_weights(const WeightArgs& a, const CUtensorMap& q_map, const ParamList<kWords>& list, int* status,
+                              int sm_count, long long wait_cycles, cudaStream_t stream) {
   if (a.num_items <= 0) return cudaSuccess;
   const int grid = a.num_items < sm_count ? a.num_items : sm_count;
   tc_weights_kernel<kWords><<<grid, wts::kWtsThreads, wts::kSmemBytes, stream>>>(
-      a, list, status, wait_cycles > 0 ? wait_cycles : tc::kWaitCycles);
+      a, q_map, status, wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, list);
   return cudaGetLastError();
 }
 

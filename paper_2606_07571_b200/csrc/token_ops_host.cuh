@@ -39,8 +39,8 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0;
 // Group records grow from the front of the list, row runs and page lists from its end.
 class WeightLaunches {
  public:
-  WeightLaunches(bicache_ctx* ctx, const WeightArgs& args, bool tensor, cudaStream_t stream)
-      : ctx_(ctx), base_(args), tensor_(tensor), stream_(stream) {}
+  WeightLaunches(bicache_ctx* ctx, const WeightArgs& args, const CUtensorMap& q_map, bool tensor, cudaStream_t stream)
+      : ctx_(ctx), base_(args), q_map_(q_map), tensor_(tensor), stream_(stream) {}
 
   // keys [page0 * 16, min(m, (page0 + pages) * 16)) of a prefix against num_segs row runs; `first`: the call's
   // decay and input apply (else the launch adds to what an earlier one has written)
@@ -82,15 +82,14 @@ class WeightLaunches {
       a.decay = 1.f;
       a.in = a.out;
     }
-    const int G = a.Hq / a.Hkv;
-    const int block_keys = tensor_ ? wts::kItemKeys : kWsKeys, tile_rows = tensor_ ? wts::kRowTile : kWsRows;
+    const int block_keys = tensor_ ? wts::kItemKeys : kWsKeys;
     WeightGroup* g = reinterpret_cast<WeightGroup*>(list_);
     int max_tiles = 1, max_m = 1;
     long long base_items = 0;
     for (int i = 0; i < groups_; ++i) {
       g[i].key_blocks = (g[i].m + block_keys - 1) / block_keys;
       base_items += (long long)g[i].key_blocks * a.Hkv;
-      max_tiles = std::max(max_tiles, tiles_of(g[i], G, tile_rows));
+      max_tiles = std::max(max_tiles, tiles_of(g[i]));
       max_m = std::max(max_m, g[i].m);
     }
     // How many row tiles an item covers.  Fewer tiles make more items, which fill the SMs evenly, but every
@@ -104,7 +103,7 @@ class WeightLaunches {
       long long items = 0, part = 0;
       double work = 0;
       for (int i = 0; i < groups_; ++i) {
-        const int tiles = tiles_of(g[i], G, tile_rows), sp = std::max(1, (tiles + tps - 1) / tps);
+        const int tiles = tiles_of(g[i]), sp = std::max(1, (tiles + tps - 1) / tps);
         items += (long long)g[i].key_blocks * a.Hkv * sp;
         work += (double)g[i].key_blocks * a.Hkv * (tiles + sp);
         if (sp > 1) part += (long long)sp * a.Hkv * g[i].m;
@@ -121,7 +120,7 @@ class WeightLaunches {
     bool split = false;
     for (int i = 0; i < groups_; ++i) {
       g[i].tiles_per_split = best_tps;
-      g[i].splits = std::max(1, (tiles_of(g[i], G, tile_rows) + best_tps - 1) / best_tps);
+      g[i].splits = std::max(1, (tiles_of(g[i]) + best_tps - 1) / best_tps);
       g[i].item_begin = (int)item;
       item += (long long)g[i].key_blocks * a.Hkv * g[i].splits;
       g[i].part_off = (int)part;
@@ -143,7 +142,7 @@ class WeightLaunches {
     with_param_list(list_, kParamWords - gap, [&](const auto& list) {
       constexpr int kWords = sizeof(list.w) / sizeof(int);
       if (tensor_) {
-        e = launch_tc_weights(a, list, ctx_->d_status, ctx_->sm_count, ctx_->wait_cycles, stream_);
+        e = launch_tc_weights(a, q_map_, list, ctx_->d_status, ctx_->sm_count, ctx_->wait_cycles, stream_);
       } else {
         const size_t smem = weights_simt_smem(a.D);
         if (ctx_->cfg.dtype == BICACHE_F32)
@@ -167,13 +166,15 @@ class WeightLaunches {
   }
 
  private:
-  static int tiles_of(const WeightGroup& g, int G, int tile_rows) {
-    return (int)(((long long)g.tokens * G + tile_rows - 1) / tile_rows);
+  int tiles_of(const WeightGroup& g) const {
+    if (tensor_) return (g.tokens + base_.tile_tokens - 1) / base_.tile_tokens;
+    return (int)(((long long)g.tokens * (base_.Hq / base_.Hkv) + kWsRows - 1) / kWsRows);
   }
   int front() const { return groups_ * kGroupWords; }
 
   bicache_ctx* ctx_;
   WeightArgs base_;
+  CUtensorMap q_map_;
   bool tensor_, first_ = true;
   cudaStream_t stream_;
   int groups_ = 0, back_ = kParamWords;
@@ -258,7 +259,20 @@ int prefix_weights_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_
   a.Hq = cfg.num_q_heads;
   a.Hkv = cfg.num_kv_heads;
   a.D = cfg.head_dim;
-  WeightLaunches launches(ctx, a, ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT, static_cast<cudaStream_t>(stream_));
+  // a row tile of the tensor-core kernel holds the query heads of whole tokens
+  const bool tensor = ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && G <= wts::kRowTile;
+  CUtensorMap q_map;
+  std::memset(&q_map, 0, sizeof(q_map));
+  if (tensor) {
+    long long rows_total = 0;                                     // rows q is known to have
+    for (int i = 0; i < R; ++i)
+      if (prefix_id[i] >= 0 && seqlen[i] > 0) rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
+    a.tile_tokens = wts::kRowTile / G;
+    // box coordinates are 32-bit; without boxes every row tile is gathered
+    a.boxes = rows_total > 0 && rows_total < 0x7fffffffLL &&
+              encode_map(&q_map, q, rows_total, cfg.num_q_heads, q_row_stride, G, a.tile_tokens);
+  }
+  WeightLaunches launches(ctx, a, q_map, tensor, static_cast<cudaStream_t>(stream_));
   std::vector<WeightSeg> segs;
   for (const Run& r : runs) {
     segs.clear();
