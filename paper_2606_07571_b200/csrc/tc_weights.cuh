@@ -37,10 +37,7 @@ constexpr int kKeyBytes = kItemKeys * 128 * 2;   // 64 KB
 constexpr int kKSlots = 2, kQSlots = 3;
 constexpr int kSumWarps = 16;
 constexpr int kMmaWarpW = 16, kKeyWarp = 17, kRowWarp = 18;
-constexpr int kWtsThreads = 640;             // 20 warps: five to a scheduler
-constexpr int kLaunchRegs = 96;              // what the compiler gives 640 threads
-constexpr int kSumRegs = 104, kFetchRegs = 64;   // after the split, per thread
-static_assert(32 * kSumWarps * kSumRegs + 128 * kFetchRegs <= kWtsThreads * kLaunchRegs, "register split within the block's share");
+constexpr int kWtsThreads = 640;             // 20 warps: five to a scheduler, 96 registers a thread
 constexpr int kGroupKeys = 4 * kItemKeys / kSumWarps;      // keys of a sum warp
 constexpr int kLaneKeys = kGroupKeys / 32;                 // whose sums end in a lane
 constexpr int kMaxTerms = 48;                // row tiles a thread adds before the lanes are put together
@@ -116,6 +113,10 @@ __device__ __forceinline__ bool mbar_test(unsigned bar, unsigned parity) {
       : "memory");
   return ok != 0;
 }
+// bytes to come, without an arrival
+__device__ __forceinline__ void mbar_expect_tx(unsigned bar, unsigned bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -141,15 +142,12 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
   const unsigned k_ring = smem_u32(smem), q_ring = k_ring + kKSlots * kKeyBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
+  // Set-up, all of it side by side: thread 0 the barriers, warp 16 TMEM, warp 17 its own barriers and the first keys,
+  // every role its first item (the first reads of the parameters miss their cache), warps 18 and 19 the first
+  // log-sum-exps; then one barrier for the block.
   if (tid == 0) {
+    const int state = *reinterpret_cast<volatile int*>(status);
     sy->wait_cycles = wait_cycles;
-    if ((smem_u32(smem) & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
-    sy->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
-    sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
-    for (int i = 0; i < kKSlots; ++i) {
-      mbar_init(smem_u32(&sy->k_full[i]), 32);
-      mbar_init(smem_u32(&sy->k_free[i]), 1);
-    }
     for (int i = 0; i < kQSlots; ++i) {
       mbar_init(smem_u32(&sy->q_full[i]), 64);
       mbar_init(smem_u32(&sy->q_free[i]), 1 + kSumWarps);     // the MMAs; the warps that read the log-sum-exps
@@ -161,20 +159,27 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
     for (int i = 0; i < kSumWarps; ++i) mbar_init(smem_u32(&sy->hop[i >> 2][i & 3]), 1);
     mbar_init(smem_u32(&sy->drain), 1);
     fence_barrier_init();
+    if ((smem_u32(smem) & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
+    sy->dead = state != 0 || (smem_u32(smem) & 1023u) != 0 ? 1 : 0;
+    sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
   }
-  if (warp == kMmaWarpW) {
-    tmem_alloc(smem_u32(&sy->tmem_base), kTmemCols);
-    tmem_relinquish();
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&sy->tmem_base);
-  const bool dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
+  unsigned tmem = 0;
+  bool dead = false;
+  auto set_up = [&]() {
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    tmem = *reinterpret_cast<volatile unsigned*>(&sy->tmem_base);
+    dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
+  };
 
   if (warp < kSumWarps) {
     // ================================ exponentials and sums ================================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
+    {
+      const Item it = read_item(a, list, blockIdx.x);         // only brings the parameters into their cache
+      asm volatile("" ::"r"(it.hk), "r"(it.keys), "r"(it.tile_end));
+    }
+    set_up();
     const int lg = warp & 3, kg = warp >> 2;                  // lane group, key group
     const unsigned s_addr = tmem + kg * kGroupKeys + ((unsigned)(lg * 32) << 16);
     const float sl2 = a.scale * 1.4426950408889634f;
@@ -299,9 +304,12 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
     }
     tc_fence_before();
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFetchRegs));
+    Item it = read_item(a, list, blockIdx.x);
     if (warp == kMmaWarpW) {
       // ====================================== MMA issue ======================================
+      tmem_alloc(smem_u32(&sy->tmem_base), kTmemCols);
+      tmem_relinquish();
+      set_up();
       bool ok = !dead;
       unsigned qt = 0, kt = 0;                                // row tiles and key blocks consumed
       const unsigned el = elect_one() ? 1u : 0u;
@@ -310,7 +318,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       auto kstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 64); };
       auto qstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 1024); };
       for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-        const Item it = read_item(a, list, item);
+        if (item != blockIdx.x) it = read_item(a, list, item);
         if (it.tile_begin >= it.tile_end) continue;           // no rows: no keys are staged either
         const unsigned ks = kt % kKSlots;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_full[ks]), (kt / kKSlots) & 1, abort_flag));
@@ -345,16 +353,19 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       __syncwarp();
     } else if (warp == kKeyWarp) {
       // ======================================== keys =========================================
-      bool ok = !dead;
+      if (lane == 0) {
+        for (int i = 0; i < kKSlots; ++i) {
+          mbar_init(smem_u32(&sy->k_full[i]), 32);
+          mbar_init(smem_u32(&sy->k_free[i]), 1);
+        }
+        fence_barrier_init();
+      }
+      __syncwarp();
       unsigned kt = 0;
       int armed[kKSlots] = {-1, -1};                          // the last phase armed with copies, per slot
-      for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-        const Item it = read_item(a, list, item);
-        if (it.tile_begin >= it.tile_end) continue;
+      auto fetch = [&]() {
         const WeightGroup& g = weight_group(list, it.g);
         const unsigned ks = kt % kKSlots;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[ks]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
-        if (!ok) break;
         const int npages = (it.keys + kPageSize - 1) / kPageSize;          // up to 16
         const unsigned full = smem_u32(&sy->k_full[ks]);
         // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
@@ -368,9 +379,20 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           mbar_arrive(full);
         armed[ks] = (int)((kt / kKSlots) & 1);
         ++kt;
+      };
+      // the first item's keys need no free slot and nobody else's barriers
+      int item = blockIdx.x;
+      if (it.tile_begin < it.tile_end) fetch();
+      set_up();
+      bool ok = !dead;
+      for (item += gridDim.x; item < a.num_items && ok; item += gridDim.x) {
+        it = read_item(a, list, item);
+        if (it.tile_begin >= it.tile_end) continue;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[kt % kKSlots]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
+        if (ok) fetch();
       }
       // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-      if (!dead && (!ok || *abort_flag) && lane == 0) {
+      if ((!ok || *abort_flag) && lane == 0) {
         for (int s = 0; s < kKSlots; ++s)
           if (armed[s] >= 0)
             for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->k_full[s]), (unsigned)armed[s]); ++n) __nanosleep(256);
@@ -394,7 +416,6 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         tok_in[i] = r / G;
         head_in[i] = r - tok_in[i] * G;
       }
-      bool ok = !dead;
       unsigned qt = 0;
       int boxed[kQSlots] = {-1, -1, -1};                      // the last phase armed with a box, per slot
       int pending = -1;                                       // slot whose copies have not been announced yet
@@ -415,7 +436,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       };
       auto next_item = [&]() {                                // to the next item that has row tiles
         for (; item < a.num_items; item += gridDim.x) {
-          const Item it = read_item(a, list, item);
+          if (item != blockIdx.x) it = read_item(a, list, item);
           if (it.tile_begin >= it.tile_end) continue;
           const WeightGroup& g = weight_group(list, it.g);
           tile = it.tile_begin;
@@ -445,7 +466,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int tok = tok0 + tok_in[i];
-          src[i] = 0;
+          src[i] = -1;
           lse[i] = INFINITY;
           if (tok_in[i] < T && tok <= last) {
             while (tok >= run_end[i]) read_run(i, run[i] + 1);
@@ -458,16 +479,18 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       };
       next_item();
       if (item < a.num_items) look_up();
+      set_up();
+      bool ok = !dead;
       while (item < a.num_items && ok) {
         const int box_head = hk * G, box_first = (int)box_row;
         const bool boxes = one_run;
-        float nl[2];
-        unsigned live[2];
+        float row_lse[2];
+        unsigned rows[2];                                     // the rows that exist
         long long from[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          nl[i] = isinf(lse[i]) ? -INFINITY : lse[i] * -1.4426950408889634f;
-          live[i] = __ballot_sync(0xffffffffu, nl[i] != -INFINITY);
+          row_lse[i] = lse[i];
+          rows[i] = __ballot_sync(0xffffffffu, src[i] >= 0);
           from[i] = src[i];
         }
         if (++tile >= tile_end) {
@@ -486,32 +509,38 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         ok = __all_sync(0xffffffffu, mbar_wait(q_free, free_parity, abort_flag));
         if (!ok) break;
         const unsigned dst = q_ring + slot * kTileBytes;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) sy->neg_lse2[slot][w * 64 + i * 32 + lane] = nl[i];
         if (boxes) {
           // rows past the tile's last token come along (or as zeros, past the tensor): they add nothing
           if (lane == 0) {
-            mbar_arrive_expect_tx(q_full, (unsigned)(T * G * 128));         // each warp fetches one half of the dims
+            mbar_expect_tx(q_full, (unsigned)(T * G * 128));                // each warp fetches one half of the dims
             tma_load_3d(dst + w * 16384, &q_map, w * 64, box_head, box_first, q_full);
             boxed[slot] = (int)(((qt - 1) / kQSlots) & 1);
-          } else {
-            mbar_arrive(q_full);
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (rows[i] == 0u) continue;                      // rows that do not exist may hold anything
+            const int r0 = w * 64 + i * 32;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int r = 2 * j + (lane >> 4);
+              const long long s = __shfl_sync(0xffffffffu, from[i], r);
+              const bool exists = (rows[i] >> r) & 1u;
+              cp_async16(dst + r0 * 128 + (j >> 2) * 1024 + chunk_off[j & 3], a.q + (exists ? s : 0) + c16 * 16,
+                         exists ? 16u : 0u);
+            }
+          }
+          cp_async_commit();
+        }
+        // the log-sum-exps arrive while the rows are on their way
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          sy->neg_lse2[slot][w * 64 + i * 32 + lane] = isinf(row_lse[i]) ? -INFINITY : row_lse[i] * -1.4426950408889634f;
+        if (boxes) {
+          __syncwarp();                                       // lane 0 has announced the bytes
+          mbar_arrive(q_full);
           continue;
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (live[i] == 0u) continue;                        // rows that add nothing may hold anything
-          const int r0 = w * 64 + i * 32;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int r = 2 * j + (lane >> 4);
-            const long long s = __shfl_sync(0xffffffffu, from[i], r);
-            cp_async16(dst + r0 * 128 + (j >> 2) * 1024 + chunk_off[j & 3], a.q + s + c16 * 16,
-                       (live[i] >> r) & 1u ? 16u : 0u);
-          }
-        }
-        cp_async_commit();
         if (pending >= 0) {
           cp_async_wait<1>();
           announce();
@@ -538,17 +567,10 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 }
 
 inline cudaError_t configure_tc_weights() {
-  auto configure = [](auto* kernel) {
-    cudaFuncAttributes attr;
-    cudaError_t e = cudaFuncGetAttributes(&attr, kernel);
-    // the register split must not ask for more than the block was launched with: it would wait for good
-    if (e == cudaSuccess && attr.numRegs < wts::kLaunchRegs) e = cudaErrorInvalidConfiguration;
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wts::kSmemBytes);
-    return e;
-  };
-  cudaError_t e = configure(tc_weights_kernel<kParamWordsSmall>);
-  if (e == cudaSuccess) e = configure(tc_weights_kernel<kParamWordsMid>);
-  if (e == cudaSuccess) e = configure(tc_weights_kernel<kParamWords>);
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsSmall>, attr, wts::kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsMid>, attr, wts::kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWords>, attr, wts::kSmemBytes);
   return e;
 }
 

@@ -85,32 +85,39 @@ class WeightLaunches {
     const int block_keys = tensor_ ? wts::kItemKeys : kWsKeys;
     WeightGroup* g = reinterpret_cast<WeightGroup*>(list_);
     int max_tiles = 1, max_m = 1;
-    long long base_items = 0;
+    // long groups first: the short items of the others even out what these leave
+    std::stable_sort(g, g + groups_, [&](const WeightGroup& x, const WeightGroup& y) { return tiles_of(x) > tiles_of(y); });
     for (int i = 0; i < groups_; ++i) {
       g[i].key_blocks = (g[i].m + block_keys - 1) / block_keys;
-      base_items += (long long)g[i].key_blocks * a.Hkv;
       max_tiles = std::max(max_tiles, tiles_of(g[i]));
       max_m = std::max(max_m, g[i].m);
     }
-    // How many row tiles an item covers.  Fewer tiles make more items, which fill the SMs evenly, but every
-    // item costs its prologue (about a tile) and more than one range per key the second kernel (about three).
-    // Counted in tiles: the waves of items for one group, the work per SM and half an item for several.
+    // How many row tiles an item covers at most.  Fewer tiles make more items, which fill the SMs evenly, but every
+    // item costs its start and the sum over its lanes (about two tiles, 2.5 us) and more than one range per key the
+    // second kernel (about three).  Counted in tiles: the fullest SM, items being dealt out in turn.
     const int slots = tensor_ ? ctx_->sm_count : 2 * ctx_->sm_count;
+    const int choices = std::min(max_tiles, std::max(4, 128 / groups_));
+    auto splits_of = [&](int tiles, int tps) { return std::max(1, (tiles + tps - 1) / tps); };
+    std::vector<int> load(slots);
     int best_tps = max_tiles;
-    double best = 1e300;
-    for (int s = 1; s <= std::min(max_tiles, 32); ++s) {
+    long long best = 0x7fffffffffffffffLL;
+    for (int s = 1; s <= std::min(choices, 32); ++s) {
       const int tps = (max_tiles + s - 1) / s;
-      long long items = 0, part = 0;
-      double work = 0;
+      long long part = 0, even = 0;
+      int at = 0;
+      std::fill(load.begin(), load.end(), 0);
       for (int i = 0; i < groups_; ++i) {
-        const int tiles = tiles_of(g[i]), sp = std::max(1, (tiles + tps - 1) / tps);
-        items += (long long)g[i].key_blocks * a.Hkv * sp;
-        work += (double)g[i].key_blocks * a.Hkv * (tiles + sp);
+        const int tiles = tiles_of(g[i]), sp = splits_of(tiles, tps), cost = (tiles + sp - 1) / sp + 2;
+        const long long items = (long long)g[i].key_blocks * a.Hkv * sp;
+        even += items / slots * cost;
+        for (int left = (int)(items % slots); left > 0; --left) {
+          load[at] += cost;
+          at = at + 1 == slots ? 0 : at + 1;
+        }
         if (sp > 1) part += (long long)sp * a.Hkv * g[i].m;
       }
       if (part > ctx_->part_capacity_rowheads * ctx_->cfg.head_dim) break;
-      const double waves = (double)((items + slots - 1) / slots);
-      const double c = (groups_ == 1 ? waves * (tps + 1) : work / std::min<double>(slots, items) + 0.5 * tps) + (s > 1 ? 3.0 : 0.0);
+      const long long c = even + *std::max_element(load.begin(), load.end()) + (part > 0 ? 3 : 0);
       if (c < best) {
         best = c;
         best_tps = tps;
@@ -119,8 +126,9 @@ class WeightLaunches {
     long long item = 0, part = 0;
     bool split = false;
     for (int i = 0; i < groups_; ++i) {
-      g[i].tiles_per_split = best_tps;
-      g[i].splits = std::max(1, (tiles_of(g[i]) + best_tps - 1) / best_tps);
+      const int tiles = tiles_of(g[i]);
+      g[i].splits = splits_of(tiles, best_tps);
+      g[i].tiles_per_split = (tiles + g[i].splits - 1) / g[i].splits;
       g[i].item_begin = (int)item;
       item += (long long)g[i].key_blocks * a.Hkv * g[i].splits;
       g[i].part_off = (int)part;
