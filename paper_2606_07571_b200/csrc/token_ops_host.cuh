@@ -466,7 +466,7 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
   if (rows == 0) return BICACHE_OK;
   DeviceGuard guard(ctx->cfg.device);
   const int per_block = kRopeThreads / a.pairs;
-  const int blocks = (int)std::min<long long>((rows + per_block - 1) / per_block, 8LL * ctx->sm_count);
+  const int blocks = (int)std::min<long long>((rows + per_block - 1) / per_block, 2LL * ctx->sm_count);
   rope_table_kernel<<<blocks, kRopeThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, rows, reinterpret_cast<float2*>(table));
   ctx->launches++;
   return cuda_status(ctx, cudaGetLastError(), "rope_table");

@@ -1,7 +1,7 @@
 """GPU parity of the rotary calls against the fp64 oracle.
 
-Tolerance: the part of a turn enters as fp32 in [-1/8, 1/8) turn (2^-27 half turns, 2.4e-8 rad), sincospif is good to 2
-units in the last place (2^-23 below 1): cos and sin are off by at most E = 1.5e-7.  The factor and the products
+Tolerance: the part of a turn enters as fp32 in [-1/8, 1/8) turn (2^-27 half turns, 2.4e-8 rad); cosine and sine are good
+to 2 units in the last place (2^-23 below 1): they are off by at most E = 1.5e-7.  The factor and the products
 and their sum are four fp32 roundings of 2^-24, each at most (|a| + |b|) scale.  One rounding to the type follows:
 half a step, eps / 2 of the value."""
 import numpy as np
