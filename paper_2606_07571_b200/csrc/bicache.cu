@@ -1183,21 +1183,35 @@ int32_t bicache_read_prefix_layer(bicache_ctx* ctx, int32_t prefix_id, int32_t l
   if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out))
     return fail(ctx, BICACHE_ERR_INVALID, "bad k/v pointer");
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const int need = (int)e.pages.size();
-  cudaError_t ce =
-      cudaMemcpyAsync(ctx->d_put_pages, pages_of(e, layer).data(), sizeof(int) * need, cudaMemcpyHostToDevice, stream);
-  if (ce == cudaSuccess && e.m > 0) {
-    const int chunks_per_row = cfg.head_dim * ctx->esize / 16;
-    const long long total = (long long)e.m * cfg.num_kv_heads * chunks_per_row;
-    const int threads = 256;
-    const int blocks = (int)std::min<long long>((total + threads - 1) / threads, (long long)ctx->sm_count * 16);
-    const PoolView pv = pool_view(ctx);
-    gather_prefix_kernel<<<blocks, threads, 0, stream>>>(
-        pv.k + ctx->layer_off[layer], pv.v + ctx->layer_off[layer],
-        static_cast<char*>(k_out), static_cast<char*>(v_out), ctx->d_put_pages, e.m, cfg.num_kv_heads,
-        chunks_per_row, kv_row_stride * ctx->esize, pv.page_bytes, pv.swizzled);
+  const std::vector<int32_t>& pages = pages_of(e, layer);
+  const int need = (int)pages.size();
+  const int chunks_per_row = cfg.head_dim * ctx->esize / 16;
+  const long long total = (long long)e.m * cfg.num_kv_heads * chunks_per_row;
+  const int threads = 256;
+  const int blocks = (int)std::min<long long>((total + threads - 1) / threads, (long long)ctx->sm_count * 16);
+  const PoolView pv = pool_view(ctx);
+  cudaError_t ce = cudaSuccess;
+  if (e.m > 0 && need <= kParamWords) {                 // the page list fits the launch parameters
+    int list[kParamWords];
+    std::memcpy(list, pages.data(), sizeof(int) * need);
+    with_param_list(list, need, [&](const auto& params) {
+      read_layer_kernel<<<blocks, threads, 0, stream>>>(
+          pv.k + ctx->layer_off[layer], pv.v + ctx->layer_off[layer], static_cast<char*>(k_out),
+          static_cast<char*>(v_out), e.m, cfg.num_kv_heads, chunks_per_row, kv_row_stride * ctx->esize, pv.page_bytes,
+          pv.swizzled, params);
+    });
     ctx->launches++;
     ce = cudaGetLastError();
+  } else if (e.m > 0) {
+    ce = cudaMemcpyAsync(ctx->d_put_pages, pages.data(), sizeof(int) * need, cudaMemcpyHostToDevice, stream);
+    if (ce == cudaSuccess) {
+      gather_prefix_kernel<<<blocks, threads, 0, stream>>>(
+          pv.k + ctx->layer_off[layer], pv.v + ctx->layer_off[layer],
+          static_cast<char*>(k_out), static_cast<char*>(v_out), ctx->d_put_pages, e.m, cfg.num_kv_heads,
+          chunks_per_row, kv_row_stride * ctx->esize, pv.page_bytes, pv.swizzled);
+      ctx->launches++;
+      ce = cudaGetLastError();
+    }
   }
   if (ce != cudaSuccess) return fail(ctx, BICACHE_ERR_CUDA, std::string("read_prefix_layer: ") + cudaGetErrorString(ce));
   return BICACHE_OK;

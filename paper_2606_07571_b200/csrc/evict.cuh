@@ -524,6 +524,29 @@ compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_consta
   }
 }
 
+// gather_prefix_kernel (the layer read-back) with the page list in the parameters: no copy before the launch, which
+// is what a read-back of a short prefix otherwise waits for (7.2 us of host time, 4.5 without).
+template <int kWords>
+__global__ void __launch_bounds__(kCompactThreads)
+read_layer_kernel(const char* __restrict__ pool_k, const char* __restrict__ pool_v, char* __restrict__ dst_k,
+                  char* __restrict__ dst_v, int m, int num_kv_heads, int chunks_per_row, long long dst_row_stride_bytes,
+                  int page_bytes, int swizzled, const __grid_constant__ ParamList<kWords> pages) {
+  const long long total = (long long)m * num_kv_heads * chunks_per_row;
+  const int row_bytes = chunks_per_row * 16;
+  for (long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x; idx < total;
+       idx += (long long)gridDim.x * blockDim.x) {
+    long long rem = idx;
+    const int c16 = (int)(rem % chunks_per_row); rem /= chunks_per_row;
+    const int hk = (int)(rem % num_kv_heads); rem /= num_kv_heads;
+    const int t = (int)rem;
+    const long long po = ((long long)pages.w[t / kPageSize] * num_kv_heads + hk) * page_bytes +
+                         page_chunk_offset(swizzled != 0, t % kPageSize, c16, row_bytes);
+    const long long d = (long long)t * dst_row_stride_bytes + (long long)hk * row_bytes + c16 * 16;
+    *reinterpret_cast<uint4*>(dst_k + d) = *reinterpret_cast<const uint4*>(pool_k + po);
+    *reinterpret_cast<uint4*>(dst_v + d) = *reinterpret_cast<const uint4*>(pool_v + po);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // bicache_prefix_weights.  For every cached key t of prefix g and KV head j
 //   out[g][j][t] = decay in[g][j][t] + sum over the rows a and query heads h of the group
