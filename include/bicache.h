@@ -376,7 +376,7 @@ int32_t bicache_prefix_weights(bicache_ctx* ctx, int32_t layer, int32_t R, const
  * rows) that stay: the first protect_first and the last protect_last of them always, then the largest
  * scores, equal scores by lower index; a NaN ranks as -inf, -0 equals +0.  idx_out: device int32 [rows][keep]
  * (idx_row_stride elements between rows), ascending.  Protected ends longer than the row are cut to it.
- * INVALID for keep outside 0 .. n, for fewer than the protected tokens, for bad strides or null pointers.
+ * INVALID for keep outside 0 .. n, n above 2^30, fewer kept than protected tokens, bad strides, null pointers.
  * rows, n and keep may be 0 (nothing is written). */
 int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const float* scores,
                               int64_t score_row_stride, int32_t keep, int32_t protect_first, int32_t protect_last,
@@ -388,7 +388,7 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
  * every i below keep, which is the destination's length.  idx: device int32; a stride of 0 gives all layers or all heads one
  * list; any order, repeats allowed.  Bit-exact copies; unused slots of the last page become zero.  An index
  * outside 0 .. (source length - 1) gives a zero token and makes bicache_device_status report INVALID until
- * it is cleared.  NOTFOUND for an unknown or evicted id; INVALID for src_id == dst_id, a keep that is not
+ * it is cleared; like any device status it stops the tensor-core calls of the context until then.  NOTFOUND for an unknown or evicted id; INVALID for src_id == dst_id, a keep that is not
  * the destination's length, layers that either prefix does not own, negative strides. */
 int32_t bicache_compact_prefix(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_t first_layer,
                                int32_t num_layers, int32_t keep, const int32_t* idx, int64_t idx_layer_stride,

@@ -592,6 +592,7 @@ struct WeightArgs {
   int page_bytes, swizzled;
   int Hq, Hkv, D;
   int num_groups, num_items;
+  int max_item_tiles;           // row tiles of the longest item
   int tile_tokens;              // tensor-core form: tokens of a row tile (as many as give at most 128 rows)
   int boxes;                    // tensor-core form: the tensor map of q is valid
 };

@@ -6,7 +6,7 @@
 // 64 of the keys, for each of which it keeps a running sum in a register; the sum over the rows of a tile, across
 // the lanes, is put off until up to 48 tiles have been added, and then costs 62 shuffles for 64 keys.  (With the
 // keys on the lanes the sum over rows needs no shuffles, but every log-sum-exp is a shared-memory operand of
-// every thread: that form ran at 4.6 ms where this one takes 4.1, 32 requests of 1024 rows and 28 heads over 16,384 keys.)
+// every thread: that form ran at 4.6 ms where this one took 4.1, 32 requests of 1024 rows and 28 heads over 16,384 keys.)
 //
 // What bounds it: one exponential per (row, key) against 256 flops of the product.  An SM computes 16
 // exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a tile of 128 x
@@ -579,8 +579,10 @@ cudaError_t launch_tc_weights(const WeightArgs& a, const CUtensorMap& q_map, con
                               int sm_count, long long wait_cycles, cudaStream_t stream) {
   if (a.num_items <= 0) return cudaSuccess;
   const int grid = a.num_items < sm_count ? a.num_items : sm_count;
-  tc_weights_kernel<kWords><<<grid, wts::kWtsThreads, wts::kSmemBytes, stream>>>(
-      a, q_map, status, wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, list);
+  // the keys of the item after next wait for a whole item: about 2,500 cycles a row tile, so the default budget
+  // grows with the longest item
+  const long long budget = wait_cycles > 0 ? wait_cycles : tc::kWaitCycles + 20000LL * a.max_item_tiles;
+  tc_weights_kernel<kWords><<<grid, wts::kWtsThreads, wts::kSmemBytes, stream>>>(a, q_map, status, budget, list);
   return cudaGetLastError();
 }
 

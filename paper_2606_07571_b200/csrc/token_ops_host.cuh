@@ -139,6 +139,7 @@ class WeightLaunches {
     }
     a.num_groups = groups_;
     a.num_items = (int)item;
+    a.max_item_tiles = best_tps;
     // the records from the end follow the groups: the list is as short as what it holds
     const int gap = back_ - front();
     for (int i = 0; i < groups_; ++i) {
@@ -508,7 +509,7 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
                               int64_t idx_row_stride, void* stream) {
   return guarded([&]() -> int32_t {
     if (!ctx) return BICACHE_ERR_INVALID;
-    if (rows < 0 || rows > 0x7fffffffLL || n < 0 || keep < 0 || keep > n || protect_first < 0 || protect_last < 0)
+    if (rows < 0 || rows > 0x7fffffffLL || n < 0 || n > (1 << 30) || keep < 0 || keep > n || protect_first < 0 || protect_last < 0)
       return fail(ctx, BICACHE_ERR_INVALID, "bad row count, length, keep or protected count");
     SelectArgs a;
     a.first = std::min(protect_first, n);

@@ -112,7 +112,8 @@ MHA, GQA7, GQA3, MQA = (4, 4, 128), (14, 2, 128), (6, 2, 128), (16, 1, 128)
     (MHA, [1], [[1]]), (GQA7, [16], [[1]]), (MQA, [17], [[3]]), (GQA3, [128], [[43]]), (MHA, [129], [[128]]),
     (GQA7, [255], [[1, 0, 36]]), (GQA3, [256], [[129, 1]]), (MQA, [257], [[5, 16, 2]]),
     (MHA, [100, 300, 15], [[7, 1], [130, 64], [200]]), (GQA7, [513, 40], [[9], [18, 19, 0, 21]]),
-    (MHA, [64, 31], [[0, 0], [5]]), (MQA, [1023], [[300]]),
+    (MHA, [64, 31], [[0, 0], [5]]), (MQA, [1023], [[300]]), ((130, 1, 128), [70], [[3]]), ((128, 1, 128), [40], [[2, 1]]),
+    ((65, 1, 128), [300], [[2, 9]]), ((10, 2, 128), [260], [[100, 3, 77]]), ((48, 1, 128), [20], [[40]]),
 ])
 @pytest.mark.parametrize("path", [binding.PATH_AUTO, binding.PATH_SIMT])
 def test_weights(heads, prefixes, suffixes, path):

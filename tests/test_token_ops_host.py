@@ -95,7 +95,7 @@ def test_select_refusals(lib, ctx):
     assert call(rows=1, ss=0, xs=0) == b.ERR_UNSUPPORTED                       # strides of a single row are not read
     assert call(keep=10, first=50, last=50, xs=10) == b.ERR_UNSUPPORTED        # protected ends cut to the row
     assert call(rows=0, scores=None, idx=None) == b.ERR_UNSUPPORTED
-    for bad in (dict(rows=-1), dict(rows=2 ** 31), dict(n=-1), dict(keep=-1), dict(keep=11), dict(first=-1), dict(last=-1),
+    for bad in (dict(rows=-1), dict(rows=2 ** 31), dict(n=-1), dict(n=2 ** 30 + 1, ss=2 ** 31, keep=4), dict(keep=-1), dict(keep=11), dict(first=-1), dict(last=-1),
                 dict(first=3, last=2), dict(keep=9, first=50, last=50), dict(scores=None), dict(idx=None),
                 dict(scores=ODD), dict(idx=ODD), dict(ss=9), dict(xs=3), dict(c=None)):
         assert call(**bad) == b.ERR_INVALID, bad
