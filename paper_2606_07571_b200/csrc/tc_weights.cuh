@@ -10,14 +10,15 @@
 //
 // What bounds it: one exponential per (row, key) against 256 flops of the product.  An SM computes 16
 // exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a tile of 128 x
-// 256 takes 2048 cycles of the one and 1024 of the other.  A thread's 64 sums leave no registers to
-// hide a polynomial's constants and latency behind: sending two of every eight pairs to the FMA pipe, which is
-// faster on its own (116 cycles against 135 for 16 keys of four warps), made the kernel 8 % slower.
+// 256 takes 2048 cycles of the one and 1024 of the other; it takes 2330 (4.1 ms, 87 % of the unit's rate).  A
+// polynomial on the FMA pipe for two of every eight pairs, which is faster by itself (116 cycles against 135 for 16
+// keys of four warps), gained nothing here: the packed instructions take two issue slots each, and with the
+// loaders' warps beside them the schedulers are full (4.2 ms; without the register split that it needs, 5.8).
 // With few rows the kernel is bound by reading the keys.
 //
-// Roles: warps 0-15 exponentials and sums (warp w: lanes 32 (w & 3) .., keys 64 (w >> 2) ..), warp 16 issues the MMAs
-// and owns TMEM (two S buffers of 256 columns), warp 17 stages keys (pages, 4 KB bulk copies: a page already is the
-// operand image), warps 18 and 19 fetch the query rows with their log-sum-exps.  A row tile is the G query heads
+// Roles: warps 0-15 exponentials and sums (warp w: lanes 32 (w & 3) .., keys 64 (w >> 2) ..), warps 16 and 17
+// fetch the query rows with their log-sum-exps, warp 18 issues the MMAs and owns TMEM (two S buffers of 256 columns),
+// warp 19 stages keys (pages, 4 KB bulk copies: a page already is the operand image).  A row tile is the G query heads
 // of as many tokens as fit 128 rows: if its tokens are one run of rows, two TMA boxes (64 dims, G heads, the
 // tokens) are the tile; a tile that spans the end of one request and the start of the next is gathered with
 // 16-byte copies.  Keys have two slots of 256 (the next item's are fetched while this one's are used), row tiles a
@@ -36,7 +37,7 @@ constexpr int kRowTile = 128;
 constexpr int kKeyBytes = kItemKeys * 128 * 2;   // 64 KB
 constexpr int kKSlots = 2, kQSlots = 3;
 constexpr int kSumWarps = 16;
-constexpr int kMmaWarpW = 16, kKeyWarp = 17, kRowWarp = 18;
+constexpr int kRowWarp = 16, kMmaWarpW = 18, kKeyWarp = 19;
 constexpr int kWtsThreads = 640;             // 20 warps: five to a scheduler, 96 registers a thread
 constexpr int kGroupKeys = 4 * kItemKeys / kSumWarps;      // keys of a sum warp
 constexpr int kLaneKeys = kGroupKeys / 32;                 // whose sums end in a lane
@@ -142,8 +143,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
   const unsigned k_ring = smem_u32(smem), q_ring = k_ring + kKSlots * kKeyBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  // Set-up, all of it side by side: thread 0 the barriers, warp 16 TMEM, warp 17 its own barriers and the first keys,
-  // every role its first item (the first reads of the parameters miss their cache), warps 18 and 19 the first
+  // Set-up, all of it side by side: thread 0 the barriers, warp 18 TMEM, warp 19 its own barriers and the first keys,
+  // every role its first item (the first reads of the parameters miss their cache), warps 16 and 17 the first
   // log-sum-exps; then one barrier for the block.
   if (tid == 0) {
     const int state = *reinterpret_cast<volatile int*>(status);
@@ -185,6 +186,9 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
     const float sl2 = a.scale * 1.4426950408889634f;
     const unsigned long long sl2_2 = pack2(sl2, sl2);
     bool ok = !dead;
+    // lanes that have a row in every full tile (128 may not be a multiple of G); what the others add up is dropped
+    const bool has_row = lg * 32 + lane < a.tile_tokens * (a.Hq / a.Hkv);
+    const unsigned full = __ballot_sync(0xffffffffu, has_row);
     unsigned slot = 0, slot_parity = 0, b = 0, b_parity = 0;  // row tile ring and S buffer of the next tile
     unsigned handed = 0;                                      // items whose sums went from group to group
     const unsigned q_full0 = smem_u32(&sy->q_full[0]), q_free0 = smem_u32(&sy->q_free[0]);
@@ -211,8 +215,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           tc_fence_after();
           const bool adds = nl != -INFINITY;
           const unsigned live = __ballot_sync(0xffffffffu, adds);
-          const bool computes = active && live != 0u;
-          if (computes) {
+          if (active && live != 0u) {
             const unsigned long long nl2 = pack2(nl, nl);
             const unsigned s_tile = s_addr + b * kItemKeys;
             // without branches inside: the compiler overlaps the end of one run of 16 keys with the start of the next
@@ -236,7 +239,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
                 }
               }
             };
-            if (live == 0xffffffffu) sum_tile(std::false_type()); else sum_tile(std::true_type());
+            if (live == full) sum_tile(std::false_type()); else sum_tile(std::true_type());
           }
           tc_fence_before();
           if (lane == 0) mbar_arrive(s_free0 + b * 8);
@@ -252,7 +255,11 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           // half; lane l ends with the keys from kLaneKeys * l on.
           float v[kGroupKeys];
 #pragma unroll
-          for (int p = 0; p < kGroupKeys / 2; ++p) unpack2(acc[p], v[2 * p], v[2 * p + 1]);
+          for (int p = 0; p < kGroupKeys / 2; ++p) {
+            unpack2(acc[p], v[2 * p], v[2 * p + 1]);
+            v[2 * p] = has_row ? v[2 * p] : 0.f;
+            v[2 * p + 1] = has_row ? v[2 * p + 1] : 0.f;
+          }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) {
             const bool upper = (lane & o) != 0;
@@ -472,7 +479,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
             while (tok >= run_end[i]) read_run(i, run[i] + 1);
             const long long row = run_row[i] + tok;
             const int h = hk * G + head_in[i];
-            src[i] = (row * a.q_stride + (long long)h * 128) * 2;
+            src[i] = one_run ? 0 : (row * a.q_stride + (long long)h * 128) * 2;
             lse[i] = a.lse[row * a.Hq + h];
           }
         }
