@@ -268,10 +268,21 @@ select_tokens_kernel(SelectArgs a) {
     while (span > 0 && inside > k && inside > kSelRanked) {
       ++pass;
       unsigned least = 0xffffffffu, most = 0u;
-      each_inside([&](unsigned e) {
-        least = min(least, e);
-        most = max(most, e);
-      });
+#pragma unroll 2
+      for (int v = qa + tid; v < qb; v += kSelThreads) {               // without branches: many are inside
+        const uint4 q = quad_at(v);
+        const unsigned e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool in = e[j] - base <= span;
+          least = min(least, in ? e[j] : 0xffffffffu);
+          most = max(most, in ? e[j] : 0u);
+        }
+      }
+      if (edge >= 0 && edge_key - base <= span) {
+        least = min(least, edge_key);
+        most = max(most, edge_key);
+      }
       least = block_min(least, warp_lo);
       most = ~block_min(~most, warp_hi);
       if (parts > 1) {
