@@ -364,7 +364,8 @@ int32_t bicache_build_depth_table(const int32_t* ratio_idx, const int32_t* depth
  * 0 (may be scores_out itself, else must not overlap it; NULL allowed only with decay 0).  A prefix whose
  * requests are all empty gets decay * in.  Elements of other tokens are left as they are.
  * Sums in fp32 with the rounding error carried along (bf16, head_dim 128) or in fp64, in a fixed order: the
- * same call gives the same bits.  Uses the context's workspace as scratch.  Errors as for bicache_attend;
+ * same call gives the same bits.  Uses the context's workspace as scratch: two calls, or replays of
+ * graphs that hold such calls, must not overlap (one stream per context at a time).  Errors as for bicache_attend;
  * INVALID also for decay or softmax_scale that is not finite. */
 int32_t bicache_prefix_weights(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
                                const int64_t* row_off, const int32_t* seqlen, const void* q, int64_t q_row_stride,
@@ -424,7 +425,8 @@ int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, 
  * q, q_out: device [rows][Hq][D] of the context's dtype, k, k_out [rows][Hkv][D]; row strides in elements.
  * A tensor may be rotated in place (the same pointer and stride); other overlap is not allowed.  q or k may be
  * NULL together with its output (that tensor is left out).  INVALID for an odd rot_dim or one outside 2 .. D,
- * frequencies that are not finite or beyond +-2^20, attention_scale not finite or 0, bad pointers or strides. */
+ * frequencies that are not finite or beyond +-2^20, attention_scale (or its inverse, where that is the factor) not
+ * finite or 0, one output for both tensors, bad pointers or strides. */
 int32_t bicache_rope(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
                      int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale,
                      const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride,

@@ -1183,6 +1183,7 @@ int32_t bicache_read_prefix_layer(bicache_ctx* ctx, int32_t prefix_id, int32_t l
   if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out))
     return fail(ctx, BICACHE_ERR_INVALID, "bad k/v pointer");
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  DeviceGuard guard(cfg.device);
   const std::vector<int32_t>& pages = pages_of(e, layer);
   const int need = (int)pages.size();
   const int chunks_per_row = cfg.head_dim * ctx->esize / 16;

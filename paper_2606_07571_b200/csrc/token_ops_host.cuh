@@ -396,6 +396,7 @@ bool rope_angles(RopeAngles* a, int32_t rot_dim, const double* inv_freq, const i
   a->positions = positions;
   a->position0 = position0;
   a->scale = inverse ? 1.f / attention_scale : attention_scale;
+  if (!std::isfinite(a->scale)) return false;                     // the inverse of a subnormal scale
   a->negate = inverse ? 1 : 0;
   return true;
 }
@@ -423,6 +424,7 @@ int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t 
   const int64_t in_strides[2] = {q_row_stride, k_row_stride}, out_strides[2] = {q_out_row_stride, k_out_row_stride};
   const int heads[2] = {cfg.num_q_heads, cfg.num_kv_heads};
   if (rows > 0 && !q && !k && !q_out && !k_out) return fail(ctx, BICACHE_ERR_INVALID, "nothing to rotate");
+  if (rows > 0 && q_out && q_out == k_out) return fail(ctx, BICACHE_ERR_INVALID, "queries and keys have one output");
   for (int i = 0; i < 2 && rows > 0; ++i) {              // no rows: an empty tensor has no address
     if (!ins[i] != !outs[i]) return fail(ctx, BICACHE_ERR_INVALID, "a tensor without its output, or the reverse");
     if (!ins[i]) continue;

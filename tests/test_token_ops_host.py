@@ -135,3 +135,16 @@ def test_rope_refusals(lib, ctx):
     for bad in (dict(rows=-1), dict(rot=0), dict(rot=9), dict(rot=258), dict(f=None), dict(f=(float("nan"),) * 32),
                 dict(scale=0.0), dict(t=None), dict(t=A4), dict(pos=ODD), dict(c=None)):
         assert table(**bad) == b.ERR_INVALID, bad
+
+
+def test_rope_refuses_one_output_for_both_tensors_and_an_infinite_inverse_scale(lib, ctx):
+    f = (C.c_double * 64)(*[0.5] * 64)
+
+    def call(inverse=0, scale=1.0, qo=A16, ko=A16 * 2, rows=3):
+        return lib.bicache_rope(ctx, rows, None, 0, 128, 0, inverse, f, scale, A16 * 3, 512, qo, 512, A16 * 4, 256, ko, 512, None)
+    assert call() == b.ERR_UNSUPPORTED
+    assert call(ko=A16) == b.ERR_INVALID
+    assert call(ko=A16, rows=0) == b.ERR_UNSUPPORTED             # no rows: the address is not used
+    # 2^-140: a subnormal whose reciprocal is not finite
+    assert call(scale=2.0 ** -140) == b.ERR_UNSUPPORTED
+    assert call(inverse=1, scale=2.0 ** -140) == b.ERR_INVALID
