@@ -1,6 +1,7 @@
 // Token eviction from a stored prefix: the choice of the tokens to keep, their copy into a shorter prefix,
 // and the CUDA-core form of the accumulated attention weights (fp32, head dims other than 128).
 #pragma once
+#include <algorithm>
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include "common.cuh"
@@ -55,6 +56,7 @@ constexpr int kSelRanked = 256;                 // at most so many are ranked di
 constexpr int kSelStaged = 49152;               // scores of a block's part kept in shared memory (192 KB)
 constexpr int kSelRunQuads = 5;                 // scores / 4 of a thread's run: odd, so that runs start on different banks
 constexpr int kSelMaxCluster = 8;
+static_assert(kSelStaged < 65536 && 4 * kSelRunQuads * kSelThreads < 65536, "two counts in 32 bits");
 static_assert(kSelBins == 2 * kSelThreads && kSelWarps == 32, "two bins to a thread, a warp over the warps' results");
 
 // NaN counts as -inf; -0 as +0; larger score <=> larger integer.  Never 0 nor 0xffffffff.
@@ -69,32 +71,36 @@ struct SelectArgs {
   int* idx;
   long long idx_stride;
   int n, keep, first, last;                     // protected: t < first, t >= n - last; first + last <= min(n, keep)
+  int rows, ahead;                              // rows that the GPU works on at a time
 };
 
-// exclusive prefix sum of v over the block, in thread order; *total receives the sum.  Two barriers.
-__device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
+// exclusive prefix sum of v over the block, in thread order; *total receives the sum.  One barrier; warp_sums may be
+// written again after the next.
+__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned* warp_sums, unsigned* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int incl = v;
+  unsigned incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, incl, o);
+    const unsigned x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  const int w = warp_sums[lane];
-  const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+  const unsigned w = warp_sums[lane];
+  const unsigned before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u);
   *total = __reduce_add_sync(0xffffffffu, w);
-  __syncthreads();                              // warp_sums may be written again
   return before + incl - v;
 }
 
-// smallest v of the block.  One barrier; warp_mins may be written again after the next.
-__device__ __forceinline__ unsigned block_min(unsigned v, unsigned* warp_mins) {
-  v = __reduce_min_sync(0xffffffffu, v);
-  if ((threadIdx.x & 31) == 0) warp_mins[threadIdx.x >> 5] = v;
+// smallest lo and largest hi of the block.  One barrier; ranges may be written again after the next.
+__device__ __forceinline__ void block_range(unsigned& lo, unsigned& hi, uint2* ranges) {
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if ((threadIdx.x & 31) == 0) ranges[threadIdx.x >> 5] = make_uint2(lo, hi);
   __syncthreads();
-  return __reduce_min_sync(0xffffffffu, warp_mins[threadIdx.x & 31]);
+  const uint2 r = ranges[threadIdx.x & 31];
+  lo = __reduce_min_sync(0xffffffffu, r.x);
+  hi = __reduce_max_sync(0xffffffffu, r.y);
 }
 
 template <bool kStaged>
@@ -110,8 +116,8 @@ select_tokens_kernel(SelectArgs a) {
   extern __shared__ __align__(16) unsigned staged[];
   __shared__ __align__(16) Shared sh;
   __shared__ __align__(16) unsigned gathered[kSelGathered];           // all parts' scores inside the range
-  __shared__ int warp_sums[kSelWarps];
-  __shared__ unsigned warp_lo[kSelWarps], warp_hi[kSelWarps];
+  __shared__ unsigned warp_sums[2][kSelWarps];                         // in turn, where one scan follows another
+  __shared__ uint2 ranges[kSelWarps];
   __shared__ int found_bin, found_above, found_count;
   __shared__ unsigned found_key;
   const int tid = threadIdx.x, lane = tid & 31;
@@ -184,8 +190,14 @@ select_tokens_kernel(SelectArgs a) {
   }
   reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);    // both digits: 4 * 1024 bins
   if (tid == 0) sh.num_gathered = 0;
-  lo = block_min(lo, warp_lo);
-  hi = ~block_min(~hi, warp_hi);
+  block_range(lo, hi, ranges);
+  // The row is here; the one that this SM takes next comes into L2 while this one is worked on.
+  if (kStaged && part == 0 && tid == 0 && row_index + a.ahead < a.rows) {
+    const uintptr_t next = reinterpret_cast<uintptr_t>(row + a.ahead * a.score_stride);
+    const uintptr_t from = (next + 15) & ~(uintptr_t)15, to = (next + 4ull * n) & ~(uintptr_t)15;
+    if (to > from)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((unsigned)(to - from)) : "memory");
+  }
   if (parts > 1) {
     if (tid == 0) {
       sh.range[0][0] = lo;
@@ -218,8 +230,8 @@ select_tokens_kernel(SelectArgs a) {
           c1 += g[p].y;
         }
     }
-    int total;
-    const int above1 = block_scan(c0 + c1, warp_sums, &total), above0 = above1 + c1;
+    unsigned total;
+    const int above1 = (int)block_scan((unsigned)(c0 + c1), warp_sums[0], &total), above0 = above1 + c1;
     const bool in1 = above1 < k && k <= above0, in0 = above0 < k && k <= above0 + c0;
     if (in0 || in1) {
       found_bin = in1 ? bin0 + 1 : bin0;
@@ -285,8 +297,7 @@ select_tokens_kernel(SelectArgs a) {
         least = min(least, edge_key);
         most = max(most, edge_key);
       }
-      least = block_min(least, warp_lo);
-      most = ~block_min(~most, warp_hi);
+      block_range(least, most, ranges);
       if (parts > 1) {
         if (tid == 0) {
           sh.range[pass & 1][0] = least;
@@ -386,12 +397,11 @@ select_tokens_kernel(SelectArgs a) {
       n_above += (q.x >= from) + (q.y >= from) + (q.z >= from) + (q.w >= from);
       n_equal += (q.x == base) + (q.y == base) + (q.z == base) + (q.w == base);
     }
-    int total_above, total_equal;
-    block_scan(n_above, warp_sums, &total_above);
-    block_scan(n_equal, warp_sums, &total_equal);
+    unsigned total;                                                    // a part has less than 2^16 scores
+    block_scan((unsigned)n_above | (unsigned)n_equal << 16, warp_sums[1], &total);
     if (tid == 0) {
-      sh.above = total_above;
-      sh.equal = total_equal;
+      sh.above = (int)(total & 0xffffu);
+      sh.equal = (int)(total >> 16);
     }
     cluster.sync();
     const Shared* o = other(lane % parts);
@@ -402,6 +412,7 @@ select_tokens_kernel(SelectArgs a) {
   // A staged row's list is put together where its scores were: what is kept of the slots so far needs no more
   // room than they did, and they are in registers.
   int* const list = kStaged ? reinterpret_cast<int*>(staged) : out;
+  int sums = 0;                                                        // narrow() has been behind a barrier
   for (int round = quad_begin; round < quad_end; round += kSelRunQuads * kSelThreads) {
     unsigned e[4 * kSelRunQuads];                                      // this thread's run
     const int v0 = round + tid * kSelRunQuads;
@@ -416,16 +427,16 @@ select_tokens_kernel(SelectArgs a) {
     int n_above = 0, n_equal = 0;
 #pragma unroll
     for (int i = 0; i < 4 * kSelRunQuads; ++i) n_above += e[i] >= from ? 1 : 0;
-    int total_above, total_equal = 0, equal = at_equal;
-    const int above = at_above + block_scan(n_above, warp_sums, &total_above);
-    int at = above - (kStaged ? list_begin : 0);
-    const int token = v0 * 4 - shift;
     if (split) {
 #pragma unroll
       for (int i = 0; i < 4 * kSelRunQuads; ++i) n_equal += e[i] == base ? 1 : 0;
-      equal += block_scan(n_equal, warp_sums, &total_equal);
-      at += min(equal, k);
     }
+    unsigned total;                                                    // both counts in one: 20,480 scores a round
+    const unsigned place = block_scan((unsigned)n_above | (unsigned)n_equal << 16, warp_sums[sums], &total);
+    sums ^= 1;
+    int equal = at_equal + (int)(place >> 16);
+    int at = at_above + (int)(place & 0xffffu) + (split ? min(equal, k) : 0) - (kStaged ? list_begin : 0);
+    const int token = v0 * 4 - shift;
     // the run's equal scores all stay or all go, but for one run of the row
     if (equal < k && equal + n_equal > k) {
 #pragma unroll
@@ -437,8 +448,8 @@ select_tokens_kernel(SelectArgs a) {
       for (int i = 0; i < 4 * kSelRunQuads; ++i)
         if (e[i] >= cut) list[at++] = token + i;
     }
-    at_above += total_above;
-    at_equal += total_equal;
+    at_above += (int)(total & 0xffffu);
+    at_equal += (int)(total >> 16);
   }
   if (kStaged) {
     __syncthreads();
@@ -449,7 +460,7 @@ select_tokens_kernel(SelectArgs a) {
 }
 
 // Blocks per row: as few as hold it.
-inline cudaError_t launch_select(const SelectArgs& a, long long rows, cudaStream_t stream) {
+inline cudaError_t launch_select(SelectArgs a, long long rows, int sm_count, cudaStream_t stream) {
   const int quads = (a.n + 3 + 3) / 4;                                 // up to three slots before the first token
   int parts = 1;
   while (parts < kSelMaxCluster && (quads + parts - 1) / parts * 4 > kSelStaged) parts *= 2;
@@ -458,6 +469,8 @@ inline cudaError_t launch_select(const SelectArgs& a, long long rows, cudaStream
     select_tokens_kernel<false><<<(unsigned)rows, kSelThreads, 0, stream>>>(a);
     return cudaGetLastError();
   }
+  a.rows = (int)rows;
+  a.ahead = std::max(1, sm_count / parts);                             // a block takes the SM's registers
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * parts), 1, 1);
   cfg.blockDim = dim3(kSelThreads, 1, 1);

@@ -530,7 +530,7 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
     a.n = n;
     a.keep = keep;
     DeviceGuard guard(ctx->cfg.device);
-    const cudaError_t e = launch_select(a, rows, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_select(a, rows, ctx->sm_count, static_cast<cudaStream_t>(stream));
     ctx->launches++;
     return cuda_status(ctx, e, "select_tokens");
   });
