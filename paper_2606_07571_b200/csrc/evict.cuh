@@ -55,7 +55,9 @@ constexpr int kSelGathered = kSelBins;          // scores of the first digit's b
 constexpr int kSelRanked = 256;                 // at most so many are ranked directly
 constexpr int kSelStaged = 49152;               // scores of a block's part kept in shared memory (192 KB)
 constexpr int kSelRunQuads = 5;                 // scores / 4 of a thread's run: odd, so that runs start on different banks
+constexpr int kSelMaxRun = 13;                  // quads of a thread's run of a staged row, at most: 52 bits
 constexpr int kSelMaxCluster = 8;
+static_assert(kSelStaged / 4 <= 12 * kSelThreads, "a run and one quad more, where that makes it odd");
 static_assert(kSelStaged < 65536 && 4 * kSelRunQuads * kSelThreads < 65536, "two counts in 32 bits");
 static_assert(kSelBins == 2 * kSelThreads && kSelWarps == 32, "two bins to a thread, a warp over the warps' results");
 
@@ -73,6 +75,50 @@ struct SelectArgs {
   int n, keep, first, last;                     // protected: t < first, t >= n - last; first + last <= min(n, keep)
   int rows, ahead;                              // rows that the GPU works on at a time
 };
+
+// The row starts `shift` scores past a 16-byte boundary.  Slot s holds token s - shift, so that 16-byte loads
+// and 16-byte shared-memory words line up; slots below `shift` and past the end are no tokens.
+struct SelectRow {
+  int shift, slots, quads;
+  int slot_begin, slot_end;                     // slots that compete
+};
+__device__ __forceinline__ SelectRow select_row(const SelectArgs& a, const float* row) {
+  SelectRow r;
+  r.shift = (int)((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
+  r.slots = a.n + r.shift;
+  r.quads = (r.slots + 3) >> 2;
+  r.slot_begin = a.first + r.shift;
+  r.slot_end = a.n - a.last + r.shift;
+  return r;
+}
+__device__ __forceinline__ uint4 select_load(const SelectRow& r, const float* row, int v) {       // slots 4 v .. 4 v + 3
+  float4 f;
+  if (4 * v >= r.shift && 4 * v + 3 < r.slots) {
+    f = *reinterpret_cast<const float4*>(row + 4 * v - r.shift);
+  } else {
+    float* e = reinterpret_cast<float*>(&f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int s = 4 * v + j;
+      e[j] = s >= r.shift && s < r.slots ? row[s - r.shift] : 0.f;
+    }
+  }
+  return make_uint4(select_key(f.x), select_key(f.y), select_key(f.z), select_key(f.w));
+}
+// a slot that does not compete is marked: protected tokens stay (largest key), other slots never do
+__device__ __forceinline__ uint4 select_marked(const SelectRow& r, uint4 q, int v) {
+  auto mark = [&](unsigned key, int s) {
+    return s >= r.slot_begin && s < r.slot_end ? key : (s >= r.shift && s < r.slots ? 0xffffffffu : 0u);
+  };
+  return make_uint4(mark(q.x, 4 * v), mark(q.y, 4 * v + 1), mark(q.z, 4 * v + 2), mark(q.w, 4 * v + 3));
+}
+// the competing slot outside the whole quads [qa, qb) that falls to this thread, or -1
+__device__ __forceinline__ int select_edge(int slot_begin, int slot_end, int qa, int qb) {
+  const int t = threadIdx.x;
+  if (t < 4) return slot_begin + t < min(qa * 4, slot_end) ? slot_begin + t : -1;
+  if (t < 8) return slot_begin < slot_end && qb * 4 + t - 4 < slot_end ? qb * 4 + t - 4 : -1;
+  return -1;
+}
 
 // exclusive prefix sum of v over the block, in thread order; *total receives the sum.  One barrier; warp_sums may be
 // written again after the next.
@@ -103,7 +149,13 @@ __device__ __forceinline__ void block_range(unsigned& lo, unsigned& hi, uint2* r
   hi = __reduce_max_sync(0xffffffffu, r.y);
 }
 
-template <bool kStaged>
+// What a thread knows of its run of up to 52 slots: bit b of the two words is slot 4 * first quad + b.
+struct SelectMasks {
+  unsigned above[2];                            // stays for sure
+  unsigned in[2];                               // inside the range
+};
+__device__ __forceinline__ int mask_count(const unsigned* m) { return __popc(m[0]) + __popc(m[1]); }
+
 __global__ void __launch_bounds__(kSelThreads)
 select_tokens_kernel(SelectArgs a) {
   namespace cg = cooperative_groups;
@@ -116,58 +168,29 @@ select_tokens_kernel(SelectArgs a) {
   extern __shared__ __align__(16) unsigned staged[];
   __shared__ __align__(16) Shared sh;
   __shared__ __align__(16) unsigned gathered[kSelGathered];           // all parts' scores inside the range
-  __shared__ unsigned warp_sums[2][kSelWarps];                         // in turn, where one scan follows another
+  __shared__ unsigned warp_sums[2][kSelWarps];                         // narrow()'s, the places'
   __shared__ uint2 ranges[kSelWarps];
   __shared__ int found_bin, found_above, found_count;
   __shared__ unsigned found_key;
   const int tid = threadIdx.x, lane = tid & 31;
   const cg::cluster_group cluster = cg::this_cluster();
-  const int parts = kStaged ? (int)cluster.num_blocks() : 1, part = kStaged ? (int)cluster.block_rank() : 0;
+  const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
   auto sync_parts = [&]() {
     if (parts > 1) cluster.sync(); else __syncthreads();
   };
   auto other = [&](int p) { return parts > 1 ? cluster.map_shared_rank(&sh, p) : &sh; };
   const long long row_index = blockIdx.x / parts;
   const float* __restrict__ row = a.scores + row_index * a.score_stride;
-  int* out = a.idx + row_index * a.idx_stride;
-  const int n = a.n;
-  // The row starts `shift` scores past a 16-byte boundary.  Slot s holds token s - shift, so that 16-byte loads
-  // and 16-byte shared-memory words line up; slots below `shift` and past the end are no tokens.
-  const int shift = (int)((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
-  const int slots = n + shift, quads = (slots + 3) >> 2;
-  const int part_quads = (quads + parts - 1) / parts;
-  const int quad_begin = min(quads, part * part_quads), quad_end = min(quads, quad_begin + part_quads);
-  auto load_quad = [&](int v) {                                        // slots 4 v .. 4 v + 3, from memory
-    float4 f;
-    if (4 * v >= shift && 4 * v + 3 < slots) {
-      f = *reinterpret_cast<const float4*>(row + 4 * v - shift);
-    } else {
-      float* e = reinterpret_cast<float*>(&f);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = 4 * v + j - shift;
-        e[j] = t >= 0 && t < n ? row[t] : 0.f;
-      }
-    }
-    return make_uint4(select_key(f.x), select_key(f.y), select_key(f.z), select_key(f.w));
-  };
-  auto quad_at = [&](int v) { return kStaged ? reinterpret_cast<const uint4*>(staged)[v - quad_begin] : load_quad(v); };
+  const SelectRow r = select_row(a, row);
+  const int part_quads = (r.quads + parts - 1) / parts;
+  const int quad_begin = min(r.quads, part * part_quads), quad_end = min(r.quads, quad_begin + part_quads);
+  uint4* const quads = reinterpret_cast<uint4*>(staged);               // quad v of the row at v - quad_begin
   // The part's competing slots [slot_begin, slot_end): whole quads [qa, qb), and up to three slots on each side,
   // one to a thread.
-  const int slot_begin = max(a.first + shift, quad_begin * 4), slot_end = min(n - a.last + shift, quad_end * 4);
+  const int slot_begin = max(r.slot_begin, quad_begin * 4), slot_end = min(r.slot_end, quad_end * 4);
   const int qa = (slot_begin + 3) >> 2, qb = max(qa, slot_end >> 2);
-  int edge = -1;
-  if (tid < 4 && slot_begin + tid < min(qa * 4, slot_end)) edge = slot_begin + tid;
-  if (tid >= 4 && tid < 8 && slot_begin < slot_end && qb * 4 + tid - 4 < slot_end) edge = qb * 4 + tid - 4;
-  const unsigned edge_key = edge >= 0 ? select_key(row[edge - shift]) : 0u;
-
-  // a slot that does not compete is marked: protected tokens stay (largest key), other slots never do
-  auto marked = [&](uint4 q, int v) {
-    auto mark = [&](unsigned key, int s) {
-      return s >= slot_begin && s < slot_end ? key : (s >= shift && s < slots ? 0xffffffffu : 0u);
-    };
-    return make_uint4(mark(q.x, 4 * v), mark(q.y, 4 * v + 1), mark(q.z, 4 * v + 2), mark(q.w, 4 * v + 3));
-  };
+  const int edge = select_edge(slot_begin, slot_end, qa, qb);
+  const unsigned edge_key = edge >= 0 ? select_key(row[edge - r.shift]) : 0u;
 
   unsigned lo = edge >= 0 ? edge_key : 0xffffffffu, hi = edge_key;
   constexpr int kAhead = 4;                                            // loads in flight per thread
@@ -175,13 +198,13 @@ select_tokens_kernel(SelectArgs a) {
     uint4 k[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      if (v0 + j * kSelThreads < quad_end) k[j] = load_quad(v0 + j * kSelThreads);
+      if (v0 + j * kSelThreads < quad_end) k[j] = select_load(r, row, v0 + j * kSelThreads);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int v = v0 + j * kSelThreads;
       if (v >= quad_end) break;
       const bool whole = v >= qa && v < qb;
-      if (kStaged) reinterpret_cast<uint4*>(staged)[v - quad_begin] = whole ? k[j] : marked(k[j], v);
+      quads[v - quad_begin] = whole ? k[j] : select_marked(r, k[j], v);
       if (whole) {
         lo = min(min(min(lo, k[j].x), k[j].y), min(k[j].z, k[j].w));
         hi = max(max(max(hi, k[j].x), k[j].y), max(k[j].z, k[j].w));
@@ -192,9 +215,9 @@ select_tokens_kernel(SelectArgs a) {
   if (tid == 0) sh.num_gathered = 0;
   block_range(lo, hi, ranges);
   // The row is here; the one that this SM takes next comes into L2 while this one is worked on.
-  if (kStaged && part == 0 && tid == 0 && row_index + a.ahead < a.rows) {
+  if (part == 0 && tid == 0 && row_index + a.ahead < a.rows) {
     const uintptr_t next = reinterpret_cast<uintptr_t>(row + a.ahead * a.score_stride);
-    const uintptr_t from = (next + 15) & ~(uintptr_t)15, to = (next + 4ull * n) & ~(uintptr_t)15;
+    const uintptr_t from = (next + 15) & ~(uintptr_t)15, to = (next + 4ull * a.n) & ~(uintptr_t)15;
     if (to > from)
       asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((unsigned)(to - from)) : "memory");
   }
@@ -212,7 +235,7 @@ select_tokens_kernel(SelectArgs a) {
   // The k-th largest of the competing scores is in [base, base + span], where `inside` of them are and it is the
   // k-th from the top.  narrow(): the digit's histogram, summed over `among` parts, shortens the range.
   int k = a.keep - a.first - a.last, inside = 0, pass = 0, digit = 0;
-  unsigned base = 0, span = 0;                                         // below every competing key: all are kept
+  unsigned base = 0, span = 0;
   auto narrow = [&](int among, int buffer) {
     // counts from the top: thread t holds bins 2046 - 2 t and 2047 - 2 t
     const int bin0 = kSelBins - 2 - 2 * tid;
@@ -245,11 +268,234 @@ select_tokens_kernel(SelectArgs a) {
     span = min(span - ((unsigned)found_bin << digit), (1u << digit) - 1u);
     digit = max(0, digit - kSelDigitBits);
   };
-  // f(score) for every competing score inside the range
+  const bool some = k > 0 && k < a.n - a.first - a.last;               // not all, not none of those that compete
+  if (some) {
+    base = lo;
+    span = hi - lo;
+    digit = max(0, (32 - __clz(span)) - kSelDigitBits);
+#pragma unroll 2
+    for (int v = qa + tid; v < qb; v += kSelThreads) {                 // every score is inside the range
+      const uint4 q = quads[v - quad_begin];
+      atomicAdd(&sh.hist[0][(q.x - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.y - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.z - base) >> digit], 1);
+      atomicAdd(&sh.hist[0][(q.w - base) >> digit], 1);
+    }
+    if (edge >= 0) atomicAdd(&sh.hist[0][(edge_key - base) >> digit], 1);
+    sync_parts();
+    narrow(parts, 0);
+  } else {
+    base = k > 0 ? 1u : 0xfffffffeu;                                   // between the marks: no score has these values
+  }
+
+  // From here on a thread has a run of slots of its own, as bits: what is above the range, what is inside.  An odd
+  // number of quads, so that the runs of a quarter warp start on different banks.
+  const int run = ((part_quads + kSelThreads - 1) / kSelThreads) | 1;
+  const int my_quads = min(run, quad_end - quad_begin - tid * run);    // may be below 0
+  const unsigned* const mine = staged + 4 * tid * run;
+  SelectMasks m = {{0u, 0u}, {0u, 0u}};
+  {
+    const unsigned top = base + span;
+#pragma unroll
+    for (int i = 0; i < kSelMaxRun; ++i) {
+      if (i >= my_quads) break;
+      const uint4 q = reinterpret_cast<const uint4*>(mine)[i];
+      const unsigned e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int w = (4 * i + j) >> 5;
+        const unsigned bit = 1u << ((4 * i + j) & 31);
+        if (e[j] > top) m.above[w] |= bit;
+        if (e[j] >= base) m.in[w] |= bit;
+      }
+    }
+    m.in[0] &= ~m.above[0];
+    m.in[1] &= ~m.above[1];
+  }
+  // f(score, word, bit) for every score of the run inside the range
   auto each_inside = [&](auto&& f) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      for (unsigned left = m.in[w]; left != 0u; left &= left - 1u) {
+        const int b = __ffs((int)left) - 1;
+        f(mine[32 * w + b], w, 1u << b);
+      }
+  };
+  auto refine = [&]() {                                                // the range has become shorter
+    const unsigned top = base + span;
+    each_inside([&](unsigned e, int w, unsigned bit) {
+      if (e > top) m.above[w] |= bit;
+      if (e - base > span) m.in[w] &= ~bit;
+    });
+  };
+
+  // A bin of many scores is often one of many equal ones: their smallest and largest say so, and else where
+  // the next digit begins.  A bin too full to be gathered takes further digits.
+  while (span > 0 && inside > k && inside > kSelRanked) {
+    ++pass;
+    unsigned least = 0xffffffffu, most = 0u;
+    each_inside([&](unsigned e, int, unsigned) {
+      least = min(least, e);
+      most = max(most, e);
+    });
+    block_range(least, most, ranges);
+    if (parts > 1) {
+      if (tid == 0) {
+        sh.range[pass & 1][0] = least;
+        sh.range[pass & 1][1] = most;
+      }
+      cluster.sync();
+      const Shared* o = other(lane % parts);
+      least = __reduce_min_sync(0xffffffffu, o->range[pass & 1][0]);
+      most = __reduce_max_sync(0xffffffffu, o->range[pass & 1][1]);
+    }
+    base = least;
+    span = most - least;
+    digit = max(0, (32 - __clz(span)) - kSelDigitBits);
+    if (span == 0 || inside <= kSelGathered) break;
+    each_inside([&](unsigned e, int, unsigned) { atomicAdd(&sh.hist[pass & 1][(e - base) >> digit], 1); });
+    sync_parts();
+    // every part has read the digit before this one: its bins are cleared for the next
+    reinterpret_cast<int2*>(sh.hist[(pass + 1) & 1])[tid] = make_int2(0, 0);
+    narrow(parts, pass & 1);
+    refine();
+  }
+  if (span > 0 && inside > k) {
+    // gather the scores inside; from here on every part of the cluster does the same work on the same list
+    const int lists = (pass + 1) & 1, bins = pass & 1;                 // one digit's bins hold the part's list
+    unsigned* const part_list = reinterpret_cast<unsigned*>(sh.hist[lists]);
+    {
+      const int count = mask_count(m.in);
+      int at = count;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, at, o);
+        if (lane >= o) at += x;
+      }
+      int first = 0;
+      if (lane == 31 && at > 0) first = atomicAdd(&sh.num_gathered, at);
+      at += __shfl_sync(0xffffffffu, first, 31) - count;
+      each_inside([&](unsigned e, int, unsigned) { part_list[at++] = e; });
+    }
+    if (parts == 1 && tid < 4 && inside + tid < kSelGathered) part_list[inside + tid] = 0u;     // read in fours below
+    sync_parts();
+    unsigned* list = part_list;
+    if (parts > 1) {
+      const int theirs = lane < parts ? other(lane)->num_gathered : 0;
+      for (int i = tid; i < kSelGathered; i += kSelThreads) {          // thread i takes the i-th of all parts' scores
+        int from = -1, at = i;
+#pragma unroll
+        for (int p = 0; p < kSelMaxCluster; ++p) {
+          const int c = __shfl_sync(0xffffffffu, theirs, p);
+          if (from < 0 && at < c) from = p;
+          if (from < 0) at -= c;
+        }
+        gathered[i] = from >= 0 ? (unsigned)other(from)->hist[lists][at] : 0u;         // past the end: below any score
+      }
+      list = gathered;
+      __syncthreads();
+    }
+    const int all = inside;
+    while (span > 0 && inside > k) {
+      if (all <= kSelRanked) {
+        if (tid < all) {
+          const unsigned key = list[tid];
+          int greater = 0, same = 0;
+          for (int i = 0; i < all; i += 4) {
+            const uint4 c = *reinterpret_cast<const uint4*>(&list[i]);
+            greater += (c.x > key) + (c.y > key) + (c.z > key) + (c.w > key);
+            same += (c.x == key) + (c.y == key) + (c.z == key) + (c.w == key);
+          }
+          if (greater < k && k <= greater + same) {                    // by every thread with that score, alike
+            found_key = key;
+            found_above = greater;
+            found_count = same;
+          }
+        }
+        __syncthreads();
+        base = found_key;
+        k -= found_above;
+        inside = found_count;
+        span = 0;
+      } else {
+        reinterpret_cast<int2*>(sh.hist[bins])[tid] = make_int2(0, 0);
+        __syncthreads();
+        for (int i = tid; i < all; i += kSelThreads) {
+          const unsigned d = list[i] - base;
+          if (d <= span) atomicAdd(&sh.hist[bins][d >> digit], 1);
+        }
+        __syncthreads();
+        narrow(1, bins);
+      }
+    }
+    refine();
+  }
+
+  // Kept: what is above the range, and the first k of what is inside (all of it, or equal scores).
+  const int n_in = mask_count(m.in);
+  unsigned total;                                                      // a part has less than 2^16 slots
+  const unsigned place = block_scan((unsigned)mask_count(m.above) | (unsigned)n_in << 16, warp_sums[1], &total);
+  const int part_above = (int)(total & 0xffffu), part_in = (int)(total >> 16);
+  int at_above = 0, at_in = 0;                                         // of the parts before this one
+  if (parts > 1) {
+    if (tid == 0) {
+      sh.above = part_above;
+      sh.equal = part_in;
+    }
+    cluster.sync();
+    const Shared* o = other(lane % parts);
+    at_above = __reduce_add_sync(0xffffffffu, lane < part ? o->above : 0);
+    at_in = __reduce_add_sync(0xffffffffu, lane < part ? o->equal : 0);
+  }
+  const int in_before = at_in + (int)(place >> 16);
+  if (in_before >= k) {
+    m.in[0] = m.in[1] = 0u;
+  } else {
+    for (int drop = n_in - (k - in_before); drop > 0; --drop) {        // one run of the row
+      const int w = m.in[1] != 0u ? 1 : 0;                             // the last of them
+      const unsigned bit = 1u << (31 - __clz((int)(w ? m.in[1] : m.in[0])));
+      if (w) m.in[1] ^= bit; else m.in[0] ^= bit;
+    }
+  }
+  // The list is put together where the scores were and leaves in order.
+  int* const list = reinterpret_cast<int*>(staged);
+  const int in_part = min(at_in, k);                                   // of those before the part
+  int at = (int)(place & 0xffffu) + min(in_before, k) - in_part;
+  const int token = (quad_begin + tid * run) * 4 - r.shift;
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+    for (unsigned left = m.above[w] | m.in[w]; left != 0u; left &= left - 1u) list[at++] = token + 32 * w + __ffs((int)left) - 1;
+  __syncthreads();
+  int* const out = a.idx + row_index * a.idx_stride + at_above + in_part;
+  const int count = part_above + min(at_in + part_in, k) - in_part;
+#pragma unroll 4
+  for (int i = tid; i < count; i += kSelThreads) out[i] = list[i];
+  if (parts > 1) cluster.sync();                                       // the others have read this block's counts
+}
+
+// Rows too long to be staged: one block, which reads the row in every pass.
+__global__ void __launch_bounds__(kSelThreads)
+select_long_rows_kernel(SelectArgs a) {
+  __shared__ __align__(16) int hist[kSelBins];
+  __shared__ unsigned warp_sums[2][kSelWarps];                         // in turn, where one scan follows another
+  __shared__ uint2 ranges[kSelWarps];
+  __shared__ int found_bin, found_above, found_count;
+  const int tid = threadIdx.x;
+  const float* __restrict__ row = a.scores + blockIdx.x * a.score_stride;
+  int* out = a.idx + blockIdx.x * a.idx_stride;
+  const SelectRow r = select_row(a, row);
+  const int qa = (r.slot_begin + 3) >> 2, qb = max(qa, r.slot_end >> 2);
+  const int edge = select_edge(r.slot_begin, r.slot_end, qa, qb);
+  const unsigned edge_key = edge >= 0 ? select_key(row[edge - r.shift]) : 0u;
+
+  // The k-th largest of the competing scores is in [base, base + span], where `inside` of them are and it is the
+  // k-th from the top.
+  int k = a.keep - a.first - a.last, inside = a.n - a.first - a.last;
+  unsigned base = 0u, span = 0xffffffffu;
+  auto each_inside = [&](auto&& f) {                                   // f(score) for every one inside the range
 #pragma unroll 2
     for (int v = qa + tid; v < qb; v += kSelThreads) {
-      const uint4 q = quad_at(v);
+      const uint4 q = select_load(r, row, v);
       const unsigned d[4] = {q.x - base, q.y - base, q.z - base, q.w - base};   // below base: wraps to a large value
       if (min(min(d[0], d[1]), min(d[2], d[3])) <= span) {
 #pragma unroll
@@ -259,204 +505,75 @@ select_tokens_kernel(SelectArgs a) {
     }
     if (edge >= 0 && edge_key - base <= span) f(edge_key);
   };
-  if (k <= 0) {
-    base = 0xffffffffu;
-    k = 0;
-  } else if (k < n - a.first - a.last) {
-    base = lo;
-    span = hi - lo;
-    digit = max(0, (32 - __clz(span)) - kSelDigitBits);
-#pragma unroll 2
-    for (int v = qa + tid; v < qb; v += kSelThreads) {                 // every score is inside the range
-      const uint4 q = quad_at(v);
-      atomicAdd(&sh.hist[0][(q.x - base) >> digit], 1);
-      atomicAdd(&sh.hist[0][(q.y - base) >> digit], 1);
-      atomicAdd(&sh.hist[0][(q.z - base) >> digit], 1);
-      atomicAdd(&sh.hist[0][(q.w - base) >> digit], 1);
-    }
-    if (edge >= 0) atomicAdd(&sh.hist[0][(edge_key - base) >> digit], 1);
-    sync_parts();
-    narrow(parts, 0);
-    // A bin of many scores is often one of many equal ones: their smallest and largest say so, and else where
-    // the next digit begins.  A bin too full to be gathered takes further digits over the whole row.
-    while (span > 0 && inside > k && inside > kSelRanked) {
-      ++pass;
+  if (k > 0 && inside > k) {
+    while (span > 0 && inside > k) {
+      // the range taken to what is in it (one of many equal scores becomes a range of one), then its first digit
       unsigned least = 0xffffffffu, most = 0u;
-#pragma unroll 2
-      for (int v = qa + tid; v < qb; v += kSelThreads) {               // without branches: many are inside
-        const uint4 q = quad_at(v);
-        const unsigned e[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool in = e[j] - base <= span;
-          least = min(least, in ? e[j] : 0xffffffffu);
-          most = max(most, in ? e[j] : 0u);
-        }
-      }
-      if (edge >= 0 && edge_key - base <= span) {
-        least = min(least, edge_key);
-        most = max(most, edge_key);
-      }
+      each_inside([&](unsigned e) {
+        least = min(least, e);
+        most = max(most, e);
+      });
+      reinterpret_cast<int2*>(hist)[tid] = make_int2(0, 0);
       block_range(least, most, ranges);
-      if (parts > 1) {
-        if (tid == 0) {
-          sh.range[pass & 1][0] = least;
-          sh.range[pass & 1][1] = most;
-        }
-        cluster.sync();
-        const Shared* o = other(lane % parts);
-        least = __reduce_min_sync(0xffffffffu, o->range[pass & 1][0]);
-        most = __reduce_max_sync(0xffffffffu, o->range[pass & 1][1]);
-      }
       base = least;
       span = most - least;
-      digit = max(0, (32 - __clz(span)) - kSelDigitBits);
-      if (span == 0 || inside <= kSelGathered) break;
-      each_inside([&](unsigned e) { atomicAdd(&sh.hist[pass & 1][(e - base) >> digit], 1); });
-      sync_parts();
-      // every part has read the digit before this one: its bins are cleared for the next
-      reinterpret_cast<int2*>(sh.hist[(pass + 1) & 1])[tid] = make_int2(0, 0);
-      narrow(parts, pass & 1);
-    }
-    if (span > 0 && inside > k) {
-      // gather the scores inside; from here on every part of the cluster does the same work on the same list
-      const int lists = (pass + 1) & 1, bins = pass & 1;               // one digit's bins hold the part's list
-      unsigned* const mine = reinterpret_cast<unsigned*>(sh.hist[lists]);
-      each_inside([&](unsigned e) { mine[atomicAdd(&sh.num_gathered, 1)] = e; });
-      if (parts == 1 && tid < 4 && inside + tid < kSelGathered) mine[inside + tid] = 0u;      // read in fours below
-      sync_parts();
-      unsigned* list = mine;
-      if (parts > 1) {
-        const int theirs = lane < parts ? other(lane)->num_gathered : 0;
-        for (int i = tid; i < kSelGathered; i += kSelThreads) {        // thread i takes the i-th of all parts' scores
-          int from = -1, at = i;
-#pragma unroll
-          for (int p = 0; p < kSelMaxCluster; ++p) {
-            const int m = __shfl_sync(0xffffffffu, theirs, p);
-            if (from < 0 && at < m) from = p;
-            if (from < 0) at -= m;
-          }
-          gathered[i] = from >= 0 ? (unsigned)other(from)->hist[lists][at] : 0u;       // past the end: below any score
-        }
-        list = gathered;
-        __syncthreads();
+      if (span == 0) break;
+      const int digit = max(0, (32 - __clz(span)) - kSelDigitBits);
+      each_inside([&](unsigned e) { atomicAdd(&hist[(e - base) >> digit], 1); });
+      __syncthreads();
+      // counts from the top: thread t holds bins 2046 - 2 t and 2047 - 2 t
+      const int bin0 = kSelBins - 2 - 2 * tid;
+      const int2 h = *reinterpret_cast<const int2*>(&hist[bin0]);
+      unsigned total;
+      const int above1 = (int)block_scan((unsigned)(h.x + h.y), warp_sums[0], &total), above0 = above1 + h.y;
+      const bool in1 = above1 < k && k <= above0, in0 = above0 < k && k <= above0 + h.x;
+      if (in0 || in1) {
+        found_bin = in1 ? bin0 + 1 : bin0;
+        found_above = in1 ? above1 : above0;
+        found_count = in1 ? h.y : h.x;
       }
-      const int all = inside;
-      while (span > 0 && inside > k) {
-        if (all <= kSelRanked) {
-          if (tid < all) {
-            const unsigned key = list[tid];
-            int greater = 0, same = 0;
-            for (int i = 0; i < all; i += 4) {
-              const uint4 c = *reinterpret_cast<const uint4*>(&list[i]);
-              greater += (c.x > key) + (c.y > key) + (c.z > key) + (c.w > key);
-              same += (c.x == key) + (c.y == key) + (c.z == key) + (c.w == key);
-            }
-            if (greater < k && k <= greater + same) {                  // by every thread with that score, alike
-              found_key = key;
-              found_above = greater;
-              found_count = same;
-            }
-          }
-          __syncthreads();
-          base = found_key;
-          k -= found_above;
-          inside = found_count;
-          span = 0;
-        } else {
-          reinterpret_cast<int2*>(sh.hist[bins])[tid] = make_int2(0, 0);
-          __syncthreads();
-          for (int i = tid; i < all; i += kSelThreads) {
-            const unsigned d = list[i] - base;
-            if (d <= span) atomicAdd(&sh.hist[bins][d >> digit], 1);
-          }
-          __syncthreads();
-          narrow(1, bins);
-        }
-      }
+      __syncthreads();
+      k -= found_above;
+      inside = found_count;
+      base += (unsigned)found_bin << digit;
+      span = min(span - ((unsigned)found_bin << digit), (1u << digit) - 1u);
     }
+  } else {
+    base = k > 0 ? 1u : 0xfffffffeu;                                   // between the marks: no score has these values
+    span = 0u;
   }
-  // Kept: scores above `base`, and the first k of those equal to it; where all of these are kept (or none competes),
-  // scores from `base` on.  (With inside == k the range may still be wider than one value.)
-  const bool split = inside > k;
-  const unsigned least = split ? base + 1u : base;
-
-  const unsigned from = max(least, 1u);                                // key 0 is no token
-  auto keys_at = [&](int v) {                                          // with marks in the slots that do not compete
-    uint4 q = make_uint4(0, 0, 0, 0);
-    if (v < quad_end) q = quad_at(v);
-    if (!kStaged && (v < qa || v >= qb)) q = marked(q, v);
-    return q;
-  };
-  // Where the part's list starts: behind what the parts before it keep, which the cluster has to count first.
-  int at_above = 0, at_equal = 0;
-  if (parts > 1) {
-    int n_above = 0, n_equal = 0;
-    for (int v = quad_begin + tid; v < quad_end; v += kSelThreads) {
-      const uint4 q = keys_at(v);
-      n_above += (q.x >= from) + (q.y >= from) + (q.z >= from) + (q.w >= from);
-      n_equal += (q.x == base) + (q.y == base) + (q.z == base) + (q.w == base);
-    }
-    unsigned total;                                                    // a part has less than 2^16 scores
-    block_scan((unsigned)n_above | (unsigned)n_equal << 16, warp_sums[1], &total);
-    if (tid == 0) {
-      sh.above = (int)(total & 0xffffu);
-      sh.equal = (int)(total >> 16);
-    }
-    cluster.sync();
-    const Shared* o = other(lane % parts);
-    at_above = __reduce_add_sync(0xffffffffu, lane < part ? o->above : 0);
-    at_equal = __reduce_add_sync(0xffffffffu, lane < part ? o->equal : 0);
-  }
-  const int list_begin = at_above + (split ? min(at_equal, k) : 0);
-  // A staged row's list is put together where its scores were: what is kept of the slots so far needs no more
-  // room than they did, and they are in registers.
-  int* const list = kStaged ? reinterpret_cast<int*>(staged) : out;
-  int sums = 0;                                                        // narrow() has been behind a barrier
-  for (int round = quad_begin; round < quad_end; round += kSelRunQuads * kSelThreads) {
+  // Kept: what is above the range, and the first k of what is inside (all of it, or equal scores).
+  const unsigned top = base + span;
+  int at_above = 0, at_in = 0, sums = 0;
+  for (int round = 0; round < r.quads; round += kSelRunQuads * kSelThreads) {
     unsigned e[4 * kSelRunQuads];                                      // this thread's run
     const int v0 = round + tid * kSelRunQuads;
 #pragma unroll
     for (int i = 0; i < kSelRunQuads; ++i) {
-      const uint4 q = keys_at(v0 + i);
+      uint4 q = make_uint4(0, 0, 0, 0);
+      if (v0 + i < r.quads) q = select_marked(r, select_load(r, row, v0 + i), v0 + i);
       e[4 * i] = q.x;
       e[4 * i + 1] = q.y;
       e[4 * i + 2] = q.z;
       e[4 * i + 3] = q.w;
     }
-    int n_above = 0, n_equal = 0;
+    int n_above = 0, n_in = 0;
 #pragma unroll
-    for (int i = 0; i < 4 * kSelRunQuads; ++i) n_above += e[i] >= from ? 1 : 0;
-    if (split) {
-#pragma unroll
-      for (int i = 0; i < 4 * kSelRunQuads; ++i) n_equal += e[i] == base ? 1 : 0;
+    for (int i = 0; i < 4 * kSelRunQuads; ++i) {
+      n_above += e[i] > top ? 1 : 0;
+      n_in += e[i] - base <= span ? 1 : 0;
     }
     unsigned total;                                                    // both counts in one: 20,480 scores a round
-    const unsigned place = block_scan((unsigned)n_above | (unsigned)n_equal << 16, warp_sums[sums], &total);
+    const unsigned place = block_scan((unsigned)n_above | (unsigned)n_in << 16, warp_sums[sums], &total);
     sums ^= 1;
-    int equal = at_equal + (int)(place >> 16);
-    int at = at_above + (int)(place & 0xffffu) + (split ? min(equal, k) : 0) - (kStaged ? list_begin : 0);
-    const int token = v0 * 4 - shift;
-    // the run's equal scores all stay or all go, but for one run of the row
-    if (equal < k && equal + n_equal > k) {
+    int in_before = at_in + (int)(place >> 16);
+    int at = at_above + (int)(place & 0xffffu) + min(in_before, k);
 #pragma unroll
-      for (int i = 0; i < 4 * kSelRunQuads; ++i)
-        if (e[i] >= from || (e[i] == base && equal++ < k)) list[at++] = token + i;
-    } else {
-      const unsigned cut = n_equal > 0 && equal < k ? base : from;
-#pragma unroll
-      for (int i = 0; i < 4 * kSelRunQuads; ++i)
-        if (e[i] >= cut) list[at++] = token + i;
-    }
+    for (int i = 0; i < 4 * kSelRunQuads; ++i)
+      if (e[i] > top || (e[i] - base <= span && in_before++ < k)) out[at++] = v0 * 4 - r.shift + i;
     at_above += (int)(total & 0xffffu);
-    at_equal += (int)(total >> 16);
+    at_in += (int)(total >> 16);
   }
-  if (kStaged) {
-    __syncthreads();
-    const int count = at_above + (split ? min(at_equal, k) : 0) - list_begin;
-    for (int i = tid; i < count; i += kSelThreads) out[list_begin + i] = list[i];
-  }
-  if (parts > 1) cluster.sync();                                       // the others have read this block's counts
 }
 
 // Blocks per row: as few as hold it.
@@ -466,7 +583,7 @@ inline cudaError_t launch_select(SelectArgs a, long long rows, int sm_count, cud
   while (parts < kSelMaxCluster && (quads + parts - 1) / parts * 4 > kSelStaged) parts *= 2;
   const int part_quads = (quads + parts - 1) / parts;
   if (part_quads * 4 > kSelStaged || rows * parts > 0x7fffffffLL) {
-    select_tokens_kernel<false><<<(unsigned)rows, kSelThreads, 0, stream>>>(a);
+    select_long_rows_kernel<<<(unsigned)rows, kSelThreads, 0, stream>>>(a);
     return cudaGetLastError();
   }
   a.rows = (int)rows;
@@ -483,7 +600,7 @@ inline cudaError_t launch_select(SelectArgs a, long long rows, int sm_count, cud
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, select_tokens_kernel<true>, a);
+  return cudaLaunchKernelEx(&cfg, select_tokens_kernel, a);
 }
 
 // ---------------------------------------------------------------------------------------------

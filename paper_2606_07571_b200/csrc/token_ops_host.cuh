@@ -476,7 +476,7 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
 }
 
 cudaError_t configure_token_ops(bool tensor_ok) {
-  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
+  cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
   const int ws = (int)weights_simt_smem(kSimtMaxD);
   auto simt = [&](auto words) {
     constexpr int kWords = decltype(words)::value;
