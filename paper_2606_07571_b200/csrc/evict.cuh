@@ -714,7 +714,7 @@ struct WeightGroup {
   int item_begin;               // first work item
   int splits, tiles_per_split;
   int part_off;                 // first partial sum (one [splits][Hkv][m] block per group)
-  int pad;
+  int tiles;                    // row tiles of the group
   long long score_off;          // elements from the scores' base to the group's block
 };
 struct WeightSeg {

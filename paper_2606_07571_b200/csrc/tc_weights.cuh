@@ -76,17 +76,18 @@ __device__ __forceinline__ Item read_item(const WeightArgs& a, const int* list, 
   Item it;
   it.g = weight_group_of(a, list, index);
   const WeightGroup& g = weight_group(list, it.g);
-  int rem = index - g.item_begin;
-  const int kb = rem % g.key_blocks;
-  rem /= g.key_blocks;
-  it.split = rem % g.splits;
-  it.hk = rem / g.splits;
+  const int rem = index - g.item_begin, at = rem / g.key_blocks, kb = rem - at * g.key_blocks;
+  it.hk = at;
+  it.split = 0;
+  if (g.splits > 1) {
+    it.hk = at / g.splits;
+    it.split = at - it.hk * g.splits;
+  }
   it.key0 = kb * kItemKeys;
   it.keys = min(kItemKeys, g.m - it.key0);
   it.tokens = g.tokens;
-  const int tiles = (it.tokens + a.tile_tokens - 1) / a.tile_tokens;
-  it.tile_begin = min(tiles, it.split * g.tiles_per_split);
-  it.tile_end = min(tiles, it.tile_begin + g.tiles_per_split);
+  it.tile_begin = min(g.tiles, it.split * g.tiles_per_split);
+  it.tile_end = min(g.tiles, it.tile_begin + g.tiles_per_split);
   return it;
 }
 
@@ -99,7 +100,7 @@ struct Sum2 {
     s = t;
   }
   // an infinite sum has no error term (it is NaN)
-  __device__ __forceinline__ double value() const { return (double)s + (isinf(s) ? 0.0 : (double)c); }
+  __device__ __forceinline__ float value() const { return isinf(s) ? s : s + c; }
 };
 
 // Has the phase completed?  Unlike try_wait this does not suspend the thread.
@@ -255,10 +256,10 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           // half; lane l ends with the keys from kLaneKeys * l on.
           float v[kGroupKeys];
 #pragma unroll
-          for (int p = 0; p < kGroupKeys / 2; ++p) {
-            unpack2(acc[p], v[2 * p], v[2 * p + 1]);
-            v[2 * p] = has_row ? v[2 * p] : 0.f;
-            v[2 * p + 1] = has_row ? v[2 * p + 1] : 0.f;
+          for (int p = 0; p < kGroupKeys / 2; ++p) unpack2(acc[p], v[2 * p], v[2 * p + 1]);
+          if (full != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < kGroupKeys; ++i) v[i] = has_row ? v[i] : 0.f;
           }
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) {
@@ -277,7 +278,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       // Lane groups 3, 2, 1, 0 add their sums in turn; group 0 writes the result.
       if (active) {
         const int first = kg * kGroupKeys + kLaneKeys * lane;
-        double sum[kLaneKeys];
+        float sum[kLaneKeys];
 #pragma unroll
         for (int i = 0; i < kLaneKeys; ++i) sum[i] = total[i].value();
         if (it.tile_begin < it.tile_end) {
@@ -286,8 +287,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           if (!ok) break;
 #pragma unroll
           for (int i = 0; i < kLaneKeys; ++i) {
-            if (lg < 3) sum[i] += (double)sy->hop_sum[first + i];
-            if (lg > 0) sy->hop_sum[first + i] = (float)sum[i];
+            if (lg < 3) sum[i] += sy->hop_sum[first + i];
+            if (lg > 0) sy->hop_sum[first + i] = sum[i];
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&sy->hop[kg][lg]));
@@ -300,10 +301,10 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
             const int t = it.key0 + first + i;
             if (t >= g.m) break;
             if (g.splits > 1) {
-              a.part[g.part_off + ((long long)it.split * a.Hkv + it.hk) * g.m + t] = (float)sum[i];
+              a.part[g.part_off + ((long long)it.split * a.Hkv + it.hk) * g.m + t] = sum[i];
             } else {
               const long long o = g.score_off + it.hk * a.head_stride + g.key0 + t;
-              a.out[o] = (float)((a.decay != 0.f ? (double)a.decay * (double)a.in[o] : 0.0) + sum[i]);
+              a.out[o] = (float)((a.decay != 0.f ? (double)a.decay * (double)a.in[o] : 0.0) + (double)sum[i]);
             }
           }
         }

@@ -127,6 +127,7 @@ class WeightLaunches {
     bool split = false;
     for (int i = 0; i < groups_; ++i) {
       const int tiles = tiles_of(g[i]);
+      g[i].tiles = tiles;
       g[i].splits = splits_of(tiles, best_tps);
       g[i].tiles_per_split = (tiles + g[i].splits - 1) / g[i].splits;
       g[i].item_begin = (int)item;
