@@ -306,9 +306,10 @@ class BiCache:
         """One layer of a stored prefix as dense rows: k_out, v_out [m, Hkv, D] (rows may be strided)."""
         assert k_out.is_cuda and v_out.is_cuda and k_out.dtype == self.dtype and k_out.shape == v_out.shape
         strides = k_out.stride()
-        assert strides[1:] == (self.D, 1) and v_out.stride() == strides
+        row, head, dim = strides
+        assert dim == 1 and head == self.D and v_out.stride() == strides
         st = self.lib.bicache_read_prefix_layer(self.ctx, prefix_id, layer, k_out.data_ptr(), v_out.data_ptr(),
-                                                strides[0], self._on_stream())
+                                                row, self._on_stream())
         self._check(st, "bicache_read_prefix_layer")
 
     def project_prefix_layer(self, prefix_id, layer, h, w_k, w_v, rope=None):

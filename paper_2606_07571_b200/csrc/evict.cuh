@@ -2,6 +2,7 @@
 // and the CUDA-core form of the accumulated attention weights (fp32, head dims other than 128).
 #pragma once
 #include <algorithm>
+#include <utility>
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include "common.cuh"
@@ -14,20 +15,30 @@ namespace bicache {
 // parameters (up to 32 KB since CUDA 12.1) and not through the workspace: nothing is uploaded, so a call
 // can be captured into a graph at any time and replayed beside other calls of the context.  A list that
 // does not fit is worked off in several launches.  A launch costs the host about 1 us per 8 KB of
-// parameters (select 4.5 us with 64 bytes, compact 8.3 us with 32 KB), so the kernels exist for lists of three lengths.
+// parameters (select 4.5 us with 64 bytes, compact 8.3 us with 32 KB), so the kernels exist for lists of four lengths.
 // ---------------------------------------------------------------------------------------------
 constexpr int kParamWords = 7936;               // 31,744 bytes: with the fixed fields below the 32,764 limit
-constexpr int kParamWordsMid = 2432, kParamWordsSmall = 896;
+using ParamLengths = std::integer_sequence<int, 224, 1216, 2432, kParamWords>;
 template <int kWords>
 struct ParamList {
   int w[kWords];
 };
 // f(list of the shortest length that holds the first `used` words of w)
+template <typename F, int kFirst, int... kRest>
+inline void with_param_list(const int* w, int used, F&& f, std::integer_sequence<int, kFirst, kRest...>) {
+  if constexpr (sizeof...(kRest) > 0) {
+    if (used > kFirst) return with_param_list(w, used, f, std::integer_sequence<int, kRest...>());
+  }
+  f(*reinterpret_cast<const ParamList<kFirst>*>(w));
+}
 template <typename F>
 inline void with_param_list(const int* w, int used, F&& f) {
-  if (used <= kParamWordsSmall) f(*reinterpret_cast<const ParamList<kParamWordsSmall>*>(w));
-  else if (used <= kParamWordsMid) f(*reinterpret_cast<const ParamList<kParamWordsMid>*>(w));
-  else f(*reinterpret_cast<const ParamList<kParamWords>*>(w));
+  with_param_list(w, used, f, ParamLengths());
+}
+// f(std::integral_constant) for every length
+template <typename F, int... kLengths>
+inline void each_param_length(F&& f, std::integer_sequence<int, kLengths...>) {
+  (f(std::integral_constant<int, kLengths>()), ...);
 }
 
 // ---------------------------------------------------------------------------------------------

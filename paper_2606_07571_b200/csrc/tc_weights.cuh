@@ -576,9 +576,10 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
 
 inline cudaError_t configure_tc_weights() {
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsSmall>, attr, wts::kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWordsMid>, attr, wts::kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<kParamWords>, attr, wts::kSmemBytes);
+  cudaError_t e = cudaSuccess;
+  each_param_length([&](auto words) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_weights_kernel<decltype(words)::value>, attr, wts::kSmemBytes);
+  }, ParamLengths());
   return e;
 }
 

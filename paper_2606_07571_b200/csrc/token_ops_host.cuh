@@ -479,15 +479,12 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
 cudaError_t configure_token_ops(bool tensor_ok) {
   cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
   const int ws = (int)weights_simt_smem(kSimtMaxD);
-  auto simt = [&](auto words) {
+  each_param_length([&](auto words) {
     constexpr int kWords = decltype(words)::value;
     const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
     if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<float, kWords>, attr, ws);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<__nv_bfloat16, kWords>, attr, ws);
-  };
-  simt(std::integral_constant<int, kParamWordsSmall>());
-  simt(std::integral_constant<int, kParamWordsMid>());
-  simt(std::integral_constant<int, kParamWords>());
+  }, ParamLengths());
   if (e == cudaSuccess && tensor_ok) e = configure_tc_weights();
   return e;
 }

@@ -430,6 +430,22 @@ def test_compact_of_more_pages_than_one_launch_takes():
     assert torch.equal(gk, want) and torch.equal(gv, -want)
 
 
+@pytest.mark.parametrize("pages", [100, 223, 224, 225, 1100, 1216, 1217, 2000, 2432, 2433, 3500])
+def test_lists_of_every_length(pages):
+    """The page lists travel as launch parameters of several lengths: weights, compaction and read-back around each."""
+    b = Batch((2, 1, 128), torch.bfloat16, [16 * pages - 3], [[5]], extra=pages // 2 + 1)
+    sin = b.fresh()
+    b.check(b.run(out := b.fresh(3), sin, 0.5), sin, 0.5)
+    keep = 16 * (pages // 2) + 1
+    dst, _, _ = b.bc.reserve_prefix(9, keep)
+    idx = torch.randint(0, b.m[0], (1, 1, keep), generator=gen(4), device="cuda", dtype=torch.int32)
+    b.bc.compact_prefix(b.pid[0], dst, idx)
+    for pid, m, want in ((dst, keep, b.k[0][0, idx[0, 0].long()]), (b.pid[0], b.m[0], b.k[0][0])):
+        gk, gv = read(b.bc, pid, 0, m)
+        assert torch.equal(gk, want) and torch.equal(gv, -want)
+    assert b.bc.device_status() == 0
+
+
 # ---------------------------------------------------------------------------------------------
 # together
 # ---------------------------------------------------------------------------------------------
