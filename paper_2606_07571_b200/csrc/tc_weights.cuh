@@ -407,8 +407,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       }
     } else {
       // ====================================== query rows ======================================
-      // One tile ahead of the copies, every lane looks up where its rows of the tile are and requests their
-      // log-sum-exps, so that neither stands between two tiles' copies.
+      // Every lane looks up where its rows of a tile are and requests their log-sum-exps while the rows of the tile
+      // before it are on their way, so that neither stands between two tiles' copies.
       const int w = warp - kRowWarp;                          // rows 64 w .. 64 w + 63 of every tile
       const int G = a.Hq / a.Hkv, T = a.tile_tokens;
       const int c16 = lane & 15;
@@ -501,11 +501,6 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           rows[i] = __ballot_sync(0xffffffffu, src[i] >= 0);
           from[i] = src[i];
         }
-        if (++tile >= tile_end) {
-          item += gridDim.x;
-          next_item();
-        }
-        if (item < a.num_items) look_up();
         const unsigned slot = qt % kQSlots;
         const unsigned q_free = smem_u32(&sy->q_free[slot]), free_parity = ((qt / kQSlots) & 1) ^ 1;
         const unsigned q_full = smem_u32(&sy->q_full[slot]);
@@ -540,20 +535,30 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           }
           cp_async_commit();
         }
-        // the log-sum-exps arrive while the rows are on their way
+        // the next tile of the item is looked up, and this one's log-sum-exps arrive, while the rows are on their way
+        const bool last_tile = tile + 1 >= tile_end;
+        if (!last_tile) {
+          ++tile;
+          look_up();
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           sy->neg_lse2[slot][w * 64 + i * 32 + lane] = isinf(row_lse[i]) ? -INFINITY : row_lse[i] * -1.4426950408889634f;
         if (boxes) {
           __syncwarp();                                       // lane 0 has announced the bytes
           mbar_arrive(q_full);
-          continue;
+        } else {
+          if (pending >= 0) {
+            cp_async_wait<1>();
+            announce();
+          }
+          pending = (int)slot;
         }
-        if (pending >= 0) {
-          cp_async_wait<1>();
-          announce();
+        if (last_tile) {                                      // the next item takes longer to work out
+          item += gridDim.x;
+          next_item();
+          if (item < a.num_items) look_up();
         }
-        pending = (int)slot;
       }
       cp_async_wait<0>();
       if (pending >= 0) announce();
