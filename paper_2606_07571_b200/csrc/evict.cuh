@@ -15,7 +15,7 @@ namespace bicache {
 // parameters (up to 32 KB since CUDA 12.1) and not through the workspace: nothing is uploaded, so a call
 // can be captured into a graph at any time and replayed beside other calls of the context.  A list that
 // does not fit is worked off in several launches.  A launch costs the host about 1 us per 8 KB of
-// parameters (select 4.5 us with 64 bytes, compact 8.3 us with 32 KB), so the kernels exist for lists of four lengths.
+// parameters (a call of 64 bytes takes 4.5 us, one of 32 KB 8.3), so the kernels exist for lists of four lengths.
 // ---------------------------------------------------------------------------------------------
 constexpr int kParamWords = 7936;               // 31,744 bytes: with the fixed fields below the 32,764 limit
 using ParamLengths = std::integer_sequence<int, 224, 1216, 2432, kParamWords>;
@@ -45,18 +45,21 @@ inline void each_param_length(F&& f, std::integer_sequence<int, kLengths...>) {
 // bicache_select_tokens: per row of scores the `keep` largest, protected ends first, ties to the lowest
 // index, as ascending indices.  Scores become unsigned integers in the same order.  The keep-th largest is
 // found digit by digit: 11 bits each, largest digit first, over the bits in which the row's scores differ
-// at all (narrow rows spread over the bins as wide ones do); the scores of the first digit's bin are gathered, the
-// further digits touch these only, and once they are few they are ranked against one another.  Then every
-// thread takes a run of scores into registers, counts what stays, learns its place from a scan, and puts the indices
-// into a list that leaves in order.
+// at all (narrow rows spread over the bins as wide ones do).  After the first digit every thread takes a run of the
+// row and keeps it as bits: what is above the digit's bin, what is inside.  Only what is inside is looked at again: its
+// range (many equal scores end the search), further digits if it is much, or a list on which it is ranked once it is
+// little.  Then a scan of the bits' counts gives every thread its place, and the indices go into a list that leaves
+// in order.
 //
 // Scores are read from memory once, in 16-byte loads, and stay in shared memory: one block per row, and a
 // cluster of up to 8 blocks, which read one another's counts through distributed shared memory, for rows that one
 // block cannot hold.  (Clusters for shorter rows were slower, for few rows as for many: a cluster barrier costs
 // about 1 us.)  A row too long for that is read again, from L2 as a rule, by every pass.
-// The bound for many rows is the instructions per score (about 1 us for each, for 36 M scores), then memory: 132 us for
-// 896 rows of 40,001 (144 MB read), where one read of the scores takes 28.  Few rows are bound by the latency of about
-// 15 phases between barriers: 9.3 us for 4 rows of 16,384.
+// The bound for many rows is the work on shared memory: 101 us for 896 rows of 40,001 (144 MB; one read takes 28), 29,000
+// cycles a row, of which reading 7000, the first digit's counts 5000 (3 to 5 cycles for 32 of them: banks
+// collide), the bits 3300, the list 4300, its way out 1500.  148 rows are a round; bringing the next round's rows into L2
+// meanwhile took 13 us off.  Few rows are bound by the latency of about 12 phases between barriers: 8.9 us for 4
+// rows of 16,384.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
@@ -65,7 +68,7 @@ constexpr int kSelBins = 1 << kSelDigitBits;
 constexpr int kSelGathered = kSelBins;          // scores of the first digit's bin that are kept apart
 constexpr int kSelRanked = 256;                 // at most so many are ranked directly
 constexpr int kSelStaged = 49152;               // scores of a block's part kept in shared memory (192 KB)
-constexpr int kSelRunQuads = 5;                 // scores / 4 of a thread's run: odd, so that runs start on different banks
+constexpr int kSelRunQuads = 5;                 // scores / 4 of a thread's run of a row that is not staged
 constexpr int kSelMaxRun = 13;                  // quads of a thread's run of a staged row, at most: 52 bits
 constexpr int kSelMaxCluster = 8;
 static_assert(kSelStaged / 4 <= 12 * kSelThreads, "a run and one quad more, where that makes it odd");
@@ -681,7 +684,7 @@ compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_consta
 }
 
 // gather_prefix_kernel (the layer read-back) with the page list in the parameters: no copy before the launch, which
-// is what a read-back of a short prefix otherwise waits for (14 us a call, 8 without).
+// is what a read-back of a short prefix otherwise waits for (14 us a call, 6.5 without).
 template <int kWords>
 __global__ void __launch_bounds__(kCompactThreads)
 read_layer_kernel(const char* __restrict__ pool_k, const char* __restrict__ pool_v, char* __restrict__ dst_k,

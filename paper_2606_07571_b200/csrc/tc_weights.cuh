@@ -10,7 +10,7 @@
 //
 // What bounds it: one exponential per (row, key) against 256 flops of the product.  An SM computes 16
 // exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a tile of 128 x
-// 256 takes 2048 cycles of the one and 1024 of the other; it takes 2330 (4.1 ms, 87 % of the unit's rate).  A
+// 256 takes 2048 cycles of the one and 1024 of the other; it takes 2330 (4.2 ms, 86 % of the unit's rate).  A
 // polynomial on the FMA pipe for two of every eight pairs, which is faster by itself (116 cycles against 135 for 16
 // keys of four warps), gained nothing here: the packed instructions take two issue slots each, and with the
 // loaders' warps beside them the schedulers are full (4.2 ms; without the register split that it needs, 5.8).
