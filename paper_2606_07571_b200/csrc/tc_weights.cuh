@@ -91,6 +91,17 @@ __device__ __forceinline__ Item read_item(const WeightArgs& a, const int* list, 
   return it;
 }
 
+// The items of a CTA: dealt out forth and back (0 1 2 | 2 1 0 | 0 1 2 ..), since they get shorter towards the end: over
+// random batches of 2 to 8 prefixes the fullest SM has 7 % more than the mean, 10 % if every round starts with CTA 0.
+struct ItemWalk {
+  int item, step;
+  __device__ __forceinline__ ItemWalk() : item(blockIdx.x), step(2 * (gridDim.x - blockIdx.x) - 1) {}
+  __device__ __forceinline__ void next() {
+    item += step;
+    step = 2 * gridDim.x - step;
+  }
+};
+
 // A running sum with its rounding error carried along (the sums run over up to millions of rows).
 struct Sum2 {
   float s, c;
@@ -194,8 +205,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
     unsigned handed = 0;                                      // items whose sums went from group to group
     const unsigned q_full0 = smem_u32(&sy->q_full[0]), q_free0 = smem_u32(&sy->q_free[0]);
     const unsigned s_full0 = smem_u32(&sy->s_full[0]), s_free0 = smem_u32(&sy->s_free[0]);
-    for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-      const Item it = read_item(a, list, item);
+    for (ItemWalk at; at.item < a.num_items && ok; at.next()) {
+      const Item it = read_item(a, list, at.item);
       const bool active = it.keys > kg * kGroupKeys;
       Sum2 total[kLaneKeys];                                  // keys kLaneKeys * lane .., over this lane group
 #pragma unroll
@@ -325,8 +336,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       // further in a row tile
       auto kstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 64); };
       auto qstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 1024); };
-      for (int item = blockIdx.x; item < a.num_items && ok; item += gridDim.x) {
-        if (item != blockIdx.x) it = read_item(a, list, item);
+      for (ItemWalk at; at.item < a.num_items && ok; at.next()) {
+        if (at.item != blockIdx.x) it = read_item(a, list, at.item);
         if (it.tile_begin >= it.tile_end) continue;           // no rows: no keys are staged either
         const unsigned ks = kt % kKSlots;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_full[ks]), (kt / kKSlots) & 1, abort_flag));
@@ -389,12 +400,12 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         ++kt;
       };
       // the first item's keys need no free slot and nobody else's barriers
-      int item = blockIdx.x;
+      ItemWalk at;
       if (it.tile_begin < it.tile_end) fetch();
       set_up();
       bool ok = !dead;
-      for (item += gridDim.x; item < a.num_items && ok; item += gridDim.x) {
-        it = read_item(a, list, item);
+      for (at.next(); at.item < a.num_items && ok; at.next()) {
+        it = read_item(a, list, at.item);
         if (it.tile_begin >= it.tile_end) continue;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[kt % kKSlots]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
         if (ok) fetch();
@@ -432,7 +443,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         mbar_arrive(smem_u32(&sy->q_full[pending]));
         pending = -1;
       };
-      int item = blockIdx.x, tile = 0, tile_end = 0, tokens = 0, hk = 0, segs = 0;
+      ItemWalk at;
+      int tile = 0, tile_end = 0, tokens = 0, hk = 0, segs = 0;
       const WeightSeg* seg = nullptr;
       // the runs of rows the lane's two rows and the tile's first token are in: number, end, row of token 0
       int run[3], run_end[3];
@@ -443,8 +455,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         run_end[i] = number + 1 < segs ? seg[number + 1].token : 0x7fffffff;
       };
       auto next_item = [&]() {                                // to the next item that has row tiles
-        for (; item < a.num_items; item += gridDim.x) {
-          if (item != blockIdx.x) it = read_item(a, list, item);
+        for (; at.item < a.num_items; at.next()) {
+          if (at.item != blockIdx.x) it = read_item(a, list, at.item);
           if (it.tile_begin >= it.tile_end) continue;
           const WeightGroup& g = weight_group(list, it.g);
           tile = it.tile_begin;
@@ -486,10 +498,10 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         }
       };
       next_item();
-      if (item < a.num_items) look_up();
+      if (at.item < a.num_items) look_up();
       set_up();
       bool ok = !dead;
-      while (item < a.num_items && ok) {
+      while (at.item < a.num_items && ok) {
         const int box_head = hk * G, box_first = (int)box_row;
         const bool boxes = one_run;
         float row_lse[2];
@@ -555,9 +567,9 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
           pending = (int)slot;
         }
         if (last_tile) {                                      // the next item takes longer to work out
-          item += gridDim.x;
+          at.next();
           next_item();
-          if (item < a.num_items) look_up();
+          if (at.item < a.num_items) look_up();
         }
       }
       cp_async_wait<0>();

@@ -94,25 +94,27 @@ class WeightLaunches {
     }
     // How many row tiles an item covers at most.  Fewer tiles make more items, which fill the SMs evenly, but every
     // item costs its start and the sum over its lanes (about two tiles, 2.5 us) and more than one range per key the
-    // second kernel (about three).  Counted in tiles: the fullest SM, items being dealt out in turn.
+    // second kernel (about three).  Counted in tiles: the fullest SM, items being dealt out forth and back.
     const int slots = tensor_ ? ctx_->sm_count : 2 * ctx_->sm_count;
     const int choices = std::min(max_tiles, std::max(4, 128 / groups_));
     auto splits_of = [&](int tiles, int tps) { return std::max(1, (tiles + tps - 1) / tps); };
     std::vector<int> load(slots);
     int best_tps = max_tiles;
     long long best = 0x7fffffffffffffffLL;
-    for (int s = 1; s <= std::min(choices, 32); ++s) {
+    for (int s = 1, before = 0; s <= std::min(choices, 32); ++s) {
       const int tps = (max_tiles + s - 1) / s;
+      if (tps == before) continue;
+      before = tps;
       long long part = 0, even = 0;
       int at = 0;
       std::fill(load.begin(), load.end(), 0);
       for (int i = 0; i < groups_; ++i) {
         const int tiles = tiles_of(g[i]), sp = splits_of(tiles, tps), cost = (tiles + sp - 1) / sp + 2;
         const long long items = (long long)g[i].key_blocks * a.Hkv * sp;
-        even += items / slots * cost;
-        for (int left = (int)(items % slots); left > 0; --left) {
-          load[at] += cost;
-          at = at + 1 == slots ? 0 : at + 1;
+        even += items / (2 * slots) * 2 * cost;                   // two rounds bring two items to each
+        for (int left = (int)(items % (2 * slots)); left > 0; --left) {
+          load[at < slots ? at : 2 * slots - 1 - at] += cost;
+          at = at + 1 == 2 * slots ? 0 : at + 1;
         }
         if (sp > 1) part += (long long)sp * a.Hkv * g[i].m;
       }
