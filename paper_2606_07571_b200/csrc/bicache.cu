@@ -1187,16 +1187,15 @@ int32_t bicache_read_prefix_layer(bicache_ctx* ctx, int32_t prefix_id, int32_t l
   const std::vector<int32_t>& pages = pages_of(e, layer);
   const int need = (int)pages.size();
   const int chunks_per_row = cfg.head_dim * ctx->esize / 16;
-  const long long total = (long long)e.m * cfg.num_kv_heads * chunks_per_row;
-  const int threads = 256;
-  const int blocks = (int)std::min<long long>((total + threads - 1) / threads, (long long)ctx->sm_count * 16);
+  const long long rows = (long long)e.m * cfg.num_kv_heads;
   const PoolView pv = pool_view(ctx);
   cudaError_t ce = cudaSuccess;
-  if (e.m > 0 && need <= kParamWords) {                 // the page list fits the launch parameters
+  if (e.m > 0 && need <= kParamWords && rows <= 0x7fffffffLL) {      // the page list fits the launch parameters
+    const int blocks = copy_blocks(rows, chunks_per_row, ctx->sm_count);
     int list[kParamWords];
     std::memcpy(list, pages.data(), sizeof(int) * need);
     with_param_list(list, need, [&](const auto& params) {
-      read_layer_kernel<<<blocks, threads, 0, stream>>>(
+      read_layer_kernel<<<blocks, kCompactThreads, 0, stream>>>(
           pv.k + ctx->layer_off[layer], pv.v + ctx->layer_off[layer], static_cast<char*>(k_out),
           static_cast<char*>(v_out), e.m, cfg.num_kv_heads, chunks_per_row, kv_row_stride * ctx->esize, pv.page_bytes,
           pv.swizzled, params);
@@ -1204,6 +1203,9 @@ int32_t bicache_read_prefix_layer(bicache_ctx* ctx, int32_t prefix_id, int32_t l
     ctx->launches++;
     ce = cudaGetLastError();
   } else if (e.m > 0) {
+    const int threads = 256;
+    const int blocks =
+        (int)std::min<long long>((rows * chunks_per_row + threads - 1) / threads, (long long)ctx->sm_count * 16);
     ce = cudaMemcpyAsync(ctx->d_put_pages, pages.data(), sizeof(int) * need, cudaMemcpyHostToDevice, stream);
     if (ce == cudaSuccess) {
       gather_prefix_kernel<<<blocks, threads, 0, stream>>>(

@@ -621,10 +621,10 @@ inline cudaError_t launch_select(SelectArgs a, long long rows, int sm_count, cud
 // bicache_compact_prefix: token i of head j of the shorter prefix becomes token idx[layer][j][i] of the
 // longer one, K and V.  A page image keeps a token's dims in two runs of 128 bytes (or one of D elements),
 // and the 16-byte chunks of a run are permuted inside it, so the copy goes chunk by chunk: half a warp
-// moves one token of one head (D = 128, bf16).  Unused slots of the last page become zero, as everywhere.
+// moves one token of one head (D = 128, bf16), a thread the same chunk of every row it comes to.  Unused slots of the last page become zero, as everywhere.
 // An index outside the prefix leaves a zero token and raises the status word.
-// Bound by memory: 8192 of 16,384 tokens, 32 heads, 4 layers (1.07 GB read and written) take 174 us, 96 % of a plain
-// copy's bandwidth; a single layer of 1001 tokens and 4 heads takes 2.8 us.
+// Bound by memory: 8192 of 16,384 tokens, 32 heads, 4 layers (1.07 GB read and written) take 169 us, 98 % of a plain
+// copy's bandwidth; a single layer of 1001 tokens and 4 heads takes 2.5 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCompactThreads = 256;
 struct CompactArgs {
@@ -643,22 +643,18 @@ struct CompactArgs {
 template <int kWords>
 __global__ void __launch_bounds__(kCompactThreads)
 compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_constant__ ParamList<kWords> list) {
-  const int slots = a.dst_pages * kPageSize;
-  const long long per_layer = (long long)slots * a.num_kv_heads * a.chunks_per_row;
-  const long long total = per_layer * a.num_layers;
-  const int row_bytes = a.chunks_per_row * 16;
-  for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < total;
-       i += (long long)gridDim.x * blockDim.x) {
-    const int layer = (int)(i / per_layer);
-    long long rem = i - layer * per_layer;
-    const int c16 = (int)(rem % a.chunks_per_row); rem /= a.chunks_per_row;
-    const int slot = (int)(rem % kPageSize); rem /= kPageSize;
-    const int hk = (int)(rem % a.num_kv_heads);
-    const int pg = (int)(rem / a.num_kv_heads);
-    const int t = (a.dst_first + pg) * kPageSize + slot;
+  const unsigned heads = a.num_kv_heads, dst_pages = a.dst_pages;
+  const unsigned rows = kPageSize * heads * dst_pages * (unsigned)a.num_layers;      // a row: a token of a head
+  const unsigned per_block = kCompactThreads / a.chunks_per_row, first = threadIdx.x / a.chunks_per_row;
+  const int c16 = threadIdx.x - first * a.chunks_per_row, row_bytes = a.chunks_per_row * 16;
+  if (first >= per_block) return;
+  for (unsigned r = blockIdx.x * per_block + first; r < rows; r += gridDim.x * per_block) {
+    const unsigned slot = r % kPageSize, page = r / kPageSize / heads, hk = r / kPageSize - page * heads;
+    const unsigned layer = page / dst_pages, pg = page - layer * dst_pages;
+    const int t = (a.dst_first + (int)pg) * kPageSize + (int)slot;
     uint4 k = make_uint4(0, 0, 0, 0), v = k;
     bool write = a.src_first == 0;                          // padding and bad indices: by the first window
-    const long long lb = layer * a.layer_bytes;
+    const long long head = layer * a.layer_bytes + (long long)hk * a.page_bytes;
     if (t < a.keep) {
       const int s = a.idx[layer * a.idx_layer_stride + hk * a.idx_head_stride + t];
       if (s < 0 || s >= a.src_m) {
@@ -667,7 +663,7 @@ compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_consta
         const int sp = s / kPageSize - a.src_first;
         write = sp >= 0 && sp < a.src_pages;
         if (write) {
-          const long long so = lb + ((long long)list.w[sp] * a.num_kv_heads + hk) * a.page_bytes +
+          const long long so = head + (long long)list.w[sp] * heads * a.page_bytes +
                                page_chunk_offset(a.swizzled != 0, s % kPageSize, c16, row_bytes);
           k = *reinterpret_cast<const uint4*>(a.pool_k + so);
           v = *reinterpret_cast<const uint4*>(a.pool_v + so);
@@ -675,10 +671,10 @@ compact_prefix_kernel(const __grid_constant__ CompactArgs a, const __grid_consta
       }
     }
     if (write) {
-      const long long po = lb + ((long long)list.w[a.src_pages + pg] * a.num_kv_heads + hk) * a.page_bytes +
-                           page_chunk_offset(a.swizzled != 0, slot, c16, row_bytes);
-      *reinterpret_cast<uint4*>(a.pool_k + po) = k;
-      *reinterpret_cast<uint4*>(a.pool_v + po) = v;
+      const long long to = head + (long long)list.w[a.src_pages + pg] * heads * a.page_bytes +
+                           page_chunk_offset(a.swizzled != 0, (int)slot, c16, row_bytes);
+      *reinterpret_cast<uint4*>(a.pool_k + to) = k;
+      *reinterpret_cast<uint4*>(a.pool_v + to) = v;
     }
   }
 }
@@ -690,20 +686,24 @@ __global__ void __launch_bounds__(kCompactThreads)
 read_layer_kernel(const char* __restrict__ pool_k, const char* __restrict__ pool_v, char* __restrict__ dst_k,
                   char* __restrict__ dst_v, int m, int num_kv_heads, int chunks_per_row, long long dst_row_stride_bytes,
                   int page_bytes, int swizzled, const __grid_constant__ ParamList<kWords> pages) {
-  const long long total = (long long)m * num_kv_heads * chunks_per_row;
-  const int row_bytes = chunks_per_row * 16;
-  for (long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x; idx < total;
-       idx += (long long)gridDim.x * blockDim.x) {
-    long long rem = idx;
-    const int c16 = (int)(rem % chunks_per_row); rem /= chunks_per_row;
-    const int hk = (int)(rem % num_kv_heads); rem /= num_kv_heads;
-    const int t = (int)rem;
-    const long long po = ((long long)pages.w[t / kPageSize] * num_kv_heads + hk) * page_bytes +
-                         page_chunk_offset(swizzled != 0, t % kPageSize, c16, row_bytes);
-    const long long d = (long long)t * dst_row_stride_bytes + (long long)hk * row_bytes + c16 * 16;
-    *reinterpret_cast<uint4*>(dst_k + d) = *reinterpret_cast<const uint4*>(pool_k + po);
-    *reinterpret_cast<uint4*>(dst_v + d) = *reinterpret_cast<const uint4*>(pool_v + po);
+  const unsigned heads = num_kv_heads, rows = (unsigned)m * heads;
+  const unsigned per_block = kCompactThreads / chunks_per_row, first = threadIdx.x / chunks_per_row;
+  const int c16 = threadIdx.x - first * chunks_per_row, row_bytes = chunks_per_row * 16;
+  if (first >= per_block) return;
+  for (unsigned r = blockIdx.x * per_block + first; r < rows; r += gridDim.x * per_block) {
+    const unsigned t = r / heads, hk = r - t * heads;
+    const long long po = ((long long)pages.w[t / kPageSize] * heads + hk) * page_bytes +
+                         page_chunk_offset(swizzled != 0, (int)(t % kPageSize), c16, row_bytes);
+    const long long to = t * dst_row_stride_bytes + (long long)hk * row_bytes + c16 * 16;
+    *reinterpret_cast<uint4*>(dst_k + to) = *reinterpret_cast<const uint4*>(pool_k + po);
+    *reinterpret_cast<uint4*>(dst_v + to) = *reinterpret_cast<const uint4*>(pool_v + po);
   }
+}
+// Blocks for `rows` rows of one of the two kernels: eight rounds of resident ones at most.  (One round: 189 us for both
+// kernels on 4 layers of 8192 x 32 rows where eight take 169; two rows to a thread at a time: 185 and 170.)
+inline int copy_blocks(long long rows, int chunks_per_row, int sm_count) {
+  const long long per_block = kCompactThreads / chunks_per_row;
+  return (int)std::min<long long>((rows + per_block - 1) / per_block, 64LL * sm_count);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -345,7 +345,9 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
   a.keep = dst.m;
   a.status = ctx->d_status;
   // one launch for all layers if they share page lists and places, else one per layer
-  const bool together = src.uniform && dst.uniform && ctx->uniform_caps;
+  const long long max_pages = (1LL << 31) / ((long long)kPageSize * cfg.num_kv_heads);     // rows are counted in 32 bits
+  const bool together = src.uniform && dst.uniform && ctx->uniform_caps &&
+                        (long long)pages_of(dst, first_layer).size() * num_layers <= max_pages;
   const int step = together ? num_layers : 1;
   int list[kParamWords];
   for (int l = first_layer; l < first_layer + num_layers; l += step) {
@@ -353,6 +355,7 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
     const int ns = (int)sp.size(), nd = (int)dp.size();
     const bool fits = ns + nd <= kParamWords;
     const int s_step = fits ? ns : kParamWords / 2, d_step = fits ? nd : kParamWords / 2;
+    if (d_step > max_pages) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "too many heads");
     a.pool_k = static_cast<char*>(cfg.k_pool) + ctx->layer_off[l];
     a.pool_v = static_cast<char*>(cfg.v_pool) + ctx->layer_off[l];
     a.idx = idx + (l - first_layer) * idx_layer_stride;
@@ -365,8 +368,7 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
         a.dst_pages = std::min(d_step, nd - d0);
         std::memcpy(list, sp.data() + s0, sizeof(int) * a.src_pages);
         std::memcpy(list + a.src_pages, dp.data() + d0, sizeof(int) * a.dst_pages);
-        const long long chunks = (long long)step * a.dst_pages * kPageSize * cfg.num_kv_heads * a.chunks_per_row;
-        const int blocks = (int)std::min<long long>((chunks + kCompactThreads - 1) / kCompactThreads, (long long)ctx->sm_count * 16);
+        const int blocks = copy_blocks((long long)step * a.dst_pages * kPageSize * cfg.num_kv_heads, a.chunks_per_row, ctx->sm_count);
         with_param_list(list, a.src_pages + a.dst_pages, [&](const auto& params) {
           compact_prefix_kernel<<<blocks, kCompactThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, params);
         });
