@@ -354,8 +354,8 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
     const std::vector<int32_t>&sp = pages_of(src, l), &dp = pages_of(dst, l);
     const int ns = (int)sp.size(), nd = (int)dp.size();
     const bool fits = ns + nd <= kParamWords;
-    const int s_step = fits ? ns : kParamWords / 2, d_step = fits ? nd : kParamWords / 2;
-    if (d_step > max_pages) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "too many heads");
+    const int s_step = fits ? ns : kParamWords / 2;
+    const int d_step = (int)std::min<long long>(fits ? nd : kParamWords / 2, max_pages);
     a.pool_k = static_cast<char*>(cfg.k_pool) + ctx->layer_off[l];
     a.pool_v = static_cast<char*>(cfg.v_pool) + ctx->layer_off[l];
     a.idx = idx + (l - first_layer) * idx_layer_stride;
