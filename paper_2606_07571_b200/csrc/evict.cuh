@@ -712,7 +712,7 @@ inline int copy_blocks(long long rows, int chunks_per_row, int sm_count) {
 //                  exp(scale q[a][h] . k[t][j] - lse[a][h]);
 // rows with an infinite lse add nothing.  The batch: groups (one per prefix), the runs of query rows that
 // belong to each, and their page lists, all in the parameter list.  Row space of a group: the tokens of its
-// requests one after the other, packed row p = token * G + head in the KV group, cut into row tiles (of 64 rows in
+// requests one after the other, packed row p = token * G + head in the KV group, cut into row tiles (of 128 rows in
 // the CUDA-core form, of whole tokens in the other).  A
 // work item is one block of keys against a range of row tiles; with several ranges (splits) the items
 // write partial sums and a second kernel adds them in a fixed order.
@@ -776,19 +776,35 @@ __device__ __forceinline__ long long weight_row(const int* list, const WeightGro
   return s[lo].row + (tok - s[lo].token);
 }
 
-// CUDA-core form.  Block: 64 keys against tiles of 64 packed rows, each thread 4 keys x 4 rows, dims in
-// shared memory as fp32 (rows padded by 4 floats: the 16-byte reads of a quarter warp fall on different
-// banks).  The sums over rows are kept in fp64 per thread and added across the 16 threads of a key at the end.
-// Bound by the fp32 products out of shared memory and the fp64 additions; bf16 with head_dim 128 takes the other form.
-constexpr int kWsKeys = 64, kWsRows = 64, kWsThreads = 256;
-inline size_t weights_simt_smem(int D) { return sizeof(float) * ((size_t)(kWsKeys + kWsRows) * (D + 4) + kWsRows); }
+// CUDA-core form.  Block: 16 * kPerThread keys against tiles of 128 packed rows, each thread kPerThread keys x 8 rows,
+// dims in shared memory as fp32 (rows padded by 4 floats: the 16-byte reads of a quarter warp fall on different
+// banks).  A thread adds the exponentials of a tile's eight rows in fp32 and keeps the sums over tiles in fp64; those
+// of the 16 threads of a key are added at the end.
+// Bound by the fp32 products and the shared-memory reads that feed them: with 8 x 8 a step of four dims is 16 reads (64
+// cycles of an SM's 128 bytes a cycle for a warp) for 256 products (64 cycles); with 4 x 8 it is 48 against 32.  So it is
+// eight keys to a thread, but four where eight do not fit shared memory (head dims past 192) and where a batch has not a
+// block for every SM (fp32, 4 heads of 64 dims: 2048 rows over 4096 keys 157 us with eight, 207 with four; 100 rows over
+// 1000 keys 16.2 and 11.8).  The first is 28 TFLOP/s; products alone, from registers, reach 52 on this part.  bf16 with
+// head_dim 128 takes the tensor-core form.
+constexpr int kWsRows = 128, kWsThreads = 256;
+constexpr int kWsAhead = 4;                             // loads of query rows a thread has on their way
+constexpr int kWsEightMaxD = 192;
+inline size_t weights_simt_smem(int D, int per_thread) {
+  return sizeof(float) * ((size_t)(16 * per_thread + kWsRows) * (D + 4) + kWsRows);
+}
 
-template <typename T, int kWords>
-__global__ void __launch_bounds__(kWsThreads)
+__device__ __forceinline__ float exp2_approx(float x) {                  // 2 ulp; 0 below 2^-126
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T, int kPerThread, int kWords>
+__global__ void __launch_bounds__(kWsThreads, 2)
 weights_simt_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ ParamList<kWords> params) {
   const int* const list = params.w;
   using Tr = ElemTraits<T>;
-  constexpr int kEsize = (int)sizeof(T), kPer = Tr::kPerChunk;
+  constexpr int kEsize = (int)sizeof(T), kPer = Tr::kPerChunk, kWsKeys = 16 * kPerThread;
   extern __shared__ float ws_smem[];
   const int D = a.D, pitch = D + 4, chunks = D / kPer;
   float* const ks = ws_smem;
@@ -813,60 +829,83 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a, const __grid_constant_
 #pragma unroll
     for (int e = 0; e < kPer; ++e) ks[key * pitch + c * kPer + e] = f[e];
   }
-  double total[4] = {0.0, 0.0, 0.0, 0.0};
+  double total[kPerThread] = {};
+  const float scale_log2 = a.scale * 1.4426950408889634f;
   const long long rows = (long long)g.tokens * G;
   const int tiles = (int)((rows + kWsRows - 1) / kWsRows);
   const int tile_begin = split * g.tiles_per_split, tile_end = min(tiles, tile_begin + g.tiles_per_split);
+  // a thread loads one chunk of every row it comes to
+  const int per_pass = kWsThreads / chunks, first = tid / chunks, c = tid - first * chunks;
+  const int load_end = first < per_pass ? kWsRows : 0;
   for (int tile = tile_begin; tile < tile_end; ++tile) {
+    const long long p0 = (long long)tile * kWsRows;
+    const int here = (int)min((long long)kWsRows, rows - p0);
     __syncthreads();                                    // the last tile's rows have been used
-    for (int i = tid; i < kWsRows * chunks; i += kWsThreads) {
-      const int r = i / chunks, c = i - r * chunks;
-      const long long p = (long long)tile * kWsRows + r;
-      float f[kPer];
+    for (int r0 = first; r0 < load_end; r0 += kWsAhead * per_pass) {
+      uint4 x[kWsAhead];
+      float l[kWsAhead];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) f[e] = 0.f;
-      float l = INFINITY;
-      if (p < rows) {
-        const int tok = (int)(p / G), h = hk * G + (int)(p - (long long)tok * G);
-        const long long row = weight_row(list, g, tok);
-        l = a.lse[row * a.Hq + h];
-        if (!isinf(l)) Tr::unpack(*reinterpret_cast<const uint4*>(a.q + (row * a.q_stride + (long long)h * D) * kEsize + c * 16), f);
+      for (int u = 0; u < kWsAhead; ++u) {
+        const int r = r0 + u * per_pass;
+        x[u] = make_uint4(0, 0, 0, 0);
+        l[u] = INFINITY;
+        if (r < here) {
+          const int tok = (int)((p0 + r) / G), h = hk * G + (int)(p0 + r - (long long)tok * G);
+          const long long row = weight_row(list, g, tok);
+          x[u] = *reinterpret_cast<const uint4*>(a.q + (row * a.q_stride + (long long)h * D) * kEsize + c * 16);
+          if (c == 0) l[u] = a.lse[row * a.Hq + h];
+        }
       }
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) qs[r * pitch + c * kPer + e] = f[e];
-      if (c == 0) ls[r] = l;
+      for (int u = 0; u < kWsAhead; ++u) {
+        const int r = r0 + u * per_pass;
+        if (r >= kWsRows) break;
+        float f[kPer];
+        Tr::unpack(x[u], f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) qs[r * pitch + c * kPer + e] = f[e];
+        if (c == 0) ls[r] = l[u];
+      }
     }
     __syncthreads();
-    float acc[4][4] = {};
-    for (int d = 0; d < D; d += 4) {
-      float4 kf[4], qf[4];
+    auto sum_rows = [&](auto count) {                   // the first 16 * count rows of the tile
+      constexpr int kRows = decltype(count)::value;
+      float acc[kPerThread][kRows] = {};
+      for (int d = 0; d < D; d += 4) {
+        float4 kf[kPerThread];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        kf[i] = *reinterpret_cast<const float4*>(&ks[(tx + 16 * i) * pitch + d]);
-        qf[i] = *reinterpret_cast<const float4*>(&qs[(ty + 16 * i) * pitch + d]);
+        for (int i = 0; i < kPerThread; ++i) kf[i] = *reinterpret_cast<const float4*>(&ks[(tx + 16 * i) * pitch + d]);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+          const float4 qf = *reinterpret_cast<const float4*>(&qs[(ty + 16 * j) * pitch + d]);
+#pragma unroll
+          for (int i = 0; i < kPerThread; ++i) {
+            acc[i][j] = fmaf(kf[i].x, qf.x, acc[i][j]);
+            acc[i][j] = fmaf(kf[i].y, qf.y, acc[i][j]);
+            acc[i][j] = fmaf(kf[i].z, qf.z, acc[i][j]);
+            acc[i][j] = fmaf(kf[i].w, qf.w, acc[i][j]);
+          }
+        }
+      }
+      float sum[kPerThread] = {};
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+        const float l = ls[ty + 16 * j];
+        if (isinf(l)) continue;                         // masked or past the end, whatever the product is
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) sum[i] += exp2_approx(fmaf(scale_log2, acc[i][j], l * -1.4426950408889634f));
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          acc[i][j] = fmaf(kf[i].x, qf[j].x, acc[i][j]);
-          acc[i][j] = fmaf(kf[i].y, qf[j].y, acc[i][j]);
-          acc[i][j] = fmaf(kf[i].z, qf[j].z, acc[i][j]);
-          acc[i][j] = fmaf(kf[i].w, qf[j].w, acc[i][j]);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float l = ls[ty + 16 * j];
-      if (isinf(l)) continue;                           // masked or past the end, whatever the product is
-#pragma unroll
-      for (int i = 0; i < 4; ++i) total[i] += (double)expf(fmaf(a.scale, acc[i][j], -l));
-    }
+      for (int i = 0; i < kPerThread; ++i) total[i] += (double)sum[i];
+    };
+    if (here <= 16) sum_rows(std::integral_constant<int, 1>());
+    else if (here <= 64) sum_rows(std::integral_constant<int, 4>());
+    else sum_rows(std::integral_constant<int, 8>());
   }
   __syncthreads();
-  double* const red = reinterpret_cast<double*>(ws_smem);          // [16][64]
+  double* const red = reinterpret_cast<double*>(ws_smem);          // [16][kWsKeys]
 #pragma unroll
-  for (int i = 0; i < 4; ++i) red[ty * kWsKeys + tx + 16 * i] = total[i];
+  for (int i = 0; i < kPerThread; ++i) red[ty * kWsKeys + tx + 16 * i] = total[i];
   __syncthreads();
   if (tid < kWsKeys && key_begin + tid < g.m) {
     double s = 0.0;
@@ -880,7 +919,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a, const __grid_constant_
     }
   }
 }
-static_assert(16 * kWsKeys * sizeof(double) <= sizeof(float) * (kWsKeys + kWsRows) * (32 + 4), "the sums are added over the tiles");
+static_assert(16 * 128 * sizeof(double) <= sizeof(float) * (128 + kWsRows) * (32 + 4), "the sums are added over the tiles");
 
 // The partial sums of the row ranges, added in order.  One thread per (KV head, key) of a group with splits.
 template <int kWords>

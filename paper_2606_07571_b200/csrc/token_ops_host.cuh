@@ -82,9 +82,12 @@ class WeightLaunches {
       a.decay = 1.f;
       a.in = a.out;
     }
-    const int block_keys = tensor_ ? wts::kItemKeys : kWsKeys;
     WeightGroup* g = reinterpret_cast<WeightGroup*>(list_);
     int max_tiles = 1, max_m = 1;
+    long long blocks8 = 0;                                            // CUDA-core form: 128 keys against a row tile
+    for (int i = 0; i < groups_; ++i) blocks8 += (long long)((g[i].m + 127) / 128) * a.Hkv * tiles_of(g[i]);
+    const int per_thread = a.D <= kWsEightMaxD && blocks8 >= ctx_->sm_count ? 8 : 4;
+    const int block_keys = tensor_ ? wts::kItemKeys : 16 * per_thread;
     // long groups first: the short items of the others even out what these leave
     std::stable_sort(g, g + groups_, [&](const WeightGroup& x, const WeightGroup& y) { return tiles_of(x) > tiles_of(y); });
     for (int i = 0; i < groups_; ++i) {
@@ -95,7 +98,7 @@ class WeightLaunches {
     // How many row tiles an item covers at most.  Fewer tiles make more items, which fill the SMs evenly, but every
     // item costs its start and the sum over its lanes (about two tiles, 2.5 us) and more than one range per key the
     // second kernel (about three).  Counted in tiles: the fullest SM, items being dealt out forth and back.
-    const int slots = tensor_ ? ctx_->sm_count : 2 * ctx_->sm_count;
+    const int slots = tensor_ || weights_simt_smem(a.D, per_thread) > 113 * 1024 ? ctx_->sm_count : 2 * ctx_->sm_count;
     const int choices = std::min(max_tiles, std::max(4, 128 / groups_));
     auto splits_of = [&](int tiles, int tps) { return std::max(1, (tiles + tps - 1) / tps); };
     std::vector<int> load(slots);
@@ -156,11 +159,11 @@ class WeightLaunches {
       if (tensor_) {
         e = launch_tc_weights(a, q_map_, list, ctx_->d_status, ctx_->sm_count, ctx_->wait_cycles, stream_);
       } else {
-        const size_t smem = weights_simt_smem(a.D);
-        if (ctx_->cfg.dtype == BICACHE_F32)
-          weights_simt_kernel<float, kWords><<<a.num_items, kWsThreads, smem, stream_>>>(a, list);
-        else
-          weights_simt_kernel<__nv_bfloat16, kWords><<<a.num_items, kWsThreads, smem, stream_>>>(a, list);
+        const size_t smem = weights_simt_smem(a.D, per_thread);
+        const bool f32 = ctx_->cfg.dtype == BICACHE_F32, eight = per_thread == 8;
+        auto* const kernel = f32 ? (eight ? weights_simt_kernel<float, 8, kWords> : weights_simt_kernel<float, 4, kWords>)
+                                 : (eight ? weights_simt_kernel<__nv_bfloat16, 8, kWords> : weights_simt_kernel<__nv_bfloat16, 4, kWords>);
+        kernel<<<a.num_items, kWsThreads, smem, stream_>>>(a, list);
         e = cudaGetLastError();
       }
       ctx_->launches++;
@@ -482,12 +485,16 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
 
 cudaError_t configure_token_ops(bool tensor_ok) {
   cudaError_t e = cudaFuncSetAttribute(select_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelStaged * 4);
-  const int ws = (int)weights_simt_smem(kSimtMaxD);
   each_param_length([&](auto words) {
     constexpr int kWords = decltype(words)::value;
-    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<float, kWords>, attr, ws);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_simt_kernel<__nv_bfloat16, kWords>, attr, ws);
+    auto allow = [&](const void* kernel, int most, int per_thread) {
+      if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)weights_simt_smem(most, per_thread));
+    };
+    allow((const void*)weights_simt_kernel<float, 8, kWords>, kWsEightMaxD, 8);
+    allow((const void*)weights_simt_kernel<__nv_bfloat16, 8, kWords>, kWsEightMaxD, 8);
+    allow((const void*)weights_simt_kernel<float, 4, kWords>, kSimtMaxD, 4);
+    allow((const void*)weights_simt_kernel<__nv_bfloat16, 4, kWords>, kSimtMaxD, 4);
   }, ParamLengths());
   if (e == cudaSuccess && tensor_ok) e = configure_tc_weights();
   return e;

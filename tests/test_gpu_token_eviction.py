@@ -136,6 +136,17 @@ def test_weights_other_types_and_head_dims(dtype, heads):
     b.check(b.run(out, sin, 0.5), sin, 0.5)
 
 
+@pytest.mark.parametrize("dtype,heads,prefixes,suffixes", [
+    (torch.float32, (4, 4, 64), [1500, 77], [[700, 3], [129]]), (torch.float32, (4, 2, 192), [3001], [[150, 1]]),
+    (torch.float32, (2, 2, 224), [3001], [[150, 1]]), (torch.bfloat16, (6, 2, 64), [4100], [[90, 17]]),
+    (torch.bfloat16, (4, 4, 160), [2500], [[128]]), (torch.float32, (5, 1, 32), [129, 10000], [[16], [17]])])
+def test_weights_that_fill_the_gpu(dtype, heads, prefixes, suffixes):
+    """Batches with a block of keys for every SM, where a thread takes more keys if they fit."""
+    b = Batch(heads, dtype, prefixes, suffixes, q_pad=1)
+    out, sin = b.fresh(), b.fresh(10)
+    b.check(b.run(out, sin, 0.5), sin, 0.5)
+
+
 @pytest.mark.parametrize("dtype,heads", [(torch.bfloat16, GQA7), (torch.float32, (4, 2, 64))])
 def test_rows_without_a_log_sum_exp_add_nothing(dtype, heads):
     b = Batch(heads, dtype, [300, 20], [[70, 33], [12]])
