@@ -365,8 +365,9 @@ int32_t bicache_build_depth_table(const int32_t* ratio_idx, const int32_t* depth
  * requests are all empty gets decay * in.  Elements of other tokens are left as they are.
  * Sums in fp32 over at most 64 terms, beyond that with the rounding error carried along or in fp64, in a fixed order: the
  * same call gives the same bits.  Uses the context's workspace as scratch: two calls, or replays of
- * graphs that hold such calls, must not overlap (one stream per context at a time).  Errors as for bicache_attend;
- * INVALID also for decay or softmax_scale that is not finite. */
+ * graphs that hold such calls, must not overlap (one stream per context at a time).  A call that finds the device
+ * status raised leaves scores_out as it is where it runs on the tensor cores (bf16, head_dim 128): a running sum is not
+ * lost.  Errors as for bicache_attend; INVALID also for decay or softmax_scale that is not finite. */
 int32_t bicache_prefix_weights(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
                                const int64_t* row_off, const int32_t* seqlen, const void* q, int64_t q_row_stride,
                                const float* lse, const float* scores_in, float* scores_out,

@@ -922,10 +922,14 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a, const __grid_constant_
 static_assert(16 * 128 * sizeof(double) <= sizeof(float) * (128 + kWsRows) * (32 + 4), "the sums are added over the tiles");
 
 // The partial sums of the row ranges, added in order.  One thread per (KV head, key) of a group with splits.
+// status: that of the kernel which wrote them, or nullptr if it has none.  Where it is raised that kernel has left some
+// of them unwritten (all, if it was raised before), and the scores stay as they are.
 template <int kWords>
 __global__ void __launch_bounds__(256)
-weights_sum_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ ParamList<kWords> params) {
+weights_sum_kernel(const __grid_constant__ WeightArgs a, const int* status,
+                   const __grid_constant__ ParamList<kWords> params) {
   const int* const list = params.w;
+  const bool complete = status == nullptr || *status == kDevOk;
   const WeightGroup& g = weight_group(list, blockIdx.y);
   if (g.splits <= 1) return;
   const long long per_split = (long long)a.Hkv * g.m;
@@ -934,7 +938,7 @@ weights_sum_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__
     double s = 0.0;
     for (int k = 0; k < g.splits; ++k) s += (double)a.part[g.part_off + k * per_split + i];
     const long long o = g.score_off + hk * a.head_stride + g.key0 + t;
-    a.out[o] = (float)((a.decay != 0.f ? (double)a.decay * a.in[o] : 0.0) + s);
+    if (complete) a.out[o] = (float)((a.decay != 0.f ? (double)a.decay * a.in[o] : 0.0) + s);
   }
 }
 

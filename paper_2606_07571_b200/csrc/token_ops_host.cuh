@@ -170,7 +170,7 @@ class WeightLaunches {
       if (e == cudaSuccess && split) {
         const long long per_group = (long long)a.Hkv * max_m;
         const unsigned blocks = (unsigned)std::min<long long>((per_group + 255) / 256, 4LL * ctx_->sm_count);
-        weights_sum_kernel<kWords><<<dim3(blocks, groups_), 256, 0, stream_>>>(a, list);
+        weights_sum_kernel<kWords><<<dim3(blocks, groups_), 256, 0, stream_>>>(a, tensor_ ? ctx_->d_status : nullptr, list);
         ctx_->launches++;
         e = cudaGetLastError();
       }

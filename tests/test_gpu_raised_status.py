@@ -1,0 +1,59 @@
+"""While the device status is raised (here by a bad compaction index) the tensor-core calls leave their outputs as
+they are, those whose work is split and put together by a second kernel too: that kernel must not write what an earlier
+call left in the workspace.  Once the status is cleared the same calls give what they gave before it."""
+import pytest
+import torch
+
+import __graft_entry__ as entry
+from paper_2606_07571_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    entry.build()
+    binding.load_library()
+
+
+def randn(shape, seed, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+
+def make(hq, hkv, m, rows):
+    """A context with a prefix of m tokens, and a function that raises its status."""
+    bc = binding.BiCache(1, hq, hkv, 128, (m + 15) // 16 + 1, torch.bfloat16, rows, 4)
+    k = randn((1, m, hkv, 128), 1)
+    pid, _, _ = bc.put_prefix(1, k, -k)
+    short, _, _ = bc.reserve_prefix(2, 4)
+
+    def raise_status():
+        bc.compact_prefix(pid, short, torch.full((1, 1, 4), m, dtype=torch.int32, device="cuda"))
+        assert bc.device_status() == binding.ERR_INVALID
+    return bc, pid, raise_status
+
+
+@pytest.mark.parametrize("m,rows,launches", [(40, 1600, 2), (300, 20, 1)])       # ranges of rows and their sums; one kernel
+def test_accumulated_weights(m, rows, launches):
+    hq, hkv = 14, 2
+    bc, pid, raise_status = make(hq, hkv, m, rows)
+    q = randn((rows, hq, 128), 2)
+    lse = torch.full((rows, hq), 5.0, device="cuda")
+    start = torch.rand((hkv, m), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+
+    def call(scores, q):
+        bc.prefix_weights(0, [pid], [0], [rows], q, lse, scores, [0], scores_in=scores, decay=0.5)
+        return scores
+    before = bc.launch_count()
+    want = call(start.clone(), q)
+    assert bc.launch_count() == before + launches
+    call(start.clone(), q * 2)                                    # the workspace holds another call's sums
+    raise_status()
+    scores = start.clone()
+    call(scores, q)
+    assert bc.device_status() == binding.ERR_INVALID
+    assert torch.equal(scores, start)
+    assert bc.device_status(clear=True) == binding.ERR_INVALID
+    assert torch.equal(call(scores, q), want)
