@@ -442,7 +442,8 @@ int32_t bicache_rope_table(bicache_ctx* ctx, int64_t rows, const int32_t* positi
 
 /* Synchronises `stream` and returns the sticky device status: OK, or TIMEOUT if a kernel gave up
  * on a bounded wait (its outputs are then undefined), INVALID if bicache_compact_prefix met an index
- * outside its source, or CUDA for a runtime error.  `clear` != 0 resets the word. */
+ * outside its source, or CUDA for a runtime error.  While it is not OK the tensor-core calls do no work and leave
+ * their outputs as they are.  `clear` != 0 resets the word. */
 int32_t bicache_device_status(bicache_ctx* ctx, void* stream, int32_t clear);
 
 /* Budget, in SM clock cycles, of every device-side wait of the tensor-core kernel (on a barrier that a

@@ -806,15 +806,16 @@ int launch_attention(bicache_ctx* ctx, const PreparedCall& pc, int32_t layer, co
   ctx->launches++;
   if (e != cudaSuccess) return fail(ctx, BICACHE_ERR_CUDA, std::string("attention launch: ") + cudaGetErrorString(e));
   if (pc.key_ranges) {
-    e = launch_merge_ranges(t, reinterpret_cast<const long long*>(base + c.tok_rows_off), c.num_splits, stream);
+    e = launch_merge_ranges(t, reinterpret_cast<const long long*>(base + c.tok_rows_off), c.num_splits, ctx->d_status, stream);
     ctx->launches++;
     if (e != cudaSuccess) return fail(ctx, BICACHE_ERR_CUDA, std::string("merge launch: ") + cudaGetErrorString(e));
   } else if (c.num_splits > 1) {
     const int grid = c.num_items / c.num_splits * (kTileRows / kMergeRowsPerBlock);
+    const int* status = pc.use_tensor ? ctx->d_status : nullptr;         // the CUDA-core kernel has none
     if (cfg.dtype == BICACHE_F32)
-      merge_partials_kernel<float><<<grid, kMergeRowsPerBlock * 32, 0, stream>>>(sv, t);
+      merge_partials_kernel<float><<<grid, kMergeRowsPerBlock * 32, 0, stream>>>(sv, t, status);
     else
-      merge_partials_kernel<__nv_bfloat16><<<grid, kMergeRowsPerBlock * 32, 0, stream>>>(sv, t);
+      merge_partials_kernel<__nv_bfloat16><<<grid, kMergeRowsPerBlock * 32, 0, stream>>>(sv, t, status);
     ctx->launches++;
     e = cudaGetLastError();
     if (e != cudaSuccess) return fail(ctx, BICACHE_ERR_CUDA, std::string("merge launch: ") + cudaGetErrorString(e));

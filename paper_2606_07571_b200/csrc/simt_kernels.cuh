@@ -407,13 +407,14 @@ simt_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t) {
 // Log-sum-exp merge of the partial results of `num_splits` disjoint key ranges:
 //   lse = log sum_s exp(lse_s),  o = sum_s exp(lse_s - lse) o_s.
 // An empty part carries lse = -inf and weighs 0.  One block per split-0 work item, one warp per
-// packed row.
+// packed row.  status: that of the kernel which wrote the partial results, or nullptr if it has none; where it is
+// raised some of them are unwritten (all, if it was raised before), and the outputs stay as they are.
 // ---------------------------------------------------------------------------------------------
 constexpr int kMergeRowsPerBlock = 8;   // packed rows per block of the merge kernel (one warp each)
 
 template <typename T>
 __global__ void __launch_bounds__(kMergeRowsPerBlock * 32)
-merge_partials_kernel(ScheduleView s, TensorArgs t) {
+merge_partials_kernel(ScheduleView s, TensorArgs t, const int* status) {
   using Tr = ElemTraits<T>;
   constexpr int kEsize = (int)sizeof(T);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -421,6 +422,7 @@ merge_partials_kernel(ScheduleView s, TensorArgs t) {
   // num_items / num_splits items of the schedule are the split-0 items.
   constexpr int kBlocksPerItem = kTileRows / kMergeRowsPerBlock;
   const WorkItem item = s.items[blockIdx.x / kBlocksPerItem];
+  const bool complete = status == nullptr || *status == kDevOk;
   const ReqMeta req = s.reqs[item.req];
   const int G = t.Hq / t.Hkv;
   const int D = t.D;
@@ -469,6 +471,7 @@ merge_partials_kernel(ScheduleView s, TensorArgs t) {
       }
     }
   }
+  if (!complete) return;
 #pragma unroll
   for (int i = 0; i < kSimtMaxD / 32; ++i)
     if (lane + 32 * i < D) Tr::store(orow + (lane + 32 * i) * kEsize, acc[i]);

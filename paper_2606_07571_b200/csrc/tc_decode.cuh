@@ -428,7 +428,8 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
 // over the num_slots partials, written as the bf16 output row.  One warp per (token, head), one
 // float4 of the 128 dims per lane; the rows of eight ranges are loaded before any is used.
 // Launched as a programmatic dependent of the key-range kernel: the grid is placed while that
-// kernel still runs and waits here for its memory to be visible.
+// kernel still runs and waits here for its memory to be visible.  Where the status is raised that
+// kernel has left some partials unwritten (all, if it was raised before): the outputs stay as they are.
 // ---------------------------------------------------------------------------------------------
 constexpr int kMergeWarps = 8;
 
@@ -438,7 +439,7 @@ template <int kSlotWarps>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 merge_ranges_kernel(const float* __restrict__ part_o, const float* __restrict__ part_lse,
                     const long long* __restrict__ tok_rows, int total_tokens, int Hq, int num_slots,
-                    char* __restrict__ out, long long out_stride, float* __restrict__ lse_out) {
+                    char* __restrict__ out, long long out_stride, float* __restrict__ lse_out, const int* status) {
   __shared__ float4 red[kSlotWarps == 1 ? 1 : kMergeWarps][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -456,6 +457,7 @@ merge_ranges_kernel(const float* __restrict__ part_o, const float* __restrict__ 
       pre[u] = *reinterpret_cast<const float4*>(part_o + (pr + min(u, num_slots - 1) * slot_stride) * 128 + lane * 4);
   }
   const long long row = tok_rows[tg];
+  const bool complete = *status == kDevOk;
   const float l0 = lane < num_slots ? part_lse[pr + lane * slot_stride] : -INFINITY;
   const float l1 = lane + 32 < num_slots ? part_lse[pr + (lane + 32) * slot_stride] : -INFINITY;
   const float mx = warp_max(fmaxf(l0, l1));
@@ -510,6 +512,7 @@ merge_ranges_kernel(const float* __restrict__ part_o, const float* __restrict__ 
       acc.w += o.w;
     }
   }
+  if (!complete) return;
   uint2 o2;
   o2.x = tc::pack_bf16(acc.x, acc.y);
   o2.y = tc::pack_bf16(acc.z, acc.w);
@@ -518,7 +521,7 @@ merge_ranges_kernel(const float* __restrict__ part_o, const float* __restrict__ 
 }
 
 inline cudaError_t launch_merge_ranges(const TensorArgs& t, const long long* tok_rows, int num_slots,
-                                       cudaStream_t stream) {
+                                       const int* status, cudaStream_t stream) {
   const long long row_heads = (long long)t.total_tokens * t.Hq;
   if (row_heads <= 0) return cudaSuccess;
   const bool slot_warps = num_slots > 16;                   // many ranges: spread them over the block's warps
@@ -534,9 +537,9 @@ inline cudaError_t launch_merge_ranges(const TensorArgs& t, const long long* tok
   cfg.numAttrs = 1;
   if (slot_warps)
     return cudaLaunchKernelEx(&cfg, merge_ranges_kernel<8>, (const float*)t.part_o, (const float*)t.part_lse, tok_rows,
-                              t.total_tokens, t.Hq, num_slots, t.out, t.out_stride, t.lse);
+                              t.total_tokens, t.Hq, num_slots, t.out, t.out_stride, t.lse, status);
   return cudaLaunchKernelEx(&cfg, merge_ranges_kernel<1>, (const float*)t.part_o, (const float*)t.part_lse, tok_rows,
-                            t.total_tokens, t.Hq, num_slots, t.out, t.out_stride, t.lse);
+                            t.total_tokens, t.Hq, num_slots, t.out, t.out_stride, t.lse, status);
 }
 
 inline cudaError_t configure_tc_decode() {

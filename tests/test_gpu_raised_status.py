@@ -57,3 +57,34 @@ def test_accumulated_weights(m, rows, launches):
     assert torch.equal(scores, start)
     assert bc.device_status(clear=True) == binding.ERR_INVALID
     assert torch.equal(call(scores, q), want)
+
+
+@pytest.mark.parametrize("kind,m,n,kernel,launches", [
+    ("attend", 4000, 9, binding.KERNEL_KEY_RANGES, 2),            # few rows against a long prefix: ranges of the keys
+    ("attend", 2000, 200, binding.KERNEL_TENSOR, 2),              # few row tiles: keys split
+    ("attend_full", 16, 2000, binding.KERNEL_TENSOR, 2),
+    ("attend", 20, 30, binding.KERNEL_TENSOR, 1)])                # one kernel
+def test_attention(kind, m, n, kernel, launches):
+    hq, hkv = 2, 1
+    bc, pid, raise_status = make(hq, hkv, m, n)
+    q, k, v = randn((n, hq, 128), 2), randn((n, hkv, 128), 3), randn((n, hkv, 128), 4)
+
+    def call(out, lse, q):
+        if kind == "attend":
+            bc.attend(0, [pid], [0], [n], q, k, v, out, lse)
+        else:
+            bc.attend_full(0, [0], [n], q, k, v, out, lse)
+    want, want_lse = torch.zeros_like(q), torch.zeros((n, hq), device="cuda")
+    before = bc.launch_count()
+    call(want, want_lse, q)
+    assert bc.launch_count() == before + launches and bc.last_attention_kernel() == kernel
+    call(torch.zeros_like(q), None, -q)                           # the workspace holds another call's partial results
+    raise_status()
+    out, lse = torch.full_like(q, 3.0), torch.full((n, hq), 7.0, device="cuda")
+    call(out, lse, q)
+    assert bc.device_status() == binding.ERR_INVALID
+    assert (out == 3.0).all() and (lse == 7.0).all()
+    assert bc.device_status(clear=True) == binding.ERR_INVALID
+    call(out, lse, q)
+    assert bc.device_status() == binding.OK
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
