@@ -457,7 +457,7 @@ merge_ranges_kernel(const float* __restrict__ part_o, const float* __restrict__ 
       pre[u] = *reinterpret_cast<const float4*>(part_o + (pr + min(u, num_slots - 1) * slot_stride) * 128 + lane * 4);
   }
   const long long row = tok_rows[tg];
-  const bool complete = *status == kDevOk;
+  const bool complete = (kSlotWarps > 1 && warp != 0) || *status == kDevOk;      // asked by the warps that write
   const float l0 = lane < num_slots ? part_lse[pr + lane * slot_stride] : -INFINITY;
   const float l1 = lane + 32 < num_slots ? part_lse[pr + (lane + 32) * slot_stride] : -INFINITY;
   const float mx = warp_max(fmaxf(l0, l1));
