@@ -393,13 +393,15 @@ bool rope_angles(RopeAngles* a, int32_t rot_dim, const double* inv_freq, const i
   a->pairs = rot_dim / 2;
   for (int i = 0; i < a->pairs; ++i) {
     if (!(std::fabs(inv_freq[i]) <= 1048576.0)) return false;
-    // inv_freq / (2 pi) to 2^-64 and better: the product with the leading part of 1 / (2 pi) as a sum of two
-    // doubles, and the product with the rest of the constant
-    const double f = inv_freq[i], high = f * 0.15915494309189535;
+    // |inv_freq| / (2 pi) to 2^-64 and better: the product with the leading part of 1 / (2 pi) as a sum of two
+    // doubles, and the product with the rest of the constant.  The sign is put back at the end: taking a small
+    // negative number modulo a turn as a double would cut it at 2^-54.
+    const double f = std::fabs(inv_freq[i]), high = f * 0.15915494309189535;
     const double low = std::fma(f, 0.15915494309189535, -high) + f * -9.839338337591243e-18;
-    const double part = high - std::floor(high);                  // whole turns per position change nothing
-    a->turn[i] = (part < 1.0 ? (unsigned long long)(part * 18446744073709551616.0) : 0ull) +
-                 (unsigned long long)(long long)std::nearbyint(low * 18446744073709551616.0);
+    const double part = high - std::floor(high);                  // exact; whole turns per position change nothing
+    const unsigned long long turn = (unsigned long long)(part * 18446744073709551616.0) +
+                                    (unsigned long long)(long long)std::nearbyint(low * 18446744073709551616.0);
+    a->turn[i] = std::signbit(inv_freq[i]) ? 0ull - turn : turn;
   }
   a->positions = positions;
   a->position0 = position0;
