@@ -399,7 +399,7 @@ int32_t bicache_compact_prefix(bicache_ctx* ctx, int32_t src_id, int32_t dst_id,
 /* ---- Rotary positions ------------------------------------------------------------------------------
  * Q and K arrive position-encoded at the attention calls; these calls encode them.  Pair i of a row at
  * position p turns by the angle p * inv_freq[i]; the angle is taken modulo whole turns in 64-bit fixed point,
- * so far positions lose nothing.  inv_freq: HOST array of rot_dim / 2 doubles, from
+ * so far positions (up to 2^36, of either sign) lose nothing.  inv_freq: HOST array of rot_dim / 2 doubles, from
  * bicache_rope_frequencies or the model's own. */
 enum {
   BICACHE_ROPE_NONE = 0,    /* base^(-2 i / rot_dim)                                                       */
@@ -422,12 +422,12 @@ int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, 
  * for every pair of the first rot_dim dims of every head, the other dims unchanged; in fp32, one rounding.
  * interleaved 0: pair i is dims (i, i + rot_dim / 2) (what bicache_project_prefix_layer_rope rotates); 1: dims
  * (2 i, 2 i + 1).  inverse != 0 undoes the rotation: angles negated, 1 / attention_scale.
- * Row r has position positions[r] (device int32) or, with positions NULL, position0 + r.
+ * Row r has position positions[r] (device int32) or, with positions NULL, position0 + r, within +-2^36.
  * q, q_out: device [rows][Hq][D] of the context's dtype, k, k_out [rows][Hkv][D]; row strides in elements.
  * A tensor may be rotated in place (the same pointer and stride); other overlap is not allowed.  q or k may be
  * NULL together with its output (that tensor is left out).  INVALID for an odd rot_dim or one outside 2 .. D,
  * frequencies that are not finite or beyond +-2^20, attention_scale (or its inverse, where that is the factor) not
- * finite or 0, one output for both tensors, bad pointers or strides. */
+ * finite or 0, positions beyond 2^36, one output for both tensors, bad pointers or strides. */
 int32_t bicache_rope(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
                      int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale,
                      const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride,

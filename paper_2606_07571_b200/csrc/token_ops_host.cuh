@@ -385,6 +385,14 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
 
 // ---- rotary positions ---------------------------------------------------------------------------
 
+// Positions position0 .. position0 + rows - 1 that the angles hold: a frequency is off by up to 1.5 x 2^-64 turns, so 2^36
+// positions on an angle is off by 3.5e-8 radians, which the rounding to fp32 hides; far beyond that it would not be.
+bool rope_positions_ok(const int32_t* positions, int64_t position0, int64_t rows) {
+  constexpr int64_t kFar = 1LL << 36;
+  if (positions || rows == 0) return true;                        // 32-bit positions, or none
+  return position0 >= -kFar && position0 <= kFar && rows - 1 <= kFar - position0;
+}
+
 // Frequencies to turns per position in 64-bit fixed point.
 bool rope_angles(RopeAngles* a, int32_t rot_dim, const double* inv_freq, const int32_t* positions, int64_t position0,
                  float attention_scale, bool inverse) {
@@ -422,6 +430,7 @@ int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t 
     return fail(ctx, BICACHE_ERR_INVALID, "rot_dim must be even and within the head");
   if (!inv_freq) return fail(ctx, BICACHE_ERR_INVALID, "null frequencies");
   if (!aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "misaligned positions");
+  if (!rope_positions_ok(positions, position0, rows)) return fail(ctx, BICACHE_ERR_INVALID, "positions beyond 2^36");
   RopeAngles a;
   if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, inverse != 0))
     return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
@@ -472,6 +481,7 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
     return fail(ctx, BICACHE_ERR_INVALID, "rot_dim must be even, 2 to 256");
   if (!inv_freq) return fail(ctx, BICACHE_ERR_INVALID, "null frequencies");
   if ((rows > 0 && !table) || !aligned16(table) || !aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "bad pointer");
+  if (!rope_positions_ok(positions, position0, rows)) return fail(ctx, BICACHE_ERR_INVALID, "positions beyond 2^36");
   RopeAngles a;
   if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, false))
     return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");

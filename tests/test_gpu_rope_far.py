@@ -60,3 +60,13 @@ def test_far_int32_positions(bc, sign):
     bound = E + 2.0 ** -24 + 2 * np.pi * 1.5 * 2.0 ** -33
     err = np.abs(table.double().cpu().numpy() - exact(pos, sign * FREQ))
     assert (err <= bound).all(), err.max()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("position0", [2 ** 36 - 6, -2 ** 36, 2 ** 33 + 1, -2 ** 32 - 5])
+def test_consecutive_positions_up_to_the_ends_of_their_range(bc, position0, sign):
+    table = torch.empty((7, len(FREQ), 2), device="cuda")
+    bc.rope_table(sign * FREQ, table, position0=position0)
+    bound = E + 2.0 ** -24 + 2 * np.pi * 1.5 * 2.0 ** -28
+    err = np.abs(table.double().cpu().numpy() - exact(range(position0, position0 + 7), sign * FREQ))
+    assert (err <= bound).all(), err.max()

@@ -1,0 +1,43 @@
+"""CPU tests of the token-eviction and rotary calls at the ends of their arguments' ranges, through a host-only context
+(which answers UNSUPPORTED once the arguments are in order)."""
+import ctypes as C
+
+import pytest
+
+import __graft_entry__ as entry
+from paper_2606_07571_b200 import binding as b
+
+A16, A4 = 0x10000, 0x10004                        # pointers that are never followed
+
+
+@pytest.fixture(scope="module")
+def lib():
+    entry.build()
+    return b.load_library()
+
+
+@pytest.fixture
+def ctx(lib):
+    cfg = b.Config(3, 4, 2, 128, 16, 32, b.BF16, -1)
+    c = C.c_void_p()
+    assert lib.bicache_create(C.byref(cfg), C.byref(c)) == b.OK
+    yield c
+    lib.bicache_destroy(c)
+
+
+def test_positions_beyond_what_the_angles_hold_are_refused(lib, ctx):
+    f = (C.c_double * 64)(*[0.5] * 64)
+
+    def rope(position0, rows=3, pos=None):
+        return lib.bicache_rope(ctx, rows, pos, position0, 128, 0, 0, f, 1.0, A16, 512, A16, 512, None, 0, None, 0, None)
+
+    def table(position0, rows=3, pos=None):
+        return lib.bicache_rope_table(ctx, rows, pos, position0, 128, f, 1.0, A16, None)
+    for call in (rope, table):
+        for position0 in (-2 ** 36, -5, 0, 2 ** 31, 2 ** 36 - 2):
+            assert call(position0) == b.ERR_UNSUPPORTED, position0
+        for position0 in (-2 ** 63, -2 ** 36 - 1, 2 ** 36 - 1, 2 ** 50, 2 ** 63 - 1):
+            assert call(position0) == b.ERR_INVALID, position0
+            assert call(position0, pos=A4) == b.ERR_UNSUPPORTED        # the positions are an array: not read
+            assert call(position0, rows=0) == b.ERR_UNSUPPORTED
+        assert call(0, rows=2 ** 36 + 2) == b.ERR_INVALID
