@@ -404,7 +404,7 @@ int32_t bicache_compact_prefix(bicache_ctx* ctx, int32_t src_id, int32_t dst_id,
 enum {
   BICACHE_ROPE_NONE = 0,    /* base^(-2 i / rot_dim)                                                       */
   BICACHE_ROPE_LINEAR = 1,  /* the same divided by `factor` (positions interpolated)                       */
-  BICACHE_ROPE_NTK = 2,     /* base * factor^(rot_dim / (rot_dim - 2)) as the base                         */
+  BICACHE_ROPE_NTK = 2,     /* base * factor^(rot_dim / (rot_dim - 2)) as the base (rot_dim 2: the plain one) */
   BICACHE_ROPE_YARN = 3,    /* divided by `factor` for slow pairs, kept for fast ones; between the pairs that
                                turn high_turns and low_turns times over original_length the share of
                                interpolation is linear in the pair's index                                */
@@ -414,7 +414,8 @@ enum {
 /* inv_freq[0 .. rot_dim / 2 - 1] (host) for one of the rules above.  factor is not read by NONE;
  * original_length, low_turns and high_turns are read by YARN and BANDS only.  No context, no device work.
  * INVALID for an odd or non-positive rot_dim or one above 256, a base that is not above 1, factor not above
- * 0, original_length < 1 or not 0 < low_turns < high_turns where they are read. */
+ * 0, original_length < 1 or not 0 < low_turns < high_turns where they are read, and for a factor so small that a
+ * frequency is not finite (inv_freq is then left as it was). */
 int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
                                  int32_t original_length, double low_turns, double high_turns, double* inv_freq);
 

@@ -586,6 +586,7 @@ int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, 
     lo = std::max(std::floor(index_of(high_turns)), 0.0);
     hi = std::min(std::ceil(index_of(low_turns)), rot_dim - 1.0);
   }
+  double made[kRopeMaxPairs];
   for (int32_t i = 0; i < rot_dim / 2; ++i) {
     double f = std::pow(b, -2.0 * i / rot_dim);
     if (scaling == BICACHE_ROPE_LINEAR) {
@@ -596,8 +597,10 @@ int32_t bicache_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, 
       slow = std::min(1.0, std::max(0.0, slow));
       f = f / factor * slow + f * (1.0 - slow);
     }
-    inv_freq[i] = f;
+    if (!std::isfinite(f)) return BICACHE_ERR_INVALID;            // a factor so small that dividing by it overflows
+    made[i] = f;
   }
+  std::copy(made, made + rot_dim / 2, inv_freq);
   return BICACHE_OK;
 }
 

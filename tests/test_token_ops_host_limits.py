@@ -2,6 +2,7 @@
 (which answers UNSUPPORTED once the arguments are in order)."""
 import ctypes as C
 
+import numpy as np
 import pytest
 
 import __graft_entry__ as entry
@@ -41,3 +42,19 @@ def test_positions_beyond_what_the_angles_hold_are_refused(lib, ctx):
             assert call(position0, pos=A4) == b.ERR_UNSUPPORTED        # the positions are an array: not read
             assert call(position0, rows=0) == b.ERR_UNSUPPORTED
         assert call(0, rows=2 ** 36 + 2) == b.ERR_INVALID
+
+
+@pytest.mark.parametrize("args", [
+    (4, 1e4, "ntk", 1e-300, 0, 1.0, 2.0),         # the base becomes 0
+    (128, 1e4, "linear", 5e-324, 0, 1.0, 2.0), (128, 1e4, "yarn", 5e-324, 4096, 1.0, 32.0),
+    (128, 1e4, "bands", 5e-324, 8192, 1.0, 4.0)])
+def test_factors_that_leave_no_finite_frequency_are_refused(lib, args):
+    with pytest.raises(b.BiCacheError) as ei:
+        b.rope_frequencies(*args)
+    assert ei.value.status == b.ERR_INVALID
+
+
+def test_far_scaling_that_stays_finite_is_not_refused(lib):
+    for args in ((4, 1e4, "ntk", 1e300, 0, 1.0, 2.0), (128, 1e4, "linear", 1e300, 0, 1.0, 2.0),
+                 (128, 1e4, "linear", 1e-300, 0, 1.0, 2.0)):
+        assert np.isfinite(b.rope_frequencies(*args)).all()
