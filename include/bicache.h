@@ -390,8 +390,9 @@ int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const f
  * every i below keep, which is the destination's length.  idx: device int32; a stride of 0 gives all layers or all heads one
  * list; any order, repeats allowed.  Bit-exact copies; unused slots of the last page become zero.  An index
  * outside 0 .. (source length - 1) gives a zero token and makes bicache_device_status report INVALID until
- * it is cleared; like any device status it stops the tensor-core calls of the context until then.  NOTFOUND for an unknown or evicted id; INVALID for src_id == dst_id, a keep that is not
- * the destination's length, layers that either prefix does not own, negative strides. */
+ * it is cleared; like any device status it stops the tensor-core calls of the context until then.  NOTFOUND for an
+ * unknown or evicted id; INVALID for src_id == dst_id, a keep that is not the destination's length, layers that either
+ * prefix does not own, negative strides.  num_layers may be 0 (nothing is written, idx may be NULL). */
 int32_t bicache_compact_prefix(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_t first_layer,
                                int32_t num_layers, int32_t keep, const int32_t* idx, int64_t idx_layer_stride,
                                int64_t idx_head_stride, void* stream);

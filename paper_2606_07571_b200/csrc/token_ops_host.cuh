@@ -331,7 +331,7 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
     return fail(ctx, BICACHE_ERR_INVALID, "a prefix owns no pages in the first layer");
   if (keep != dst.m) return fail(ctx, BICACHE_ERR_INVALID, "keep is not the destination's length");
   if (idx_layer_stride < 0 || idx_head_stride < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative index stride");
-  if (!idx || !aligned4(idx)) return fail(ctx, BICACHE_ERR_INVALID, "bad index pointer");
+  if ((num_layers > 0 && !idx) || !aligned4(idx)) return fail(ctx, BICACHE_ERR_INVALID, "bad index pointer");
   if (ctx->host_only) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "host-only context has no device path");
   if (num_layers == 0) return BICACHE_OK;
   DeviceGuard guard(cfg.device);

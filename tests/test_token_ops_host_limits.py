@@ -58,3 +58,17 @@ def test_far_scaling_that_stays_finite_is_not_refused(lib):
     for args in ((4, 1e4, "ntk", 1e300, 0, 1.0, 2.0), (128, 1e4, "linear", 1e300, 0, 1.0, 2.0),
                  (128, 1e4, "linear", 1e-300, 0, 1.0, 2.0)):
         assert np.isfinite(b.rope_frequencies(*args)).all()
+
+
+def test_compaction_of_no_layers_needs_no_list(lib, ctx):
+    ids = []
+    for key, m in ((1, 40), (2, 20)):
+        pid = C.c_int32(-1)
+        assert lib.bicache_reserve_prefix_layers(ctx, C.c_uint64(key), m, 0, C.byref(pid), None, None, 0) == b.OK
+        ids.append(pid.value)
+
+    def call(num_layers, idx, keep=20):
+        return lib.bicache_compact_prefix(ctx, *ids, 1, num_layers, keep, idx, 20, 0, None)
+    assert call(0, None) == b.ERR_UNSUPPORTED     # an empty tensor has no address
+    assert call(0, A4) == b.ERR_UNSUPPORTED
+    assert call(1, None) == b.ERR_INVALID and call(0, None, keep=19) == b.ERR_INVALID
