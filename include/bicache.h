@@ -363,8 +363,10 @@ int32_t bicache_build_depth_table(const int32_t* ratio_idx, const int32_t* depth
  * offset; blocks of different prefixes must not overlap.  scores_in: the same layout, read if decay is not
  * 0 (may be scores_out itself, else must not overlap it; NULL allowed only with decay 0).  A prefix whose
  * requests are all empty gets decay * in.  Elements of other tokens are left as they are.
- * Sums in fp32 over at most 64 terms, beyond that with the rounding error carried along or in fp64, in a fixed order: the
- * same call gives the same bits.  Uses the context's workspace as scratch: two calls, or replays of
+ * Sums: a weight goes through at most 64 additions rounded to fp32, whatever the number of rows (a thread's rows of up
+ * to 48 tiles, the lanes and groups of lanes, a range of rows); longer sums carry their rounding error along or are
+ * added in fp64.  More requests of one prefix than a launch takes (900) round the result once for each launch.  The
+ * order is fixed: the same call gives the same bits.  Uses the context's workspace as scratch: two calls, or replays of
  * graphs that hold such calls, must not overlap (one stream per context at a time).  A call that finds the device
  * status raised leaves scores_out as it is where it runs on the tensor cores (bf16, head_dim 128): a running sum is not
  * lost.  Errors as for bicache_attend; INVALID also for decay or softmax_scale that is not finite. */

@@ -13,8 +13,8 @@ namespace bicache {
 // ---------------------------------------------------------------------------------------------
 // Lists in the kernel parameters.  Page lists and batch descriptions of these calls travel as launch
 // parameters (up to 32 KB since CUDA 12.1) and not through the workspace: nothing is uploaded, so a call
-// can be captured into a graph at any time and replayed beside other calls of the context.  A list that
-// does not fit is worked off in several launches.  A launch costs the host about 1 us per 8 KB of
+// can be captured into a graph at any time.  (Replays follow the context's other calls all the same: the
+// partial sums of the weights lie in the workspace.)  A list that does not fit is worked off in several launches.  A launch costs the host about 1 us per 8 KB of
 // parameters (a call of 64 bytes takes 4.5 us, one of 32 KB 8.3), so the kernels exist for lists of four lengths.
 // ---------------------------------------------------------------------------------------------
 constexpr int kParamWords = 7936;               // 31,744 bytes: with the fixed fields below the 32,764 limit
@@ -759,7 +759,8 @@ struct WeightArgs {
 __device__ __forceinline__ const WeightGroup& weight_group(const int* list, int g) {
   return *reinterpret_cast<const WeightGroup*>(&list[g * kGroupWords]);
 }
-// the group of a work item: groups are few and in order
+// the group of a work item.  They are in order; the walk is one record after the other, up to 396 of them with a
+// prefix for each request, and was measured with at most 8.
 __device__ __forceinline__ int weight_group_of(const WeightArgs& a, const int* list, int item) {
   int g = 0;
   while (g + 1 < a.num_groups && item >= weight_group(list, g + 1).item_begin) ++g;
@@ -783,9 +784,10 @@ __device__ __forceinline__ long long weight_row(const int* list, const WeightGro
 // Bound by the fp32 products and the shared-memory reads that feed them: with 8 x 8 a step of four dims is 16 reads (64
 // cycles of an SM's 128 bytes a cycle for a warp) for 256 products (64 cycles); with 4 x 8 it is 48 against 32.  So it is
 // eight keys to a thread, but four where eight do not fit shared memory (head dims past 192) and where a batch has not a
-// block for every SM (fp32, 4 heads of 64 dims: 2048 rows over 4096 keys 157 us with eight, 207 with four; 100 rows over
-// 1000 keys 16.2 and 11.8).  The first is 28 TFLOP/s; products alone, from registers, reach 52 on this part.  bf16 with
-// head_dim 128 takes the tensor-core form.
+// block for every SM (fp32, 4 heads of 64 dims: 2048 rows over 4096 keys 157 us with eight, 170 with four; 100 rows over
+// 1000 keys 16.0 and 9.7).  The first is 27 TFLOP/s; products alone, from registers, reach 52 on this part.  With 128
+// dims four would be ahead of eight there too (323 against 372 us), which the rule does not use yet.  bf16 takes as long
+// as fp32 (149 us with 64 dims, 219 with 96); with head_dim 128 it takes the tensor-core form (21 us).
 constexpr int kWsRows = 128, kWsThreads = 256;
 constexpr int kWsAhead = 4;                             // loads of query rows a thread has on their way
 constexpr int kWsEightMaxD = 192;

@@ -12,8 +12,9 @@
 // exponentials a cycle in the special-function unit and 8192 flops a cycle in the tensor pipe, so a tile of 128 x
 // 256 takes 2048 cycles of the one and 1024 of the other; it takes 2330 (4.2 ms, 86 % of the unit's rate).  A
 // polynomial on the FMA pipe for two of every eight pairs, which is faster by itself (116 cycles against 135 for 16
-// keys of four warps), gained nothing here: the packed instructions take two issue slots each, and with the
-// loaders' warps beside them the schedulers are full (4.2 ms; without the register split that it needs, 5.8).
+// keys of four warps), gained nothing here: 4.2 ms with a register split between the roles, 5.8 without it.  Why is not
+// settled.  It is not a lack of issue slots (47 % of them are used on the long prefix, the special-function unit 84 %);
+// registers are short: 64 sums and 16 loaded values a thread, and the kernel spills 84 bytes at its 96.
 // With few rows the kernel is bound by reading the keys.
 //
 // Roles: warps 0-15 exponentials and sums (warp w: lanes 32 (w & 3) .., keys 64 (w >> 2) ..), warps 16 and 17
