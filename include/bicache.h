@@ -380,7 +380,8 @@ int32_t bicache_prefix_weights(bicache_ctx* ctx, int32_t layer, int32_t R, const
  * rows) that stay: the first protect_first and the last protect_last of them always, then the largest
  * scores, equal scores by lower index; a NaN ranks as -inf, -0 equals +0.  idx_out: device int32 [rows][keep]
  * (idx_row_stride elements between rows), ascending.  Protected ends longer than the row are cut to it.
- * INVALID for keep outside 0 .. n, n above 2^30, fewer kept than protected tokens, bad strides, null pointers.
+ * INVALID for keep outside 0 .. n, n above 2^30, 2^31 rows or more, fewer kept than protected tokens, bad strides, null
+ * pointers.
  * rows, n and keep may be 0 (nothing is written). */
 int32_t bicache_select_tokens(bicache_ctx* ctx, int64_t rows, int32_t n, const float* scores,
                               int64_t score_row_stride, int32_t keep, int32_t protect_first, int32_t protect_last,

