@@ -445,6 +445,85 @@ int32_t bicache_rope_table(bicache_ctx* ctx, int64_t rows, const int32_t* positi
                            int32_t rot_dim, const double* inv_freq, float attention_scale, float* table,
                            void* stream);
 
+/* Several position axes (time, height, width of image patches or video; text tokens have the same position on
+ * every axis): pair i turns by positions[pair_axis[i]][row] * inv_freq[i].  The struct and its arrays are host memory,
+ * read during the call. */
+typedef struct {
+  int32_t rot_dim;             /* rotated dims of a head: even, 2 .. D                                */
+  int32_t interleaved;         /* pairing, as for bicache_rope                                        */
+  int32_t num_axes;            /* 1 .. 4                                                              */
+  float attention_scale;       /* as for bicache_rope                                                 */
+  const double* inv_freq;      /* rot_dim / 2 frequencies, as for bicache_rope                        */
+  const int32_t* pair_axis;    /* rot_dim / 2 entries, 0 .. num_axes - 1; NULL: axis 0 for every pair */
+} bicache_rotation;
+
+/* bicache_rope and bicache_rope_table with several position axes.  positions: device int32 [num_axes][rows] with
+ * position_axis_stride elements (>= rows, if there are several axes) between the axes; required.  The table is [rows]
+ * [rot_dim / 2][2], rot_dim up to 256 there.  inverse: as for bicache_rope.  INVALID also for a pair whose axis is not
+ * below num_axes; other arguments and errors as for bicache_rope and bicache_rope_table. */
+int32_t bicache_rope_axes(bicache_ctx* ctx, int64_t rows, const bicache_rotation* rotation, const int32_t* positions,
+                          int64_t position_axis_stride, int32_t inverse, const void* q, int64_t q_row_stride, void* q_out,
+                          int64_t q_out_row_stride, const void* k, int64_t k_row_stride, void* k_out,
+                          int64_t k_out_row_stride, void* stream);
+int32_t bicache_rope_axes_table(bicache_ctx* ctx, int64_t rows, const bicache_rotation* rotation,
+                                const int32_t* positions, int64_t position_axis_stride, float* table, void* stream);
+
+/* ---- A cache that grows: decoding token by token or block by block ---------------------------------
+ * bicache_put_prefix stores whole prefixes.  These calls work on a prefix that was reserved at its final length
+ * (bicache_reserve_prefix*) and fills up: new tokens are written behind the ones it holds
+ * (bicache_append_tokens), rows attend over the tokens it holds so far (bicache_attend_window).  Like the calls above they
+ * upload nothing and can be captured into a CUDA graph without a run before it; the graph holds page lists, lengths and
+ * offsets.  They run on the context's device whichever device is current. */
+
+/* Keys and values of a ragged batch into one layer of live prefixes: row row_off[i] + a of k and v becomes token
+ * token_off[i] + a of prefix prefix_id[i], for a < seqlen[i] (0: nothing).  Host metadata arrays of length R.  A token that is
+ * written already is replaced; one prefix may occur several times, a token only once (INVALID).  Other tokens stay as they
+ * are; where the prefix's last page is written, the slots behind its end become zero.
+ * k, v: device, rows [Hkv][D] of the context's dtype, kv_row_stride elements between rows; may be rows of one packed
+ * tensor.  Values are stored bit-exact.  Keys are rotated as bicache_rope_axes does, in fp32 with one rounding, or
+ * stored as they are if rotation is NULL.  positions: device int32 [num_axes][rows of k], position_axis_stride
+ * elements between axes (at least the end of the last row, if there are several), or NULL with one axis: a token's
+ * position is its index in the prefix.
+ * q, q_out: device, rows [Hq][D], or both NULL: the queries of the same rows, rotated to the same positions in the same
+ * launch; rows that belong to no request are left as they are.  q_out may be q itself with the same stride, else must
+ * not overlap an input.
+ * NOTFOUND for an unknown or evicted id; INVALID for tokens past the end of the prefix, a layer that it does not own,
+ * queries without a rotation, bad pointers, strides or rotations. */
+int32_t bicache_append_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
+                              const int32_t* token_off, const int64_t* row_off, const int32_t* seqlen, const void* k,
+                              const void* v, int64_t kv_row_stride, const void* q, int64_t q_row_stride, void* q_out,
+                              int64_t q_out_row_stride, const bicache_rotation* rotation, const int32_t* positions,
+                              int64_t position_axis_stride, void* stream);
+
+/* The way back: token token_off[i] + a of prefix prefix_id[i] to row row_off[i] + a of k_out and v_out, bit-exact.
+ * Tokens may be read more than once.  Arguments and errors as for bicache_append_tokens. */
+int32_t bicache_read_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
+                            const int32_t* token_off, const int64_t* row_off, const int32_t* seqlen, void* k_out,
+                            void* v_out, int64_t kv_row_stride, void* stream);
+
+/* Attention of a ragged batch over the cached tokens of its prefixes, under a sliding window whose first tokens stay
+ * visible, one layer.  Row a of request i stands at position p = query_pos[i] + a (counted in tokens of the prefix) and
+ * sees token t of prefix prefix_id[i] iff
+ *     t < cached_len[i],   t <= p + right,   and   (t < sinks or t >= p - left);
+ * left or right -1: no bound on that side.  right 0 is causal attention, -1 lets a block see all of itself.  The rows'
+ * own keys are read from the prefix like all others: append them first.  One call serves prompts, blocks and single
+ * tokens (few rows against many keys: the keys are split over the SMs and joined).
+ *   prefix_id[i]   live prefix, or -1 with cached_len 0; any order, a prefix may occur several times.
+ *   cached_len[i]  tokens that are there, 0 .. the prefix's length; what lies behind them is not read as a number.
+ *   query_pos[i]   position of the first row, >= 0; rows may stand behind the cached tokens.
+ *   row_off[i], seqlen[i], q, out, their strides, lse_out, softmax_scale: as for bicache_attend; lse_out is over the visible
+ * tokens.  A row that sees no token gets out = 0 and lse = -inf.  Rows that belong to no request are left as they are.
+ * A stored value that is not finite spreads to the rows that see its token, and may spread to others of the same request; a
+ * token that no row of the request sees has no effect, whatever it holds.
+ * Uses the context's workspace as scratch: two calls, or replays of graphs that hold such calls, must not overlap.
+ * NOTFOUND for an unknown or evicted id; INVALID for negative sizes, left or right below -1, cached_len beyond the
+ * prefix, a scale that is not finite, out being q, bad pointers or strides. */
+int32_t bicache_attend_window(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
+                              const int32_t* cached_len, const int32_t* query_pos, const int64_t* row_off,
+                              const int32_t* seqlen, const void* q, int64_t q_row_stride, void* out,
+                              int64_t out_row_stride, float* lse_out, int32_t sinks, int32_t left, int32_t right,
+                              float softmax_scale, void* stream);
+
 /* Synchronises `stream` and returns the sticky device status: OK, or TIMEOUT if a kernel gave up
  * on a bounded wait (its outputs are then undefined), INVALID if bicache_compact_prefix met an index
  * outside its source, or CUDA for a runtime error.  While it is not OK the tensor-core calls do no work and leave

@@ -32,6 +32,8 @@ EXPORTED = [
     "bicache_build_depth_table",
     "bicache_prefix_weights", "bicache_select_tokens", "bicache_compact_prefix",
     "bicache_rope_frequencies", "bicache_rope", "bicache_rope_table",
+    "bicache_rope_axes", "bicache_rope_axes_table",
+    "bicache_append_tokens", "bicache_read_tokens", "bicache_attend_window",
     "bicache_hash_tokens", "bicache_device_status", "bicache_set_wait_budget", "bicache_launch_count", "bicache_schedule_uploads", "bicache_last_attention_kernel", "bicache_last_error",
 ]
 
@@ -53,6 +55,27 @@ class Config(C.Structure):
         ("k_pool", C.c_void_p), ("v_pool", C.c_void_p),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
+
+
+class RotationStruct(C.Structure):
+    _fields_ = [
+        ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("num_axes", C.c_int32),
+        ("attention_scale", C.c_float), ("inv_freq", C.c_void_p), ("pair_axis", C.c_void_p),
+    ]
+
+
+class Rotation:
+    """bicache_rotation: how the heads of a model turn.  inv_freq: rot_dim / 2 frequencies (rope_frequencies);
+    pair_axis: the position axis of every pair (None: axis 0), num_axes of them.  Made once and passed to the calls."""
+
+    def __init__(self, inv_freq, interleaved=False, attention_scale=1.0, pair_axis=None, num_axes=1):
+        self._freq = np.array(inv_freq, dtype=np.float64)
+        self._axis = None if pair_axis is None else np.array(pair_axis, dtype=np.int32)
+        assert self._freq.ndim == 1 and (self._axis is None or self._axis.shape == self._freq.shape)
+        self.pairs, self.num_axes = len(self._freq), num_axes
+        self.struct = RotationStruct(2 * self.pairs, int(interleaved), num_axes, attention_scale, self._freq.ctypes.data,
+                                     None if self._axis is None else self._axis.ctypes.data)
+        self.pointer = C.addressof(self.struct)
 
 
 _lib = None
@@ -145,6 +168,19 @@ def load_library():
                                  vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp]
     lib.bicache_rope_table.restype = C.c_int32
     lib.bicache_rope_table.argtypes = [vp, C.c_int64, vp, C.c_int64, C.c_int32, vp, C.c_float, vp, vp]
+    lib.bicache_rope_axes.restype = C.c_int32
+    lib.bicache_rope_axes.argtypes = [vp, C.c_int64, vp, vp, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp,
+                                      C.c_int64, vp, C.c_int64, vp]
+    lib.bicache_rope_axes_table.restype = C.c_int32
+    lib.bicache_rope_axes_table.argtypes = [vp, C.c_int64, vp, vp, C.c_int64, vp, vp]
+    lib.bicache_append_tokens.restype = C.c_int32
+    lib.bicache_append_tokens.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int64, vp, C.c_int64, vp,
+                                          C.c_int64, vp, vp, C.c_int64, vp]
+    lib.bicache_read_tokens.restype = C.c_int32
+    lib.bicache_read_tokens.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int64, vp]
+    lib.bicache_attend_window.restype = C.c_int32
+    lib.bicache_attend_window.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int64, vp, C.c_int64, vp,
+                                          C.c_int32, C.c_int32, C.c_int32, C.c_float, vp]
     lib.bicache_device_status.restype = C.c_int32
     lib.bicache_device_status.argtypes = [vp, vp, C.c_int32]
     lib.bicache_hash_tokens.restype = C.c_uint64
@@ -535,6 +571,100 @@ class BiCache:
         st = self.lib.bicache_rope_table(self.ctx, rows, self._positions(positions, rows), position0, 2 * pairs, pf,
                                          attention_scale, table.data_ptr(), self._on_stream())
         self._check(st, "bicache_rope_table")
+
+    def _axis_positions(self, rotation, positions, rows):
+        """Pointer and axis stride of positions [num_axes, rows] (or [rows] with one axis)."""
+        if positions is None:
+            return None, 0
+        self._own(positions, torch.int32)
+        if positions.dim() == 1:
+            positions = positions[None]
+        assert positions.shape == (rotation.num_axes, rows) and (rows <= 1 or positions.stride(1) == 1)
+        return positions.data_ptr(), positions.stride(0)
+
+    def rope_axes(self, rotation, positions, q, q_out, k=None, k_out=None, inverse=False):
+        """rope with a Rotation of several position axes: positions int32 [num_axes, rows]."""
+        rows = (k if q is None else q).shape[0]
+        assert q is None or k is None or k.shape[0] == rows
+        at, stride = self._axis_positions(rotation, positions, rows)
+        st = self.lib.bicache_rope_axes(self.ctx, rows, rotation.pointer, at, stride, inverse,
+                                        *self._rope_pair(q, q_out, self.Hq), *self._rope_pair(k, k_out, self.Hkv),
+                                        self._on_stream())
+        self._check(st, "bicache_rope_axes")
+
+    def rope_axes_table(self, rotation, positions, table):
+        """rope_table with a Rotation of several position axes: table float32 [rows, pairs, 2]."""
+        self._own(table, torch.float32)
+        rows = table.shape[0]
+        assert table.shape == (rows, rotation.pairs, 2) and table.is_contiguous()
+        at, stride = self._axis_positions(rotation, positions, rows)
+        st = self.lib.bicache_rope_axes_table(self.ctx, rows, rotation.pointer, at, stride, table.data_ptr(),
+                                              self._on_stream())
+        self._check(st, "bicache_rope_axes_table")
+
+    # -- a cache that grows -------------------------------------------------------------------
+    def _token_args(self, prefix_id, token_off, row_off, seqlen, k, v):
+        """Host arrays of a batch of tokens, their number, and the rows that they name."""
+        pid, ppid, count = _host(prefix_id, "i")
+        tok, ptok, n_tok = _host(token_off, "i")
+        off, poff, n_off = _host(row_off, "q")
+        n, pn, n_len = _host(seqlen, "i")
+        assert count == n_tok == n_off == n_len
+        self._own(k, self.dtype)
+        self._own(v, self.dtype)
+        rows, heads, d = k.shape
+        assert v.shape == k.shape and v.stride() == k.stride() and heads == self.Hkv and d == self.D
+        assert k.stride(2) == 1 and k.stride(1) == d
+        assert not count or max(map(int.__add__, off, n) if isinstance(off, array.array) and isinstance(n, array.array)
+                                else np.add(off, n)) <= rows, "a request's rows reach past the tensors"
+        return (pid, tok, off, n), count, ppid, ptok, poff, pn, rows
+
+    def append_tokens(self, layer, prefix_id, token_off, row_off, seqlen, k, v, q=None, q_out=None, rotation=None,
+                      positions=None):
+        """Rows row_off[i] .. + seqlen[i] of k, v [rows, Hkv, D] become tokens token_off[i] .. of prefix prefix_id[i],
+        the keys rotated (rotation None: stored as they are).  positions: int32 [num_axes, rows] or [rows]; None
+        with one axis: the tokens' indices.  q [rows, Hq, D] is rotated into q_out (which may be q) alike."""
+        keep, count, ppid, ptok, poff, pn, rows = self._token_args(prefix_id, token_off, row_off, seqlen, k, v)
+        assert q is None or q.shape[0] == rows
+        at, stride = (None, 0) if rotation is None else self._axis_positions(rotation, positions, rows)
+        st = self.lib.bicache_append_tokens(self.ctx, layer, count, ppid, ptok, poff, pn, k.data_ptr(), v.data_ptr(),
+                                            k.stride(0), *self._rope_pair(q, q_out, self.Hq),
+                                            None if rotation is None else rotation.pointer, at, stride, self._on_stream())
+        self._check(st, "bicache_append_tokens")
+
+    def read_tokens(self, layer, prefix_id, token_off, row_off, seqlen, k_out, v_out):
+        """Tokens token_off[i] .. of prefix prefix_id[i] to rows row_off[i] .. of k_out, v_out [rows, Hkv, D]."""
+        keep, count, ppid, ptok, poff, pn, _ = self._token_args(prefix_id, token_off, row_off, seqlen, k_out, v_out)
+        st = self.lib.bicache_read_tokens(self.ctx, layer, count, ppid, ptok, poff, pn, k_out.data_ptr(),
+                                          v_out.data_ptr(), k_out.stride(0), self._on_stream())
+        self._check(st, "bicache_read_tokens")
+
+    def attend_window(self, layer, prefix_id, cached_len, query_pos, row_off, seqlen, q, out, lse=None, sinks=0, left=-1,
+                      right=-1, scale=None):
+        """Rows row_off[i] .. + seqlen[i] of q [rows, Hq, D], at positions query_pos[i] .., attend over the tokens
+        t < cached_len[i] of prefix prefix_id[i] with t <= p + right and (t < sinks or t >= p - left); -1: no bound."""
+        pid, ppid, count = _host(prefix_id, "i")
+        cl, pcl, n_cl = _host(cached_len, "i")
+        qp, pqp, n_qp = _host(query_pos, "i")
+        off, poff, n_off = _host(row_off, "q")
+        n, pn, n_len = _host(seqlen, "i")
+        assert count == n_cl == n_qp == n_off == n_len
+        self._own(q, self.dtype)
+        self._own(out, self.dtype)
+        rows, hq, d = q.shape
+        assert out.shape == q.shape and hq == self.Hq and d == self.D
+        assert q.stride(2) == out.stride(2) == 1 and q.stride(1) == out.stride(1) == d
+        assert not count or max(map(int.__add__, off, n) if isinstance(off, array.array) and isinstance(n, array.array)
+                                else np.add(off, n)) <= rows, "a request's rows reach past q"
+        lp = None
+        if lse is not None:
+            self._own(lse, torch.float32)
+            assert lse.is_contiguous() and lse.shape == (rows, hq)
+            lp = lse.data_ptr()
+        st = self.lib.bicache_attend_window(self.ctx, layer, count, ppid, pcl, pqp, poff, pn, q.data_ptr(), q.stride(0),
+                                            out.data_ptr(), out.stride(0), lp, sinks, left, right,
+                                            d ** -0.5 if scale is None else scale, self._on_stream())
+        self._check(st, "bicache_attend_window")
 
     def device_status(self, clear=False):
         return self.lib.bicache_device_status(self.ctx, self._stream(), 1 if clear else 0)

@@ -27,6 +27,8 @@
 #include "evict.cuh"
 #include "rope.cuh"
 #include "tc_weights.cuh"
+#include "token_cache.cuh"
+#include "window.cuh"
 
 using namespace bicache;
 
@@ -839,6 +841,7 @@ int run_attention(bicache_ctx* ctx, int kind, int32_t layer, int32_t R, const in
 }  // namespace
 
 #include "token_ops_host.cuh"
+#include "window_host.cuh"
 
 extern "C" {
 
@@ -946,7 +949,7 @@ int32_t bicache_create(const bicache_config* cfg, bicache_ctx** out) {
     delete ctx;
     return BICACHE_ERR_CUDA;
   }
-  if (configure_token_ops(tensor_ok) != cudaSuccess) {
+  if (configure_token_ops(tensor_ok) != cudaSuccess || configure_window(*cfg) != cudaSuccess) {
     destroy_host_resources(ctx);
     delete ctx;
     return BICACHE_ERR_CUDA;
@@ -1193,7 +1196,7 @@ int32_t bicache_read_prefix_layer(bicache_ctx* ctx, int32_t prefix_id, int32_t l
   cudaError_t ce = cudaSuccess;
   if (e.m > 0 && need <= kParamWords && rows <= 0x7fffffffLL) {      // the page list fits the launch parameters
     const int blocks = copy_blocks(rows, chunks_per_row, ctx->sm_count);
-    int list[kParamWords];
+    alignas(8) int list[kParamWords];
     std::memcpy(list, pages.data(), sizeof(int) * need);
     with_param_list(list, need, [&](const auto& params) {
       read_layer_kernel<<<blocks, kCompactThreads, 0, stream>>>(

@@ -20,7 +20,7 @@ namespace bicache {
 constexpr int kParamWords = 7936;               // 31,744 bytes: with the fixed fields below the 32,764 limit
 using ParamLengths = std::integer_sequence<int, 224, 1216, 2432, kParamWords>;
 template <int kWords>
-struct ParamList {
+struct alignas(8) ParamList {                   // holds records with 64-bit fields, wherever it stands among the parameters
   int w[kWords];
 };
 // f(list of the shortest length that holds the first `used` words of w)

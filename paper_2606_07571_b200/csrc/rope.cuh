@@ -27,6 +27,21 @@ struct RopeAngles {
   int negate;                              // rotate backwards
 };
 
+// Several position axes (time, height, width of image patches and video): pair i turns with the position of its own
+// axis, positions[axis(i)][row].  Two bits a pair: up to four axes.
+constexpr int kRopeMaxAxes = 4;
+struct RopeAxes : RopeAngles {
+  unsigned axis[kRopeMaxPairs / 16];
+  long long axis_stride;                   // positions between two axes
+};
+__device__ __forceinline__ long long rope_position(const RopeAngles& a, long long row, int) {
+  return a.positions ? (long long)a.positions[row] : a.position0 + row;
+}
+__device__ __forceinline__ long long rope_position(const RopeAxes& a, long long row, int pair) {
+  const int axis = (a.axis[pair >> 4] >> (2 * (pair & 15))) & 3;
+  return a.positions[axis * a.axis_stride + row];
+}
+
 __device__ __forceinline__ float2 rope_cos_sin(const RopeAngles& a, long long pos, unsigned long long turn) {
   // an eighth of a turn is added, so the two top bits count quarter turns and the rest, taken back to
   // [-1/8, 1/8) turn, is the argument
@@ -52,8 +67,9 @@ __device__ __forceinline__ float2 rope_cos_sin(const RopeAngles& a, long long po
 // ---------------------------------------------------------------------------------------------
 constexpr int kTableRows = 4;              // rows a thread has in hand
 
+template <typename A>
 __global__ void __launch_bounds__(kRopeThreads)
-rope_table_kernel(const __grid_constant__ RopeAngles a, long long rows, float2* __restrict__ table) {
+rope_table_kernel(const __grid_constant__ A a, long long rows, float2* __restrict__ table) {
   const int per_block = kRopeThreads / a.pairs;                  // rows a block handles at a time
   const int r = (int)threadIdx.x / a.pairs, pair = (int)threadIdx.x - r * a.pairs;
   if (r >= per_block) return;
@@ -64,8 +80,7 @@ rope_table_kernel(const __grid_constant__ RopeAngles a, long long rows, float2* 
 #pragma unroll
     for (int i = 0; i < kTableRows; ++i) {
       const long long at = row + i * step;
-      pos[i] = a.position0 + at;
-      if (a.positions && at < rows) pos[i] = a.positions[at];
+      pos[i] = at < rows ? rope_position(a, at, pair) : 0;
     }
 #pragma unroll
     for (int i = 0; i < kTableRows; ++i) {
@@ -113,9 +128,9 @@ template <> __device__ __forceinline__ uint4 rope_pack<__nv_bfloat16>(const floa
 // These lie in shared memory chunk by chunk, two pairs to 16 bytes, the units of a head side by side:
 // the lanes of a quarter warp read different banks.
 // ---------------------------------------------------------------------------------------------
-template <typename T, bool kInterleaved, int kRows>
+template <typename T, bool kInterleaved, int kRows, typename A>
 __global__ void __launch_bounds__(kRopeThreads)
-rope_chunks_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ RopeRows r) {
+rope_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ RopeRows r) {
   using Tr = ElemTraits<T>;
   constexpr int kPer = Tr::kPerChunk;
   constexpr int kPairs = kInterleaved ? kPer / 2 : kPer;           // pairs of a unit
@@ -155,7 +170,7 @@ rope_chunks_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__
   if (u < units) load(u);
   for (int i = threadIdx.x; i < rows * a.pairs; i += blockDim.x) {
     const int row = i / a.pairs, pair = i - row * a.pairs;
-    const long long pos = a.positions ? (long long)a.positions[row0 + row] : a.position0 + row0 + row;
+    const long long pos = rope_position(a, row0 + row, pair);
     const int unit = pair / kPairs, e = pair - unit * kPairs;
     reinterpret_cast<float2*>(&cs[row][(e >> 1) * turned + unit])[e & 1] = rope_cos_sin(a, pos, a.turn[pair]);
   }
@@ -198,9 +213,9 @@ rope_chunks_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__
 // Rows, any rotated width: one thread per pair (and per dim beyond the rotated ones), element by element.
 // A block takes one row at a time.
 // ---------------------------------------------------------------------------------------------
-template <typename T>
+template <typename T, typename A>
 __global__ void __launch_bounds__(kRopeThreads)
-rope_rows_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ RopeRows r, int interleaved) {
+rope_rows_kernel(const __grid_constant__ A a, const __grid_constant__ RopeRows r, int interleaved) {
   using Tr = ElemTraits<T>;
   constexpr int kEsize = (int)sizeof(T);
   __shared__ float2 cs[kRopeMaxPairs];
@@ -208,9 +223,9 @@ rope_rows_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ R
   const int per_head = a.pairs + rest;
   const int units = per_head * (r.t[0].heads + r.t[1].heads);
   for (long long row = blockIdx.x; row < r.rows; row += gridDim.x) {
-    const long long pos = a.positions ? (long long)a.positions[row] : a.position0 + row;
     __syncthreads();
-    if ((int)threadIdx.x < a.pairs) cs[threadIdx.x] = rope_cos_sin(a, pos, a.turn[threadIdx.x]);
+    if ((int)threadIdx.x < a.pairs)
+      cs[threadIdx.x] = rope_cos_sin(a, rope_position(a, row, threadIdx.x), a.turn[threadIdx.x]);
     __syncthreads();
     for (int u = threadIdx.x; u < units; u += kRopeThreads) {
       int h = u / per_head;
@@ -236,8 +251,8 @@ rope_rows_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ R
 
 // Four rows to a block once that still gives every SM two blocks (it quarters the index arithmetic and the loads
 // in flight are what hides the latency); one row to a block below that.
-template <typename T>
-cudaError_t launch_rope(const RopeAngles& a, const RopeRows& r, bool interleaved, int sm_count, cudaStream_t stream) {
+template <typename T, typename A>
+cudaError_t launch_rope(const A& a, const RopeRows& r, bool interleaved, int sm_count, cudaStream_t stream) {
   constexpr int kPer = ElemTraits<T>::kPerChunk;
   if ((interleaved ? 2 * a.pairs : a.pairs) % kPer == 0) {
     const int turned = a.pairs / (interleaved ? kPer / 2 : kPer);
@@ -248,15 +263,15 @@ cudaError_t launch_rope(const RopeAngles& a, const RopeRows& r, bool interleaved
     const long long blocks = four ? (r.rows + 3) / 4 : r.rows;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     if (interleaved) {
-      if (four) rope_chunks_kernel<T, true, 4><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
-      else rope_chunks_kernel<T, true, 1><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      if (four) rope_chunks_kernel<T, true, 4, A><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      else rope_chunks_kernel<T, true, 1, A><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
     } else {
-      if (four) rope_chunks_kernel<T, false, 4><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
-      else rope_chunks_kernel<T, false, 1><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      if (four) rope_chunks_kernel<T, false, 4, A><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
+      else rope_chunks_kernel<T, false, 1, A><<<(unsigned)blocks, threads, 0, stream>>>(a, r);
     }
   } else {
     const long long blocks = r.rows < 16LL * sm_count ? r.rows : 16LL * sm_count;
-    rope_rows_kernel<T><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
+    rope_rows_kernel<T, A><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
   }
   return cudaGetLastError();
 }

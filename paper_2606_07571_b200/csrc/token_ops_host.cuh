@@ -352,7 +352,7 @@ int compact_prefix_impl(bicache_ctx* ctx, int32_t src_id, int32_t dst_id, int32_
   const bool together = src.uniform && dst.uniform && ctx->uniform_caps &&
                         (long long)pages_of(dst, first_layer).size() * num_layers <= max_pages;
   const int step = together ? num_layers : 1;
-  int list[kParamWords];
+  alignas(8) int list[kParamWords];
   for (int l = first_layer; l < first_layer + num_layers; l += step) {
     const std::vector<int32_t>&sp = pages_of(src, l), &dp = pages_of(dst, l);
     const int ns = (int)sp.size(), nd = (int)dp.size();
@@ -419,25 +419,15 @@ bool rope_angles(RopeAngles* a, int32_t rot_dim, const double* inv_freq, const i
   return true;
 }
 
-int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
-              int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale, const void* q,
-              int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, const void* k, int64_t k_row_stride,
-              void* k_out, int64_t k_out_row_stride, void* stream_) {
-  if (!ctx) return BICACHE_ERR_INVALID;
+// The tensors of a rotation; what is wrong with them is recorded in the context.
+int rope_tensors(const bicache_ctx* ctx, int64_t rows, const void* q, int64_t q_row_stride, void* q_out,
+                 int64_t q_out_row_stride, const void* k, int64_t k_row_stride, void* k_out, int64_t k_out_row_stride,
+                 RopeRows* r) {
   const bicache_config& cfg = ctx->cfg;
-  if (rows < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative row count");
-  if (rot_dim < 2 || rot_dim > cfg.head_dim || rot_dim % 2)
-    return fail(ctx, BICACHE_ERR_INVALID, "rot_dim must be even and within the head");
-  if (!inv_freq) return fail(ctx, BICACHE_ERR_INVALID, "null frequencies");
-  if (!aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "misaligned positions");
-  if (!rope_positions_ok(positions, position0, rows)) return fail(ctx, BICACHE_ERR_INVALID, "positions beyond 2^36");
-  RopeAngles a;
-  if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, inverse != 0))
-    return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
-  RopeRows r = RopeRows();
-  r.rows = rows;
-  r.head_bytes = cfg.head_dim * ctx->esize;
-  r.in_place = 1;
+  *r = RopeRows();
+  r->rows = rows;
+  r->head_bytes = cfg.head_dim * ctx->esize;
+  r->in_place = 1;
   const void* ins[2] = {q, k};
   void* outs[2] = {q_out, k_out};
   const int64_t in_strides[2] = {q_row_stride, k_row_stride}, out_strides[2] = {q_out_row_stride, k_out_row_stride};
@@ -455,22 +445,59 @@ int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t 
       return fail(ctx, BICACHE_ERR_INVALID, "bad row stride");
     if (ins[i] == outs[i] && in_strides[i] != out_strides[i])
       return fail(ctx, BICACHE_ERR_INVALID, "in place with two row strides");
-    r.t[i].in = static_cast<const char*>(ins[i]);
-    r.t[i].out = static_cast<char*>(outs[i]);
-    r.t[i].in_stride = in_strides[i] * ctx->esize;
-    r.t[i].out_stride = out_strides[i] * ctx->esize;
-    r.t[i].heads = heads[i];
-    if (ins[i] != outs[i]) r.in_place = 0;
+    r->t[i].in = static_cast<const char*>(ins[i]);
+    r->t[i].out = static_cast<char*>(outs[i]);
+    r->t[i].in_stride = in_strides[i] * ctx->esize;
+    r->t[i].out_stride = out_strides[i] * ctx->esize;
+    r->t[i].heads = heads[i];
+    if (ins[i] != outs[i]) r->in_place = 0;
   }
+  return BICACHE_OK;
+}
+
+template <typename A>
+int run_rope(bicache_ctx* ctx, const A& a, const RopeRows& r, bool interleaved, void* stream_) {
   if (ctx->host_only) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "host-only context has no device path");
-  if (rows == 0) return BICACHE_OK;
-  DeviceGuard guard(cfg.device);
+  if (r.rows == 0) return BICACHE_OK;
+  DeviceGuard guard(ctx->cfg.device);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const cudaError_t e = cfg.dtype == BICACHE_F32
-                            ? launch_rope<float>(a, r, interleaved != 0, ctx->sm_count, stream)
-                            : launch_rope<__nv_bfloat16>(a, r, interleaved != 0, ctx->sm_count, stream);
+  const cudaError_t e = ctx->cfg.dtype == BICACHE_F32
+                            ? launch_rope<float>(a, r, interleaved, ctx->sm_count, stream)
+                            : launch_rope<__nv_bfloat16>(a, r, interleaved, ctx->sm_count, stream);
   ctx->launches++;
   return cuda_status(ctx, e, "rope");
+}
+
+int rope_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
+              int32_t interleaved, int32_t inverse, const double* inv_freq, float attention_scale, const void* q,
+              int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, const void* k, int64_t k_row_stride,
+              void* k_out, int64_t k_out_row_stride, void* stream) {
+  if (!ctx) return BICACHE_ERR_INVALID;
+  if (rows < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative row count");
+  if (rot_dim < 2 || rot_dim > ctx->cfg.head_dim || rot_dim % 2)
+    return fail(ctx, BICACHE_ERR_INVALID, "rot_dim must be even and within the head");
+  if (!inv_freq) return fail(ctx, BICACHE_ERR_INVALID, "null frequencies");
+  if (!aligned4(positions)) return fail(ctx, BICACHE_ERR_INVALID, "misaligned positions");
+  if (!rope_positions_ok(positions, position0, rows)) return fail(ctx, BICACHE_ERR_INVALID, "positions beyond 2^36");
+  RopeAngles a;
+  if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, inverse != 0))
+    return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
+  RopeRows r;
+  const int st = rope_tensors(ctx, rows, q, q_row_stride, q_out, q_out_row_stride, k, k_row_stride, k_out,
+                              k_out_row_stride, &r);
+  return st != BICACHE_OK ? st : run_rope(ctx, a, r, interleaved != 0, stream);
+}
+
+template <typename A>
+int run_rope_table(bicache_ctx* ctx, const A& a, int64_t rows, float* table, void* stream) {
+  if (ctx->host_only) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "host-only context has no device path");
+  if (rows == 0) return BICACHE_OK;
+  DeviceGuard guard(ctx->cfg.device);
+  const int per_block = kRopeThreads / a.pairs;
+  const int blocks = (int)std::min<long long>((rows + per_block - 1) / per_block, 2LL * ctx->sm_count);
+  rope_table_kernel<A><<<blocks, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, rows, reinterpret_cast<float2*>(table));
+  ctx->launches++;
+  return cuda_status(ctx, cudaGetLastError(), "rope_table");
 }
 
 int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, int64_t position0, int32_t rot_dim,
@@ -485,14 +512,7 @@ int rope_table_impl(bicache_ctx* ctx, int64_t rows, const int32_t* positions, in
   RopeAngles a;
   if (!rope_angles(&a, rot_dim, inv_freq, positions, position0, attention_scale, false))
     return fail(ctx, BICACHE_ERR_INVALID, "a frequency that is not finite or above 2^20, or a bad scale");
-  if (ctx->host_only) return fail(ctx, BICACHE_ERR_UNSUPPORTED, "host-only context has no device path");
-  if (rows == 0) return BICACHE_OK;
-  DeviceGuard guard(ctx->cfg.device);
-  const int per_block = kRopeThreads / a.pairs;
-  const int blocks = (int)std::min<long long>((rows + per_block - 1) / per_block, 2LL * ctx->sm_count);
-  rope_table_kernel<<<blocks, kRopeThreads, 0, static_cast<cudaStream_t>(stream_)>>>(a, rows, reinterpret_cast<float2*>(table));
-  ctx->launches++;
-  return cuda_status(ctx, cudaGetLastError(), "rope_table");
+  return run_rope_table(ctx, a, rows, table, stream_);
 }
 
 cudaError_t configure_token_ops(bool tensor_ok) {

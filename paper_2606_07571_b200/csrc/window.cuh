@@ -1,0 +1,515 @@
+// bicache_attend_window: rows of a ragged batch attend over the cached tokens of their prefixes, under a sliding
+// window and a number of first tokens that stay visible.  For a row at position p of a request whose prefix holds `len`
+// tokens, token t is visible iff
+//     t < len,  t <= p + right,  and  (t < sinks or t >= p - left);
+//   o = sum over the visible t of softmax_t(scale q.k_t) v_t,   lse = log sum exp(scale q.k_t);
+// a row that sees nothing gets o = 0, lse = -inf.
+//
+// This file: the batch as the kernels see it, the CUDA-core kernel (fp32, head dims other than 128), and the
+// kernel that joins ranges of keys.
+//
+// The batch travels as launch parameters: requests, and of each the pages that some row of it sees.  A request's row
+// space is its rows x the G = Hq / Hkv query heads of a KV head (packed row = row * G + head), cut into row tiles.  A row tile
+// sees an interval of tokens (rows follow one another, so their windows join up) and the first tokens; its
+// pages - those of the first tokens, then the interval's - are put side by side, and key tiles are cut from that
+// sequence, so that the few first tokens share a tile with the window.  With few rows and many keys the key tiles are
+// dealt out to several work items (splits), whose partial results the joining kernel puts together in a fixed order.
+#pragma once
+#include "evict.cuh"
+
+namespace bicache {
+
+struct WindowReq {
+  long long row;                // first row of q, out and lse
+  int n;                        // rows
+  int pos;                      // position of the first
+  int len;                      // cached tokens
+  int sink_pages;               // pages of the list that come before the gap (0: no gap)
+  int gap;                      // pages left out behind them
+  int page_word;                // page list in the parameter words
+  int item_begin;               // first work item
+  int splits, tiles_per_split;  // ranges of key tiles
+  int part_off;                 // first partial result in row-heads (splits > 1)
+  int row_tiles;
+  int row_heads_before;         // row-heads of split requests before this one (joining kernel)
+};
+constexpr int kWindowReqWords = sizeof(WindowReq) / 4;
+static_assert(sizeof(WindowReq) % 8 == 0, "8-byte aligned records");
+
+struct WindowArgs {
+  const char* q;
+  char* out;
+  float* lse;                   // or nullptr
+  long long q_stride, out_stride;          // elements between rows
+  const char *pool_k, *pool_v;  // of the layer
+  const int* staged_pages;      // page list of the only request, if it did not fit the parameters
+  long long page_stride;        // bytes of a page of all heads
+  int page_bytes, swizzled;
+  int Hq, Hkv, D;
+  int sinks, left, right;       // left, right: -1 for no bound
+  float scale;
+  float *part_o, *part_lse;     // [row-head] x D, [row-head]
+  int num_reqs, num_items;
+};
+
+// The request of a work item: the last that starts at or before it.
+__device__ __forceinline__ const WindowReq& window_req(const int* list, int num_reqs, int item) {
+  const WindowReq* const reqs = reinterpret_cast<const WindowReq*>(list);
+  int lo = 0;
+  for (int hi = num_reqs; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (reqs[mid].item_begin <= item) lo = mid;
+    else hi = mid;
+  }
+  return reqs[lo];
+}
+
+// What a row at position p sees: tokens [first, end), and those of the first `sinks` that are below `end`.
+struct WindowBounds {
+  int first, end;
+};
+__host__ __device__ inline WindowBounds window_bounds(int sinks, int left, int right, int len, int p) {
+  WindowBounds b;
+  b.end = right < 0 || right >= len - p ? len : p + right + 1;       // p + right may not fit 32 bits
+  b.first = left < 0 || left >= p ? 0 : p - left;
+  if (b.first <= sinks) b.first = 0;
+  if (b.first > b.end) b.first = b.end;
+  return b;
+}
+
+// The pages that rows at positions pa .. pb see, side by side: `sink_pages` first pages, then from lo_page on; and what
+// some of the rows sees, in columns of that sequence: [begin, end), and [0, sink).  (Windows start and end later the later
+// the row, and rows that are past the cache by more than `left` see no window: if the first row does not, none does.)
+struct WindowPages {
+  int sink_pages, lo_page, count;
+  int shift;                    // tokens left out between the two: column of token t behind the gap is t - shift
+  int begin, end, sink;
+};
+__host__ __device__ inline WindowPages window_pages(int sinks, int left, int right, int len, int pa, int pb) {
+  const WindowBounds a = window_bounds(sinks, left, right, len, pa), b = window_bounds(sinks, left, right, len, pb);
+  const bool any = a.first < a.end;
+  WindowPages w;
+  w.sink = sinks < b.end ? sinks : b.end;
+  w.sink_pages = (w.sink + kPageSize - 1) / kPageSize;
+  w.lo_page = any ? a.first / kPageSize : w.sink_pages;
+  const int hi_page = any ? (b.end + kPageSize - 1) / kPageSize : w.lo_page;
+  if (w.lo_page <= w.sink_pages) {                                   // no gap: everything from token 0 on
+    w.count = hi_page > w.sink_pages ? hi_page : w.sink_pages;
+    w.sink_pages = w.lo_page = 0;
+  } else {
+    w.count = w.sink_pages + hi_page - w.lo_page;
+  }
+  w.shift = (w.lo_page - w.sink_pages) * kPageSize;
+  w.begin = any ? a.first - w.shift : 0;
+  w.end = any ? b.end - w.shift : 0;
+  return w;
+}
+
+// Columns of the page sequence that a row sees: [begin, end), and [0, sink).
+struct WindowColumns {
+  int begin, end, sink;
+};
+__device__ __forceinline__ WindowColumns window_columns(const WindowArgs& a, const WindowPages& w, int len, int p) {
+  const WindowBounds b = window_bounds(a.sinks, a.left, a.right, len, p);
+  WindowColumns c;
+  c.begin = b.first - w.shift;
+  c.end = b.end - w.shift;
+  c.sink = min(a.sinks, b.end);
+  if (b.first >= b.end) c.begin = c.end = 0;
+  return c;
+}
+
+// One work item.
+struct WindowItem {
+  int hk, row0, split;          // KV head, first packed row, range of key tiles
+  int tile_begin, tile_end;     // key tiles of the row tile's page sequence
+  WindowPages pages;
+};
+// kTile: tokens of a key tile.  Row tiles of a request have the same number of ranges; a range past a tile's end is empty.
+template <int kTile>
+__device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const WindowReq& r, int item, int tile_rows) {
+  WindowItem it;
+  const int G = a.Hq / a.Hkv;
+  int at = item - r.item_begin;
+  const int per_head = r.row_tiles * r.splits;
+  it.hk = at / per_head;
+  at -= it.hk * per_head;
+  const int tile = at / r.splits;
+  it.split = at - tile * r.splits;
+  it.row0 = tile * tile_rows;
+  const int last = min(it.row0 + tile_rows, r.n * G) - 1;
+  it.pages = window_pages(a.sinks, a.left, a.right, r.len, r.pos + it.row0 / G, r.pos + last / G);
+  const int tiles = (it.pages.count * kPageSize + kTile - 1) / kTile;
+  it.tile_begin = min(tiles, it.split * r.tiles_per_split);
+  it.tile_end = min(tiles, it.tile_begin + r.tiles_per_split);
+  return it;
+}
+// The pool page of page `s` of an item's sequence.
+__device__ __forceinline__ int window_page(const WindowReq& r, const int* pages, const WindowPages& w, int s) {
+  const int page = s < w.sink_pages ? s : s - w.sink_pages + w.lo_page;          // of the prefix
+  return pages[page < r.sink_pages ? page : page - r.gap];
+}
+__device__ __forceinline__ const int* window_page_list(const WindowArgs& a, const WindowReq& r, const int* list) {
+  return a.staged_pages ? a.staged_pages : list + r.page_word;
+}
+// The slots of page `s` of the sequence that some row of the item sees: [lo, hi), and [0, sink) besides.  What lies
+// in the others must not reach a sum, not even with weight 0: it may be no number.
+struct WindowSlots {
+  int lo, hi, sink;
+  __device__ __forceinline__ bool whole() const { return (lo <= 0 && hi >= kPageSize) || sink >= kPageSize; }
+  __device__ __forceinline__ bool has(int slot) const { return (slot >= lo && slot < hi) || slot < sink; }
+};
+__device__ __forceinline__ WindowSlots window_slots(const WindowPages& w, int s) {
+  return WindowSlots{w.begin - s * kPageSize, w.end - s * kPageSize, w.sink - s * kPageSize};
+}
+
+// Where the results of a packed row go.
+struct WindowRow {
+  int t, h;                     // row of the request, query head
+  __device__ __forceinline__ WindowRow(const WindowArgs& a, int hk, int p) {
+    const int G = a.Hq / a.Hkv;
+    t = p / G;
+    h = hk * G + (p - t * G);
+  }
+};
+__device__ __forceinline__ long long window_part(const WindowArgs& a, const WindowReq& r, int split, const WindowRow& w) {
+  return r.part_off + ((long long)split * r.n + w.t) * a.Hq + w.h;
+}
+
+// ---------------------------------------------------------------------------------------------
+// CUDA-core kernel.  256 threads take a row tile against key tiles of 64: queries, keys and values lie in shared memory
+// as fp32 (a row's end padded by 16 bytes, so that lanes on neighbouring rows read other banks), the values where the
+// keys were.  A row tile of 64 is a grid of 16 x 16 threads, each with 4 rows x 4 keys of the scores and 4 rows x
+// D / 16 dims of the output.  A row tile of 16, for few rows, is four groups of 4 x 16 threads, each group with a quarter
+// of the keys of a tile and a running softmax of its own; they are put together at the end.  All sums in fp32.
+// ---------------------------------------------------------------------------------------------
+constexpr int kWinThreads = 256;
+constexpr int kWinKeys = 64;
+constexpr int kWinPer = 4;                      // rows of a thread
+constexpr int kWinLanes = 16;                   // threads that share a row
+
+inline size_t window_simt_smem(int rows, int D) {
+  return sizeof(float) * ((size_t)(rows + kWinKeys) * (D + 4) + (size_t)kWinKeys * (rows + 4));
+}
+
+__device__ __forceinline__ float lanes16_max(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float lanes16_sum(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+template <typename T, int kRows, int kMaxD, int kWords>
+__global__ void __launch_bounds__(kWinThreads)
+window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__ ParamList<kWords> list) {
+  using Tr = ElemTraits<T>;
+  constexpr int kPer = Tr::kPerChunk, kEsize = (int)sizeof(T);
+  constexpr int kRowGroups = kRows / kWinPer, kParts = kWinThreads / (kRowGroups * kWinLanes);   // groups over the keys
+  constexpr int kPartKeys = kWinKeys / kParts, kMine = kPartKeys / kWinLanes;                    // of a group, of a thread
+  constexpr int kPairs = kMaxD / (2 * kWinLanes);                  // pairs of dims of a thread
+  constexpr int kPPitch = kRows + 4;
+  extern __shared__ __align__(16) float win_smem[];
+  const int D = a.D, pitch = D + 4, chunks = D / kPer;
+  float* const qs = win_smem;                                      // [kRows][pitch]
+  float* const ks = qs + kRows * pitch;                            // [kWinKeys][pitch]: keys, then values
+  float* const ps = ks + kWinKeys * pitch;                         // [kWinKeys][kPPitch]
+  const WindowReq& r = window_req(list.w, a.num_reqs, blockIdx.x);
+  const WindowItem it = window_item<kWinKeys>(a, r, blockIdx.x, kRows);
+  const int* const pages = window_page_list(a, r, list.w);
+  const int G = a.Hq / a.Hkv, packed = r.n * G;
+  const int tid = threadIdx.x, tx = tid % kWinLanes, ty = tid / kWinLanes % kRowGroups, part = tid / (kWinLanes * kRowGroups);
+
+  for (int i = tid; i < kRows * chunks; i += kWinThreads) {
+    const int row = i / chunks, c = i - row * chunks, p = it.row0 + row;
+    float f[kPer];
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (p < packed) {
+      const WindowRow w(a, it.hk, p);
+      v = *reinterpret_cast<const uint4*>(a.q + ((r.row + w.t) * a.q_stride + (long long)w.h * D) * kEsize + c * 16);
+    }
+    Tr::unpack(v, f);
+#pragma unroll
+    for (int e = 0; e < kPer; e += 4)
+      *reinterpret_cast<float4*>(&qs[row * pitch + c * kPer + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+  }
+  WindowColumns col[kWinPer];
+#pragma unroll
+  for (int i = 0; i < kWinPer; ++i) {
+    const int p = it.row0 + ty * kWinPer + i;
+    col[i] = WindowColumns{0, 0, 0};
+    if (p < packed) col[i] = window_columns(a, it.pages, r.len, r.pos + p / G);
+  }
+
+  float m_run[kWinPer], l_run[kWinPer], acc[kWinPer][2 * kPairs];
+#pragma unroll
+  for (int i = 0; i < kWinPer; ++i) {
+    m_run[i] = -INFINITY;
+    l_run[i] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] = 0.f;
+  }
+  auto stage = [&](const char* pool, int tile) {
+    for (int i = tid; i < kWinKeys * chunks; i += kWinThreads) {
+      const int key = i / chunks, c = i - key * chunks, s = tile * (kWinKeys / kPageSize) + key / kPageSize;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (s < it.pages.count && window_slots(it.pages, s).has(key % kPageSize))
+        v = *reinterpret_cast<const uint4*>(pool + window_page(r, pages, it.pages, s) * a.page_stride +
+                                            (long long)it.hk * a.page_bytes +
+                                            page_chunk_offset(a.swizzled != 0, key % kPageSize, c, chunks * 16));
+      float f[kPer];
+      Tr::unpack(v, f);
+#pragma unroll
+      for (int e = 0; e < kPer; e += 4)
+        *reinterpret_cast<float4*>(&ks[key * pitch + c * kPer + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+    }
+  };
+
+  for (int tile = it.tile_begin; tile < it.tile_end; ++tile) {
+    __syncthreads();
+    stage(a.pool_k, tile);
+    __syncthreads();
+    float s[kWinPer][kMine];
+#pragma unroll
+    for (int i = 0; i < kWinPer; ++i)
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) s[i][j] = 0.f;
+    for (int d = 0; d < D; d += 4) {
+      float4 qv[kWinPer], kv[kMine];
+#pragma unroll
+      for (int i = 0; i < kWinPer; ++i) qv[i] = *reinterpret_cast<const float4*>(&qs[(ty * kWinPer + i) * pitch + d]);
+#pragma unroll
+      for (int j = 0; j < kMine; ++j)
+        kv[j] = *reinterpret_cast<const float4*>(&ks[(part * kPartKeys + tx + j * kWinLanes) * pitch + d]);
+#pragma unroll
+      for (int i = 0; i < kWinPer; ++i)
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          s[i][j] = fmaf(qv[i].x, kv[j].x, s[i][j]);
+          s[i][j] = fmaf(qv[i].y, kv[j].y, s[i][j]);
+          s[i][j] = fmaf(qv[i].z, kv[j].z, s[i][j]);
+          s[i][j] = fmaf(qv[i].w, kv[j].w, s[i][j]);
+        }
+    }
+    __syncthreads();                                               // the keys have been read
+    stage(a.pool_v, tile);
+#pragma unroll
+    for (int i = 0; i < kWinPer; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int c = tile * kWinKeys + part * kPartKeys + tx + j * kWinLanes;
+        const bool seen = (c >= col[i].begin && c < col[i].end) || c < col[i].sink;
+        s[i][j] = seen ? s[i][j] * a.scale : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+      const float m_new = fmaxf(m_run[i], lanes16_max(mx));
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen so far: every weight is 0
+      const float alpha = expf(m_run[i] - m_use);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        s[i][j] = expf(s[i][j] - m_use);
+        sum += s[i][j];
+      }
+      l_run[i] = l_run[i] * alpha + sum;                           // of this thread's keys; added up at the end
+      m_run[i] = m_new;
+#pragma unroll
+      for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] *= alpha;
+    }
+#pragma unroll
+    for (int j = 0; j < kMine; ++j)
+      *reinterpret_cast<float4*>(&ps[(part * kPartKeys + tx + j * kWinLanes) * kPPitch + ty * kWinPer]) =
+          make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+    __syncthreads();
+#pragma unroll 4
+    for (int key = part * kPartKeys; key < (part + 1) * kPartKeys; ++key) {
+      const float4 p = *reinterpret_cast<const float4*>(&ps[key * kPPitch + ty * kWinPer]);
+      const float pr[kWinPer] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+        const int d = (g * kWinLanes + tx) * 2;
+        if (d < D) {
+          const float2 v = *reinterpret_cast<const float2*>(&ks[key * pitch + d]);
+#pragma unroll
+          for (int i = 0; i < kWinPer; ++i) {
+            acc[i][2 * g] = fmaf(pr[i], v.x, acc[i][2 * g]);
+            acc[i][2 * g + 1] = fmaf(pr[i], v.y, acc[i][2 * g + 1]);
+          }
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int i = 0; i < kWinPer; ++i) l_run[i] = lanes16_sum(l_run[i]);
+  if (kParts > 1) {
+    // the groups' results: accumulators where the keys and values were, statistics where the weights were
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWinPer; ++i) {
+      const int row = ty * kWinPer + i;
+      if (tx == 0) {
+        ps[part * kRows + row] = m_run[i];
+        ps[(kParts + part) * kRows + row] = l_run[i];
+      }
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+        const int d = (g * kWinLanes + tx) * 2;
+        if (d < D) *reinterpret_cast<float2*>(&ks[(part * kRows + row) * pitch + d]) = make_float2(acc[i][2 * g], acc[i][2 * g + 1]);
+      }
+    }
+    __syncthreads();
+    if (part != 0) return;
+#pragma unroll
+    for (int i = 0; i < kWinPer; ++i) {
+      const int row = ty * kWinPer + i;
+      float m_all = m_run[i];
+#pragma unroll
+      for (int o = 1; o < kParts; ++o) m_all = fmaxf(m_all, ps[o * kRows + row]);
+      const float m_use = m_all == -INFINITY ? 0.f : m_all;
+      float l_all = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2 * kPairs; ++g) acc[i][g] = 0.f;
+#pragma unroll
+      for (int o = 0; o < kParts; ++o) {
+        const float w = expf(ps[o * kRows + row] - m_use);
+        l_all += w * ps[(kParts + o) * kRows + row];
+#pragma unroll
+        for (int g = 0; g < kPairs; ++g) {
+          const int d = (g * kWinLanes + tx) * 2;
+          if (d < D) {
+            const float2 v = *reinterpret_cast<const float2*>(&ks[(o * kRows + row) * pitch + d]);
+            acc[i][2 * g] += w * v.x;
+            acc[i][2 * g + 1] += w * v.y;
+          }
+        }
+      }
+      m_run[i] = m_all;
+      l_run[i] = l_all;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kWinPer; ++i) {
+    const int p = it.row0 + ty * kWinPer + i;
+    if (p >= packed) break;
+    const WindowRow w(a, it.hk, p);
+    const float inv = l_run[i] == 0.f ? 0.f : 1.f / l_run[i];
+    const float lse = l_run[i] == 0.f ? -INFINITY : m_run[i] + logf(l_run[i]);
+    if (r.splits > 1) {
+      const long long at = window_part(a, r, it.split, w);
+      if (tx == 0) a.part_lse[at] = lse;
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+        const int d = (g * kWinLanes + tx) * 2;
+        if (d < D) *reinterpret_cast<float2*>(a.part_o + at * D + d) = make_float2(acc[i][2 * g] * inv, acc[i][2 * g + 1] * inv);
+      }
+    } else {
+      const long long row = r.row + w.t;
+      char* const o = a.out + (row * a.out_stride + (long long)w.h * D) * kEsize;
+      if (tx == 0 && a.lse) a.lse[row * a.Hq + w.h] = lse;
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+        const int d = (g * kWinLanes + tx) * 2;
+        if (d < D) {
+          Tr::store(o + d * kEsize, acc[i][2 * g] * inv);
+          Tr::store(o + (d + 1) * kEsize, acc[i][2 * g + 1] * inv);
+        }
+      }
+    }
+  }
+}
+
+// A page list that does not fit the parameters goes through the workspace, written by launches of this kernel.
+template <int kWords>
+__global__ void stage_pages_kernel(int* __restrict__ dst, int count, const __grid_constant__ ParamList<kWords> list) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < count) dst[i] = list.w[i];
+}
+
+// ---------------------------------------------------------------------------------------------
+// Joins the ranges of a row-head: with l_s the log-sum-exp of range s and o_s its normalised result,
+//   lse = log sum_s exp(l_s),  o = sum_s exp(l_s - lse) o_s,
+// the ranges in ascending order.  kWarps = 1: a warp per row-head; kWarps = 8: the eight warps of a block share
+// one, warp w taking ranges w, w + 8, ..; for few row-heads of many ranges.  Placed on the SMs while the kernel before
+// it still runs, and waits for its end.
+// ---------------------------------------------------------------------------------------------
+constexpr int kJoinWarps = 8;
+constexpr int kMaxWindowSplits = 64;
+
+template <typename T, int kWarps, int kWords>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+window_join_kernel(const __grid_constant__ WindowArgs a, int row_heads, const int* status,
+                   const __grid_constant__ ParamList<kWords> list) {
+  __shared__ float red[kWarps == 1 ? 1 : kJoinWarps][kSimtMaxD];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rh = kWarps == 1 ? blockIdx.x * kJoinWarps + warp : blockIdx.x;
+  if (rh >= row_heads) return;
+  // the last split request that starts at or before the row-head (requests that are not split take no room)
+  const WindowReq* const reqs = reinterpret_cast<const WindowReq*>(list.w);
+  int lo = 0;
+  for (int hi = a.num_reqs; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (reqs[mid].row_heads_before <= rh) lo = mid;
+    else hi = mid;
+  }
+  const WindowReq& r = reqs[lo];
+  const int at = rh - r.row_heads_before, t = at / a.Hq, h = at - t * a.Hq;
+  const long long stride = (long long)r.n * a.Hq, p0 = r.part_off + at;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (status && *status != kDevOk) return;                         // some ranges were not computed
+  const float l0 = lane < r.splits ? a.part_lse[p0 + lane * stride] : -INFINITY;
+  const float l1 = lane + 32 < r.splits ? a.part_lse[p0 + (lane + 32) * stride] : -INFINITY;
+  const float mx = warp_max(fmaxf(l0, l1));
+  const bool any = mx > -INFINITY || __any_sync(0xffffffffu, l0 != l0 || l1 != l1);      // a NaN spreads
+  const float w0 = any ? expf(l0 - mx) : 0.f, w1 = any ? expf(l1 - mx) : 0.f;
+  const float total = warp_sum(w0 + w1), inv = any ? 1.f / total : 0.f;
+  const long long row = r.row + t;
+  constexpr int kStep = kWarps == 1 ? 1 : kJoinWarps;
+  for (int d0 = 0; d0 < a.D; d0 += 128) {
+    const int d = d0 + lane * 4;
+    const bool mine = d < a.D;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = kWarps == 1 ? 0 : warp; s0 < r.splits; s0 += 8 * kStep) {
+      float4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (mine) v[u] = *reinterpret_cast<const float4*>(a.part_o + (p0 + min(s0 + u * kStep, r.splits - 1) * stride) * a.D + d);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int s = s0 + u * kStep;
+        const float w = __shfl_sync(0xffffffffu, s < 32 ? w0 : w1, s & 31);
+        if (mine && s < r.splits) {
+          acc.x = fmaf(w, v[u].x, acc.x);
+          acc.y = fmaf(w, v[u].y, acc.y);
+          acc.z = fmaf(w, v[u].z, acc.z);
+          acc.w = fmaf(w, v[u].w, acc.w);
+        }
+      }
+    }
+    if (!mine) continue;
+    if (kWarps == 1) {
+      char* const o = a.out + (row * a.out_stride + (long long)h * a.D + d) * (int)sizeof(T);
+      const float f[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ElemTraits<T>::store(o + e * (int)sizeof(T), f[e]);
+    } else {
+      *reinterpret_cast<float4*>(&red[warp][d]) = acc;
+    }
+  }
+  if (kWarps > 1) {
+    __syncthreads();
+    for (int d = threadIdx.x; d < a.D; d += kJoinWarps * 32) {
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) sum += red[w][d];
+      ElemTraits<T>::store(a.out + (row * a.out_stride + (long long)h * a.D + d) * (int)sizeof(T), sum * inv);
+    }
+  }
+  if (lane == 0 && warp == (kWarps == 1 ? warp : 0) && a.lse) a.lse[row * a.Hq + h] = any ? mx + logf(total) : -INFINITY;
+}
+
+}  // namespace bicache
