@@ -29,6 +29,7 @@
 #include "tc_weights.cuh"
 #include "token_cache.cuh"
 #include "window.cuh"
+#include "tc_window.cuh"
 
 using namespace bicache;
 
@@ -949,7 +950,7 @@ int32_t bicache_create(const bicache_config* cfg, bicache_ctx** out) {
     delete ctx;
     return BICACHE_ERR_CUDA;
   }
-  if (configure_token_ops(tensor_ok) != cudaSuccess || configure_window(*cfg) != cudaSuccess) {
+  if (configure_token_ops(tensor_ok) != cudaSuccess || configure_window(*cfg, tensor_ok) != cudaSuccess) {
     destroy_host_resources(ctx);
     delete ctx;
     return BICACHE_ERR_CUDA;

@@ -1,0 +1,409 @@
+// Windowed attention over cached tokens on the tensor cores (bf16, head_dim 128); see window.cuh for the batch.
+//
+// A work item is 128 packed query rows of one KV head against a range of key tiles of 64 tokens of its page sequence.  As
+// in tc_decode_kernel a CTA is small (112 KB of shared memory, 256 TMEM columns: two to an SM, so that one computes
+// softmaxes while the MMAs of the other run) and S is double-buffered: S(j+1) = Q K(j+1)^T is issued before the softmax of
+// tile j ends.  Roles: warps 0-3 softmax (one thread per row; they also gather the Q tile), warp 4 MMA issue and TMEM, warp
+// 5 stages K tiles, warp 6 V tiles.  What the window adds:
+//   - pages are looked up in the item's page sequence (first tokens, then the window's);
+//   - a row knows the columns it sees as an interval and a number of first columns.  A tile that some row of a warp
+//     does not see in full is masked with the bits of a 64-bit word, and a row that has seen nothing yet keeps -inf as
+//     its reference and 0 for it in the exponent;
+//   - slots that no row of the item sees may hold anything.  Their scores are masked one way or another; as values they would
+//     meet weight 0, and 0 times a NaN is a NaN: a page of values with such slots is gathered in 16-byte pieces with
+//     these zeroed, where whole pages come by one bulk copy;
+//   - an item that has all the keys of its rows writes the output itself, in bf16; ranges write normalised partial
+//     results for window_join_kernel.
+#pragma once
+#include "tc_decode.cuh"
+#include "window.cuh"
+
+namespace bicache {
+namespace win {
+
+using namespace dec;
+
+// the first x of 64 bits
+__device__ __forceinline__ unsigned long long low_bits(int x) {
+  return x >= 64 ? ~0ull : x <= 0 ? 0ull : (1ull << x) - 1ull;
+}
+
+}  // namespace win
+
+template <int kWords>
+__global__ void __launch_bounds__(dec::kDecThreads, 2)
+tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wait_cycles,
+                 const __grid_constant__ ParamList<kWords> params) {
+  using namespace win;
+  // No room for alignment slack with two CTAs per SM: the kernel has no static shared memory, the
+  // dynamic window starts 1024-byte aligned (the swizzled tiles need that), and a CTA that finds
+  // otherwise reports an error instead of computing.
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* const smem = smem_raw;
+  DecSync* sy = reinterpret_cast<DecSync*>(smem + kQBytes + (kKStages + kVStages) * kKvTileBytes);
+  volatile int* abort_flag = &sy->abort_flag;
+  const unsigned q_smem = smem_u32(smem);
+  const unsigned k_ring = q_smem + kQBytes, v_ring = k_ring + kKStages * kKvTileBytes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // the joining kernel may be placed on the SMs from now on (it waits for this grid's end)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const WindowReq& r = window_req(params.w, a.num_reqs, blockIdx.x);
+  const WindowItem it = window_item<kKeys>(a, r, blockIdx.x, 128);
+  const int G = a.Hq / a.Hkv;
+  const int T = it.tile_end - it.tile_begin;
+  const int rows = min(128, r.n * G - it.row0);                // rows of the item; the warps beyond them do nothing
+  const int active = (rows + 31) >> 5;
+  auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - (it.tile_begin + j) * (kKeys / kPageSize)); };
+
+  if (tid == 0) {
+    sy->wait_cycles = wait_cycles;
+    if ((q_smem & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
+    sy->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
+    sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
+    mbar_init(smem_u32(&sy->q_full), 128);
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(smem_u32(&sy->k_full[i]), 32);
+      mbar_init(smem_u32(&sy->k_free[i]), 1);
+    }
+    for (int i = 0; i < kVStages; ++i) {
+      mbar_init(smem_u32(&sy->v_full[i]), 32);
+      mbar_init(smem_u32(&sy->v_free[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sy->s_full[i]), 1);
+      mbar_init(smem_u32(&sy->p_full[i]), 32 * active);
+    }
+    mbar_init(smem_u32(&sy->pv_done), 1);
+    mbar_init(smem_u32(&sy->o_done), 1);
+    mbar_init(smem_u32(&sy->drain), 1);
+    fence_barrier_init();
+  }
+  if (warp == 4) {
+    tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&sy->tmem_base);
+  const bool dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
+  const unsigned tmem_o = tmem + 128;
+
+  if (warp < 4) {
+    // ================================ softmax and epilogue =================================
+    const int row = warp * 32 + lane;                        // row of the tile = TMEM lane
+    const unsigned lane_base = (unsigned)(warp * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f;         // scores are handled in the log2 domain
+    float m_ref = -INFINITY, l_sum = 0.f;
+    bool ok = !dead;
+    if (ok && T > 0) {
+      // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i;
+      // rows past the end are zero-filled.
+      const int r0 = warp * 32 + (lane >> 4), c16 = lane & 15;
+      const int packed_rows = r.n * G;
+      const char* const q_head = a.q + (r.row * a.q_stride + (long long)it.hk * G * 128) * 2 + c16 * 16;
+      int prow = it.row0 + r0;
+      int t = prow / G, jj = prow - t * G;
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const bool valid = prow < packed_rows;
+        const char* src = q_head;
+        if (valid) src = q_head + ((long long)t * a.q_stride + jj * 128) * 2;
+        cp_async16(q_smem + tile_chunk_offset(r0 + 2 * i, c16), src, valid ? 16u : 0u);
+        prow += 2;
+        jj += 2;
+        while (jj >= G) {                           // at most twice (G >= 1)
+          jj -= G;
+          ++t;
+        }
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async();
+      mbar_arrive(smem_u32(&sy->q_full));
+    }
+    if (warp < active) {
+      // the columns this row sees, from the first tile on; a row past the end runs along unmasked
+      WindowColumns col = WindowColumns{0, 0x7fffffff, 0};
+      if (row < rows) col = window_columns(a, it.pages, r.len, r.pos + (it.row0 + row) / G);
+      const int col0 = it.tile_begin * kKeys;
+      for (int j = 0; j < T && ok; ++j) {
+        const int b = j & 1;
+        const int begin = col.begin - col0 - j * kKeys, end = col.end - col0 - j * kKeys, sink = col.sink - col0 - j * kKeys;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->s_full[b]), (j >> 1) & 1, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        unsigned s[64];
+        tmem_ld32(tmem + b * 64 + lane_base, s);
+        tmem_ld32(tmem + b * 64 + 32 + lane_base, s + 32);
+        tmem_wait_ld();
+        if (__any_sync(0xffffffffu, begin > 0 || end < kKeys)) {
+          const unsigned long long seen = (low_bits(end) & ~low_bits(begin)) | low_bits(sink);
+          const unsigned lo = (unsigned)seen, hi = (unsigned)(seen >> 32);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (!((lo >> i) & 1u)) s[i] = 0xff800000u;             // -inf
+            if (!((hi >> i) & 1u)) s[32 + i] = 0xff800000u;
+          }
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 64; i += 4) {
+          mx0 = max3(mx0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+          mx1 = max3(mx1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+        }
+        const float mx = fmaxf(mx0, mx1) * sl2;                // scale > 0
+        if (j == 0) {
+          m_ref = mx;
+        } else if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
+          // Rare: a row's maximum exceeds the reference by more than 2^8, or it sees its first key.  O must be rescaled, and
+          // S of this tile was issued before O += P V of the previous one: wait for that first.
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->pv_done), (j - 1) & 1, abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          float alpha = 1.f;
+          if (mx > m_ref + 8.f) {
+            alpha = ex2(m_ref - mx);
+            m_ref = mx;
+          }
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            unsigned o[32];
+            tmem_ld32(tmem_o + c * 32 + lane_base, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+            tmem_st32(tmem_o + c * 32 + lane_base, o);
+          }
+          tmem_wait_st();
+          l_sum *= alpha;
+        }
+        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;     // nothing seen so far: every weight is 0
+        const unsigned long long sl2_2 = pack2(sl2, sl2), neg_m2 = pack2(neg_m, neg_m);
+        unsigned long long acc_a = pack2(0.f, 0.f), acc_b = pack2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const unsigned long long xa =
+              fma2(pack2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), sl2_2, neg_m2);
+          const unsigned long long xb =
+              fma2(pack2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), sl2_2, neg_m2);
+          float x0, x1, x2, x3;
+          unpack2(xa, x0, x1);
+          unpack2(xb, x2, x3);
+          const float p0 = ex2(x0), p1 = ex2(x1), p2 = ex2(x2), p3 = ex2(x3);
+          acc_a = add2(acc_a, pack2(p0, p1));
+          acc_b = add2(acc_b, pack2(p2, p3));
+          s[2 * i] = pack_bf16(p0, p1);                          // what the MMA takes; the sum takes them unrounded
+          s[2 * i + 1] = pack_bf16(p2, p3);
+        }
+        tmem_st32(tmem + b * 64 + lane_base, s);               // P over the first 32 columns of this S
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(smem_u32(&sy->p_full[b]));
+        float s0, s1, s2, s3;
+        unpack2(acc_a, s0, s1);
+        unpack2(acc_b, s2, s3);
+        l_sum += (s0 + s1) + (s2 + s3);
+      }
+      // -------- epilogue: the output, or the normalised partial of this key range --------
+      if (ok && T > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->o_done), 0, abort_flag));
+        tc_fence_after();
+      }
+      if (ok) {
+        const bool mine = row < rows;
+        const WindowRow w(a, it.hk, it.row0 + (mine ? row : 0));
+        const long long at = window_part(a, r, it.split, w), out_row = r.row + w.t;
+        const bool whole = r.splits == 1;
+        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
+        const float lse = l_sum == 0.f ? -INFINITY : (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+        // A thread holds a row (128 values).  It goes to shared memory first (the K/V rings are free by now: every tile has been
+        // consumed; rows 528 bytes apart keep the 16-byte stores conflict-free) and leaves as one bulk copy.
+        unsigned char* const stage_row = smem + kQBytes + row * 528;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          unsigned o[32];
+          if (T > 0) {
+            tmem_ld32(tmem_o + c * 32 + lane_base, o);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = 0u;
+          }
+          if (whole) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint4 v;
+              v.x = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+              v.y = pack_bf16(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+              v.z = pack_bf16(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+              v.w = pack_bf16(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+              *reinterpret_cast<uint4*>(stage_row + (c * 32 + i) * 2) = v;
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<float4*>(stage_row + (c * 32 + i) * 4) =
+                  make_float4(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv,
+                              __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+          }
+        }
+        fence_proxy_async();
+        if (mine) {
+          const void* const dst = whole ? (const void*)(a.out + (out_row * a.out_stride + (long long)w.h * 128) * 2)
+                                        : (const void*)(a.part_o + at * 128);
+          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                       ::"l"(dst), "r"(smem_u32(stage_row)), "r"(whole ? 256u : 512u) : "memory");
+          bulk_commit_group();
+          if (!whole) a.part_lse[at] = lse;
+          else if (a.lse) a.lse[out_row * a.Hq + w.h] = lse;
+          bulk_wait_all();
+        }
+      }
+      tc_fence_before();
+    }
+  } else if (warp == 4) {
+    // ====================================== MMA issue ======================================
+    bool ok = !dead && T > 0;
+    if (ok) {
+      const unsigned long long q_desc = make_desc(q_smem, 16, 2048);
+      const unsigned el = elect_one() ? 1u : 0u;               // the lane that issues every MMA of this warp
+      // a K step of 16 dims: 32 bytes inside the swizzled row; dims 64.. sit 1024 bytes further
+      auto kstep = [](int k) { return (unsigned long long)((k & 3) * 2 + (k >> 2) * 64); };
+      auto issue_s = [&](int j) {
+        const int b = j & 1, ks = j % kKStages;
+        bool good = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_full[ks]), (j / kKStages) & 1, abort_flag));
+        if (!good) return false;
+        tc_fence_after();
+        const unsigned long long k_desc = make_desc(k_ring + ks * kKvTileBytes, 16, 2048);
+        unsigned long long qa[8], kb[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          qa[k] = q_desc + kstep(k);
+          kb[k] = k_desc + kstep(k);
+        }
+        mma_ss_batch8(el, tmem + b * 64, qa, kb, kIdescS64);
+        mma_commit_pred(el, smem_u32(&sy->s_full[b]));
+        mma_commit_pred(el, smem_u32(&sy->k_free[ks]));
+        return true;
+      };
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->q_full), 0, abort_flag));
+      if (ok) ok = issue_s(0);
+      for (int j = 0; j < T && ok; ++j) {
+        const int b = j & 1;
+        if (j + 1 < T) {
+          ok = issue_s(j + 1);
+          if (!ok) break;
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->p_full[b]), (j >> 1) & 1, abort_flag));
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->v_full[b]), (j >> 1) & 1, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        // V is the MN-major operand: 64-dim halves 1024 bytes apart, 8-key groups 2048 bytes; a K
+        // step of 16 keys is one page image (4096 bytes).  Pages past the last are skipped.
+        const unsigned long long v_desc = make_desc(v_ring + b * kKvTileBytes, 1024, 2048);
+        const unsigned long long vb[4] = {v_desc, v_desc + 256ull, v_desc + 512ull, v_desc + 768ull};
+        mma_ts_batch4_first(el, tmem_o, tmem + b * 64, vb, kIdescPV, j > 0 ? 1u : 0u, tile_pages(j));
+        mma_commit_pred(el, smem_u32(&sy->v_free[b]));
+        mma_commit_pred(el, smem_u32(&sy->pv_done));
+        if (j == T - 1) mma_commit_pred(el, smem_u32(&sy->o_done));
+      }
+      // Whatever happened, let every MMA issued so far finish before TMEM is released.
+      __syncwarp();
+      mma_commit_elect(smem_u32(&sy->drain));
+      mbar_wait_issued(smem_u32(&sy->drain), 0);
+    }
+    __syncwarp();
+  } else {
+    // ======================================= loads ========================================
+    // Warp 5 stages the K tiles, warp 6 the V tiles.
+    const int is_v = warp - 5;
+    bool ok = !dead;
+    const int stages = is_v ? kVStages : kKStages;
+    int armed[kKStages] = {-1, -1, -1};      // the last tile armed with bulk copies, per stage
+    const unsigned ring = is_v ? v_ring : k_ring;
+    const int* const pages = window_page_list(a, r, params.w);
+    const char* const pool = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes;
+    for (int j = 0; j < T && ok; ++j) {
+      const int b = j % stages;
+      const unsigned free_bar = smem_u32(is_v ? &sy->v_free[b] : &sy->k_free[b]);
+      const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
+      // the page of lanes 0-3, looked up while the slot is still in use
+      const int npages = tile_pages(j), s = (it.tile_begin + j) * (kKeys / kPageSize) + lane;
+      const char* src = pool;
+      bool bulk = lane < npages;
+      WindowSlots slots = WindowSlots{0, kPageSize, 0};
+      if (bulk) {
+        src = pool + window_page(r, pages, it.pages, s) * a.page_stride;
+        if (is_v) {
+          slots = window_slots(it.pages, s);
+          bulk = slots.whole();
+        }
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
+      if (!ok) break;
+      const unsigned dst = ring + b * kKvTileBytes;
+      const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
+      if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
+      const unsigned pieces = ~bulks & ((1u << npages) - 1u);
+      if (pieces != 0) {
+        for (int p = 0; p < npages; ++p) {
+          if (!((pieces >> p) & 1u)) continue;
+          const char* const from =
+              reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), p));
+          WindowSlots sl;
+          sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
+          sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
+          sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
+          // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
+#pragma unroll
+          for (int i = 0; i < kPageBytes / 512; ++i) {
+            const unsigned at = (unsigned)(i * 512 + lane * 16);
+            cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
+          }
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async();
+      }
+      // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
+      if (lane == 0) {
+        mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
+        armed[b] = j;
+      } else {
+        mbar_arrive(full);
+      }
+    }
+    cp_async_wait<0>();
+    // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
+    if (!dead && (!ok || *abort_flag) && lane == 0) {
+      for (int b = 0; b < stages; ++b)
+        if (armed[b] >= 0) {
+          const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
+          for (unsigned n = 0; n < 4096 && !mbar_try_wait(full, (armed[b] / stages) & 1); ++n) __nanosleep(256);
+        }
+    }
+  }
+
+  __syncthreads();
+  if (warp == 4) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kDecTmemCols);
+  }
+  if (tid == 0 && !dead && *abort_flag) atomicCAS(status, kDevOk, kDevTimeout);
+}
+
+template <int kWords>
+inline cudaError_t configure_tc_window() {
+  return cudaFuncSetAttribute(tc_window_kernel<kWords>, cudaFuncAttributeMaxDynamicSharedMemorySize, dec::kDecSmemBytes);
+}
+
+template <int kWords>
+inline cudaError_t launch_tc_window(const WindowArgs& a, const ParamList<kWords>& list, int* status, long long wait_cycles,
+                                    cudaStream_t stream) {
+  tc_window_kernel<kWords><<<(unsigned)a.num_items, dec::kDecThreads, dec::kDecSmemBytes, stream>>>(
+      a, status, wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, list);
+  return cudaGetLastError();
+}
+
+}  // namespace bicache

@@ -482,6 +482,22 @@ class WindowSimtLaunches : public WindowLaunches {
   }
 };
 
+class WindowTensorLaunches : public WindowLaunches {
+ public:
+  WindowTensorLaunches(bicache_ctx* ctx, const WindowArgs& args, cudaStream_t stream)
+      : WindowLaunches(ctx, args, WindowForm{128, dec::kKeys, 2 * ctx->sm_count, 4, 4}, stream) {}
+
+ protected:
+  cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
+    cudaError_t e = cudaSuccess;
+    with_param_list(list, words, [&](const auto& params) {
+      e = launch_tc_window(a, params, ctx_->d_status, ctx_->wait_cycles, stream_);
+    }, WindowLengths());
+    return e;
+  }
+  const int* status() const override { return ctx_->d_status; }
+};
+
 int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id, const int32_t* cached_len,
                        const int32_t* query_pos, const int64_t* row_off, const int32_t* seqlen, const void* q,
                        int64_t q_row_stride, void* out, int64_t out_row_stride, float* lse_out, int32_t sinks,
@@ -556,6 +572,12 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     }
     return launches.flush();
   };
+  // the tensor-core kernel takes the row maximum before scaling, which needs a positive scale
+  if (ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && softmax_scale > 0.f) {
+    ctx->last_kernel = BICACHE_KERNEL_KEY_RANGES;
+    WindowTensorLaunches launches(ctx, a, stream);
+    return run(launches, [](int) { return true; });
+  }
   ctx->last_kernel = BICACHE_KERNEL_SIMT;
   // a row tile of 16 where that holds a request's rows of a KV head, else of 64
   WindowSimtLaunches few(ctx, a, 16, stream), many(ctx, a, 64, stream);
@@ -563,7 +585,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   return st != BICACHE_OK ? st : run(many, [&](int n) { return (long long)n * G > 16; });
 }
 
-cudaError_t configure_window(const bicache_config& cfg) {
+cudaError_t configure_window(const bicache_config& cfg, bool tensor_ok) {
   cudaError_t e = cudaSuccess;
   each_param_length([&](auto words) {
     constexpr int kWords = decltype(words)::value;
@@ -574,6 +596,10 @@ cudaError_t configure_window(const bicache_config& cfg) {
                                    cudaFuncAttributeMaxDynamicSharedMemorySize, (int)window_simt_smem(rows, decltype(dim)::value));
       });
   }, WindowSimtLengths());
+  if (tensor_ok)
+    each_param_length([&](auto words) {
+      if (e == cudaSuccess) e = configure_tc_window<decltype(words)::value>();
+    }, WindowLengths());
   return e;
 }
 
