@@ -8,6 +8,7 @@ from __future__ import annotations
 import array
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -222,6 +223,22 @@ def _host(a, code):
     a = array.array(code, a)
     address, n = a.buffer_info()
     return a, address, n
+
+
+def _host_list(a, code):
+    """_host for the calls that take a list entry per request: struct.pack converts long lists a third faster."""
+    if isinstance(a, np.ndarray):
+        return _host(a, code)
+    n = len(a)
+    packed = struct.pack("%d%s" % (n, code), *a)
+    return packed, packed, n
+
+
+def _rows_within(off, n, count, rows):
+    """Does no run of rows, packed by _host_list, end past `rows`?"""
+    if count > 8:
+        return int((np.frombuffer(off, np.int64) + np.frombuffer(n, np.int32)).max()) <= rows
+    return all(o + k <= rows for o, k in zip(struct.unpack("%dq" % count, off), struct.unpack("%di" % count, n)))
 
 
 # torch.cuda.current_stream builds a Stream object (2 us); the bare handle is what the library takes
@@ -538,7 +555,7 @@ class BiCache:
         return positions.data_ptr()
 
     def _rope_pair(self, x, y, heads):
-        """Pointers and strides of a tensor and its rotated form."""
+        """Pointers and strides of a tensor of rows and its rotated form (or what attention makes of it)."""
         if x is None:
             assert y is None
             return None, 0, None, 0
@@ -604,66 +621,60 @@ class BiCache:
 
     # -- a cache that grows -------------------------------------------------------------------
     def _token_args(self, prefix_id, token_off, row_off, seqlen, k, v):
-        """Host arrays of a batch of tokens, their number, and the rows that they name."""
-        pid, ppid, count = _host(prefix_id, "i")
-        tok, ptok, n_tok = _host(token_off, "i")
-        off, poff, n_off = _host(row_off, "q")
-        n, pn, n_len = _host(seqlen, "i")
+        """Number of requests, the host arrays of a batch of tokens, rows of the tensors and their stride."""
+        _, ppid, count = _host_list(prefix_id, "i")
+        _, ptok, n_tok = _host_list(token_off, "i")
+        _, poff, n_off = _host_list(row_off, "q")
+        _, pn, n_len = _host_list(seqlen, "i")
         assert count == n_tok == n_off == n_len
-        self._own(k, self.dtype)
-        self._own(v, self.dtype)
-        rows, heads, d = k.shape
-        assert v.shape == k.shape and v.stride() == k.stride() and heads == self.Hkv and d == self.D
-        assert k.stride(2) == 1 and k.stride(1) == d
-        assert not count or max(map(int.__add__, off, n) if isinstance(off, array.array) and isinstance(n, array.array)
-                                else np.add(off, n)) <= rows, "a request's rows reach past the tensors"
-        return (pid, tok, off, n), count, ppid, ptok, poff, pn, rows
+        dtype, device = self.dtype, self.device
+        assert k.dtype == v.dtype == dtype and k.device == v.device == device, "%s tensors on %s are needed" % (dtype, device)
+        (rows, heads, d), strides = k.shape, k.stride()
+        assert v.shape == k.shape and v.stride() == strides and heads == self.Hkv and d == self.D
+        assert strides[2] == 1 and strides[1] == d
+        assert _rows_within(poff, pn, count, rows), "a request's rows reach past the tensors"
+        return count, ppid, ptok, poff, pn, rows, strides[0]
 
     def append_tokens(self, layer, prefix_id, token_off, row_off, seqlen, k, v, q=None, q_out=None, rotation=None,
                       positions=None):
         """Rows row_off[i] .. + seqlen[i] of k, v [rows, Hkv, D] become tokens token_off[i] .. of prefix prefix_id[i],
         the keys rotated (rotation None: stored as they are).  positions: int32 [num_axes, rows] or [rows]; None
         with one axis: the tokens' indices.  q [rows, Hq, D] is rotated into q_out (which may be q) alike."""
-        keep, count, ppid, ptok, poff, pn, rows = self._token_args(prefix_id, token_off, row_off, seqlen, k, v)
+        count, ppid, ptok, poff, pn, rows, row = self._token_args(prefix_id, token_off, row_off, seqlen, k, v)
         assert q is None or q.shape[0] == rows
         at, stride = (None, 0) if rotation is None else self._axis_positions(rotation, positions, rows)
         st = self.lib.bicache_append_tokens(self.ctx, layer, count, ppid, ptok, poff, pn, k.data_ptr(), v.data_ptr(),
-                                            k.stride(0), *self._rope_pair(q, q_out, self.Hq),
+                                            row, *self._rope_pair(q, q_out, self.Hq),
                                             None if rotation is None else rotation.pointer, at, stride, self._on_stream())
         self._check(st, "bicache_append_tokens")
 
     def read_tokens(self, layer, prefix_id, token_off, row_off, seqlen, k_out, v_out):
         """Tokens token_off[i] .. of prefix prefix_id[i] to rows row_off[i] .. of k_out, v_out [rows, Hkv, D]."""
-        keep, count, ppid, ptok, poff, pn, _ = self._token_args(prefix_id, token_off, row_off, seqlen, k_out, v_out)
+        count, ppid, ptok, poff, pn, _, row = self._token_args(prefix_id, token_off, row_off, seqlen, k_out, v_out)
         st = self.lib.bicache_read_tokens(self.ctx, layer, count, ppid, ptok, poff, pn, k_out.data_ptr(),
-                                          v_out.data_ptr(), k_out.stride(0), self._on_stream())
+                                          v_out.data_ptr(), row, self._on_stream())
         self._check(st, "bicache_read_tokens")
 
     def attend_window(self, layer, prefix_id, cached_len, query_pos, row_off, seqlen, q, out, lse=None, sinks=0, left=-1,
                       right=-1, scale=None):
         """Rows row_off[i] .. + seqlen[i] of q [rows, Hq, D], at positions query_pos[i] .., attend over the tokens
         t < cached_len[i] of prefix prefix_id[i] with t <= p + right and (t < sinks or t >= p - left); -1: no bound."""
-        pid, ppid, count = _host(prefix_id, "i")
-        cl, pcl, n_cl = _host(cached_len, "i")
-        qp, pqp, n_qp = _host(query_pos, "i")
-        off, poff, n_off = _host(row_off, "q")
-        n, pn, n_len = _host(seqlen, "i")
+        _, ppid, count = _host_list(prefix_id, "i")
+        _, pcl, n_cl = _host_list(cached_len, "i")
+        _, pqp, n_qp = _host_list(query_pos, "i")
+        _, poff, n_off = _host_list(row_off, "q")
+        _, pn, n_len = _host_list(seqlen, "i")
         assert count == n_cl == n_qp == n_off == n_len
-        self._own(q, self.dtype)
-        self._own(out, self.dtype)
-        rows, hq, d = q.shape
-        assert out.shape == q.shape and hq == self.Hq and d == self.D
-        assert q.stride(2) == out.stride(2) == 1 and q.stride(1) == out.stride(1) == d
-        assert not count or max(map(int.__add__, off, n) if isinstance(off, array.array) and isinstance(n, array.array)
-                                else np.add(off, n)) <= rows, "a request's rows reach past q"
+        q_at, q_row, out_at, out_row = self._rope_pair(q, out, self.Hq)
+        rows = q.shape[0]
+        assert _rows_within(poff, pn, count, rows), "a request's rows reach past q"
         lp = None
         if lse is not None:
             self._own(lse, torch.float32)
-            assert lse.is_contiguous() and lse.shape == (rows, hq)
+            assert lse.is_contiguous() and lse.shape == (rows, self.Hq)
             lp = lse.data_ptr()
-        st = self.lib.bicache_attend_window(self.ctx, layer, count, ppid, pcl, pqp, poff, pn, q.data_ptr(), q.stride(0),
-                                            out.data_ptr(), out.stride(0), lp, sinks, left, right,
-                                            d ** -0.5 if scale is None else scale, self._on_stream())
+        st = self.lib.bicache_attend_window(self.ctx, layer, count, ppid, pcl, pqp, poff, pn, q_at, q_row, out_at, out_row, lp,
+                                            sinks, left, right, self.D ** -0.5 if scale is None else scale, self._on_stream())
         self._check(st, "bicache_attend_window")
 
     def device_status(self, clear=False):

@@ -47,7 +47,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // the joining kernel may be placed on the SMs from now on (it waits for this grid's end)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const WindowReq& r = window_req(params.w, a.num_reqs, blockIdx.x);
+  const int status_now = *reinterpret_cast<volatile int*>(status);      // arrives while the item is looked up
+  const WindowReq& r = window_req(a, params.w, blockIdx.x);
   const WindowItem it = window_item<kKeys>(a, r, blockIdx.x, 128);
   const int G = a.Hq / a.Hkv;
   const int T = it.tile_end - it.tile_begin;
@@ -55,20 +56,67 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   const int active = (rows + 31) >> 5;
   auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - (it.tile_begin + j) * (kKeys / kPageSize)); };
 
+  // Set-up, all of it side by side: thread 0 its barriers, warp 4 TMEM, warps 5 and 6 their own barriers and the first
+  // tiles, for which they need nobody.
+  const int is_v = warp - 5;
+  const int stages = is_v ? kVStages : kKStages;
+  int armed[kKStages] = {-1, -1, -1};        // load warps: the last tile armed with bulk copies, per stage
+  // One tile into its slot, which is free.
+  auto load_tile = [&](int j) {
+    const int b = j % stages;
+    const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
+    const unsigned dst = (is_v ? v_ring : k_ring) + b * kKvTileBytes;
+    const int npages = tile_pages(j), s = (it.tile_begin + j) * (kKeys / kPageSize) + lane;
+    const char* src = nullptr;
+    bool bulk = lane < npages;
+    WindowSlots slots = WindowSlots{0, kPageSize, 0};
+    if (bulk) {
+      src = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes +
+            window_page(r, window_page_list(a, r, params.w), it.pages, s) * a.page_stride;
+      if (is_v) {
+        slots = window_slots(it.pages, s);
+        bulk = slots.whole();
+      }
+    }
+    const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
+    if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
+    const unsigned pieces = ~bulks & ((1u << npages) - 1u);
+    if (pieces != 0) {
+      for (int p = 0; p < npages; ++p) {
+        if (!((pieces >> p) & 1u)) continue;
+        const char* const from =
+            reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), p));
+        WindowSlots sl;
+        sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
+        sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
+        sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
+        // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
+#pragma unroll
+        for (int i = 0; i < kPageBytes / 512; ++i) {
+          const unsigned at = (unsigned)(i * 512 + lane * 16);
+          cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
+        }
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async();
+    }
+    // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
+    if (lane == 0) {
+      mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
+      armed[b] = j;
+    } else {
+      mbar_arrive(full);
+    }
+  };
+  const int ahead = min(T, stages);          // tiles that find their slots free
+  bool begun = false;
   if (tid == 0) {
     sy->wait_cycles = wait_cycles;
     if ((q_smem & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
-    sy->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
+    sy->dead = status_now != 0 || (q_smem & 1023u) != 0 ? 1 : 0;
     sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
-    mbar_init(smem_u32(&sy->q_full), 128);
-    for (int i = 0; i < kKStages; ++i) {
-      mbar_init(smem_u32(&sy->k_full[i]), 32);
-      mbar_init(smem_u32(&sy->k_free[i]), 1);
-    }
-    for (int i = 0; i < kVStages; ++i) {
-      mbar_init(smem_u32(&sy->v_full[i]), 32);
-      mbar_init(smem_u32(&sy->v_free[i]), 1);
-    }
+    mbar_init(smem_u32(&sy->q_full), 32 * active);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sy->s_full[i]), 1);
       mbar_init(smem_u32(&sy->p_full[i]), 32 * active);
@@ -77,10 +125,21 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     mbar_init(smem_u32(&sy->o_done), 1);
     mbar_init(smem_u32(&sy->drain), 1);
     fence_barrier_init();
-  }
-  if (warp == 4) {
+  } else if (warp == 4) {
     tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
     tmem_relinquish();
+  } else if (warp >= 5) {
+    if (lane == 0) {
+      for (int i = 0; i < stages; ++i) {
+        mbar_init(smem_u32(is_v ? &sy->v_full[i] : &sy->k_full[i]), 32);
+        mbar_init(smem_u32(is_v ? &sy->v_free[i] : &sy->k_free[i]), 1);
+      }
+      fence_barrier_init();
+    }
+    __syncwarp();
+    begun = status_now == 0 && (q_smem & 1023u) == 0;
+    if (begun)
+      for (int j = 0; j < ahead; ++j) load_tile(j);
   }
   tc_fence_before();
   __syncthreads();
@@ -96,36 +155,33 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     const float sl2 = a.scale * 1.4426950408889634f;         // scores are handled in the log2 domain
     float m_ref = -INFINITY, l_sum = 0.f;
     bool ok = !dead;
-    if (ok && T > 0) {
-      // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i;
-      // rows past the end are zero-filled.
-      const int r0 = warp * 32 + (lane >> 4), c16 = lane & 15;
-      const int packed_rows = r.n * G;
-      const char* const q_head = a.q + (r.row * a.q_stride + (long long)it.hk * G * 128) * 2 + c16 * 16;
-      int prow = it.row0 + r0;
-      int t = prow / G, jj = prow - t * G;
-#pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
-        const bool valid = prow < packed_rows;
-        const char* src = q_head;
-        if (valid) src = q_head + ((long long)t * a.q_stride + jj * 128) * 2;
-        cp_async16(q_smem + tile_chunk_offset(r0 + 2 * i, c16), src, valid ? 16u : 0u);
-        prow += 2;
-        jj += 2;
-        while (jj >= G) {                           // at most twice (G >= 1)
-          jj -= G;
-          ++t;
-        }
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-      fence_proxy_async();
-      mbar_arrive(smem_u32(&sy->q_full));
-    }
     if (warp < active) {
-      // the columns this row sees, from the first tile on; a row past the end runs along unmasked
+      if (ok && T > 0) {
+        // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i.
+        // Rows past the end stay what they are: a row of Q meets no other row's results.
+        const int r0 = warp * 32 + (lane >> 4), c16 = lane & 15;
+        const char* const q_head = a.q + (r.row * a.q_stride + (long long)it.hk * G * 128) * 2 + c16 * 16;
+        const int prow = it.row0 + r0;
+        int t = prow / G, jj = prow - t * G;
+        const int here = min(32, rows - warp * 32);
+#pragma unroll 4
+        for (int i = lane >> 4; i < here; i += 2) {
+          cp_async16(q_smem + tile_chunk_offset(warp * 32 + i, c16), q_head + ((long long)t * a.q_stride + jj * 128) * 2, 16u);
+          jj += 2;
+          while (jj >= G) {                         // at most twice (G >= 1)
+            jj -= G;
+            ++t;
+          }
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async();
+        mbar_arrive(smem_u32(&sy->q_full));
+      }
+      // the columns this row sees, from the first tile on; a row past the end runs along unmasked and asks for nothing
+      const bool mine = row < rows;
       WindowColumns col = WindowColumns{0, 0x7fffffff, 0};
-      if (row < rows) col = window_columns(a, it.pages, r.len, r.pos + (it.row0 + row) / G);
+      if (mine) col = window_columns(a, it.pages, r.len, r.pos + (it.row0 + row) / G);
       const int col0 = it.tile_begin * kKeys;
       for (int j = 0; j < T && ok; ++j) {
         const int b = j & 1;
@@ -152,7 +208,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
           mx0 = max3(mx0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
           mx1 = max3(mx1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
         }
-        const float mx = fmaxf(mx0, mx1) * sl2;                // scale > 0
+        const float mx = mine ? fmaxf(mx0, mx1) * sl2 : -INFINITY;       // scale > 0
         if (j == 0) {
           m_ref = mx;
         } else if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
@@ -211,7 +267,6 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
         tc_fence_after();
       }
       if (ok) {
-        const bool mine = row < rows;
         const WindowRow w(a, it.hk, it.row0 + (mine ? row : 0));
         const long long at = window_part(a, r, it.split, w), out_row = r.row + w.t;
         const bool whole = r.splits == 1;
@@ -257,7 +312,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
           bulk_commit_group();
           if (!whole) a.part_lse[at] = lse;
           else if (a.lse) a.lse[out_row * a.Hq + w.h] = lse;
-          bulk_wait_all();
+          bulk_wait_read();                                        // the rows have left shared memory
         }
       }
       tc_fence_before();
@@ -317,66 +372,15 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   } else {
     // ======================================= loads ========================================
     // Warp 5 stages the K tiles, warp 6 the V tiles.
-    const int is_v = warp - 5;
     bool ok = !dead;
-    const int stages = is_v ? kVStages : kKStages;
-    int armed[kKStages] = {-1, -1, -1};      // the last tile armed with bulk copies, per stage
-    const unsigned ring = is_v ? v_ring : k_ring;
-    const int* const pages = window_page_list(a, r, params.w);
-    const char* const pool = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes;
-    for (int j = 0; j < T && ok; ++j) {
-      const int b = j % stages;
-      const unsigned free_bar = smem_u32(is_v ? &sy->v_free[b] : &sy->k_free[b]);
-      const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
-      // the page of lanes 0-3, looked up while the slot is still in use
-      const int npages = tile_pages(j), s = (it.tile_begin + j) * (kKeys / kPageSize) + lane;
-      const char* src = pool;
-      bool bulk = lane < npages;
-      WindowSlots slots = WindowSlots{0, kPageSize, 0};
-      if (bulk) {
-        src = pool + window_page(r, pages, it.pages, s) * a.page_stride;
-        if (is_v) {
-          slots = window_slots(it.pages, s);
-          bulk = slots.whole();
-        }
-      }
+    for (int j = begun ? ahead : 0; j < T && ok; ++j) {
+      const unsigned free_bar = smem_u32(is_v ? &sy->v_free[j % stages] : &sy->k_free[j % stages]);
       ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
-      if (!ok) break;
-      const unsigned dst = ring + b * kKvTileBytes;
-      const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
-      if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
-      const unsigned pieces = ~bulks & ((1u << npages) - 1u);
-      if (pieces != 0) {
-        for (int p = 0; p < npages; ++p) {
-          if (!((pieces >> p) & 1u)) continue;
-          const char* const from =
-              reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), p));
-          WindowSlots sl;
-          sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
-          sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
-          sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
-          // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
-#pragma unroll
-          for (int i = 0; i < kPageBytes / 512; ++i) {
-            const unsigned at = (unsigned)(i * 512 + lane * 16);
-            cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
-          }
-        }
-        cp_async_commit();
-        cp_async_wait<0>();
-        fence_proxy_async();
-      }
-      // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
-      if (lane == 0) {
-        mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
-        armed[b] = j;
-      } else {
-        mbar_arrive(full);
-      }
+      if (ok) load_tile(j);
     }
     cp_async_wait<0>();
     // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
+    if ((!ok || *abort_flag) && lane == 0) {
       for (int b = 0; b < stages; ++b)
         if (armed[b] >= 0) {
           const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);

@@ -10,6 +10,7 @@
 #pragma once
 #include "evict.cuh"
 #include "rope.cuh"
+#include "window.cuh"
 
 namespace bicache {
 
@@ -18,7 +19,7 @@ namespace bicache {
 struct TokenRun {
   long long row;                // first row in the tensors
   int start;                    // first token of the run in the row space
-  int n;                        // rows; cleared slots follow them in the row space
+  int n;                        // rows; in the row space one entry for the cleared slots may follow them
   int token;                    // first token in the prefix
   int clear;                    // the first cleared slot, as a token of the prefix
   int page_word;                // page list from the page of `token` on
@@ -40,29 +41,17 @@ struct TokenArgs {
   int num_runs, tokens;         // runs in the list, tokens of the row space
 };
 
-// The run that token `t` of the row space belongs to: the last that starts at or before it.
-__device__ __forceinline__ const TokenRun& token_run(const int* list, int num_runs, int t) {
-  const TokenRun* const runs = reinterpret_cast<const TokenRun*>(list);
-  int lo = 0;
-  for (int hi = num_runs; hi - lo > 1;) {
-    const int mid = (lo + hi) >> 1;
-    if (runs[mid].start <= t) lo = mid;
-    else hi = mid;
-  }
-  return runs[lo];
-}
-
 // Where a token of the row space lies.
 struct TokenPlace {
-  long long row;                // in the tensors; -1: a slot to clear
+  long long row;                // in the tensors; -1: the slots from `slot` on are cleared
   long long page;               // bytes from the layer's pool to its page
   long long at;                 // what stands for the row in rope_position: the row, or the token
   int slot;
 };
 __device__ __forceinline__ TokenPlace token_place(const TokenArgs& g, const int* list, bool by_token, int t) {
-  const TokenRun& r = token_run(list, g.num_runs, t);
+  const TokenRun& r = last_start<TokenRun>(list, g.num_runs, g.tokens, t, [](const TokenRun& x) { return x.start; });
   const int i = t - r.start;
-  const int token = i < r.n ? r.token + i : r.clear + (i - r.n);
+  const int token = i < r.n ? r.token + i : r.clear;
   TokenPlace p;
   p.row = i < r.n ? r.row + i : -1;
   p.page = list[r.page_word + token / kPageSize - r.token / kPageSize] * g.page_stride;
@@ -166,9 +155,11 @@ append_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ TokenA
       } else {
         char* const to = (which == 1 ? g.pool_k : g.pool_v) + place[i].page + (long long)h * g.page_bytes;
         const bool swz = g.swizzled != 0;
-        *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, place[i].slot, chunk, g.head_bytes)) = x[i];
-        if (!kInterleaved && turns)
-          *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, place[i].slot, chunk + turned, g.head_bytes)) = y[i];
+        for (int s = place[i].slot, end = place[i].row >= 0 ? s + 1 : kPageSize; s < end; ++s) {
+          *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, s, chunk, g.head_bytes)) = x[i];
+          if (!kInterleaved && turns)
+            *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, s, chunk + turned, g.head_bytes)) = y[i];
+        }
       }
     }
   }
@@ -219,9 +210,11 @@ append_elements_kernel(const __grid_constant__ A a, const __grid_constant__ Toke
         if (turns) *reinterpret_cast<T*>(out + d1 * kEsize) = x1;
       } else {
         char* const out = (which == 1 ? g.pool_k : g.pool_v) + pl.page + (long long)h * g.page_bytes;
-        auto at = [&](int d) { return out + page_chunk_offset(g.swizzled != 0, pl.slot, d / kPer, g.head_bytes) + d % kPer * kEsize; };
-        *reinterpret_cast<T*>(at(d0)) = x0;
-        if (turns) *reinterpret_cast<T*>(at(d1)) = x1;
+        for (int s = pl.slot, end = data ? s + 1 : kPageSize; s < end; ++s) {
+          auto at = [&](int d) { return out + page_chunk_offset(g.swizzled != 0, s, d / kPer, g.head_bytes) + d % kPer * kEsize; };
+          *reinterpret_cast<T*>(at(d0)) = x0;
+          if (turns) *reinterpret_cast<T*>(at(d1)) = x1;
+        }
       }
     }
   }

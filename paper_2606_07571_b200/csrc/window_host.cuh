@@ -52,14 +52,17 @@ constexpr int kTokenWords = 7552;
 using TokenLengths = std::integer_sequence<int, 224, 2432, kTokenWords>;
 static_assert(sizeof(RopeAxes) + sizeof(TokenArgs) + 64 + 4 * kTokenWords <= 32764, "launch parameters");
 
-// Checks of a batch of (prefix, tokens, rows) triples; *rows_end receives the end of the last row.
+// Checks of a batch of (prefix, tokens, rows) triples; *rows_end receives the end of the last row, *entries the prefixes.
 int check_tokens(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id, const int32_t* token_off,
-                 const int64_t* row_off, const int32_t* seqlen, bool write, int64_t* rows_end) {
+                 const int64_t* row_off, const int32_t* seqlen, bool write, int64_t* rows_end,
+                 std::vector<const PrefixEntry*>* entries) {
   if (layer < 0 || layer >= ctx->cfg.num_layers) return fail(ctx, BICACHE_ERR_INVALID, "layer out of range");
   if (R < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative request count");
   if (R > 0 && (!prefix_id || !token_off || !row_off || !seqlen)) return fail(ctx, BICACHE_ERR_INVALID, "null metadata array");
   struct Span { int32_t id, begin, end; };
   std::vector<Span> spans;
+  spans.reserve(write ? std::max(R, 0) : 0);
+  entries->reserve(std::max(R, 0));
   int64_t total = 0;
   *rows_end = 0;
   for (int i = 0; i < R; ++i) {
@@ -68,18 +71,18 @@ int check_tokens(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     auto found = ctx->by_id.find(prefix_id[i]);
     if (found == ctx->by_id.end()) return fail(ctx, BICACHE_ERR_NOTFOUND, "unknown or evicted prefix id");
     const PrefixEntry& e = *found->second;
+    entries->push_back(&e);
     if (e.first_layer > layer) return fail(ctx, BICACHE_ERR_INVALID, "the prefix owns no pages in this layer");
     if (seqlen[i] > e.m || token_off[i] > e.m - seqlen[i])
       return fail(ctx, BICACHE_ERR_INVALID, "tokens past the end of the prefix");
     if (seqlen[i] == 0) continue;
-    total += seqlen[i] + kPageSize;
+    total += seqlen[i] + 1LL;
     *rows_end = std::max(*rows_end, row_off[i] + seqlen[i]);
     if (write) spans.push_back(Span{prefix_id[i], token_off[i], token_off[i] + seqlen[i]});
   }
   if (total > 0x7fffffffLL) return fail(ctx, BICACHE_ERR_INVALID, "batch too large");
-  std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) {
-    return x.id != y.id ? x.id < y.id : x.begin < y.begin;
-  });
+  auto before = [](const Span& x, const Span& y) { return x.id != y.id ? x.id < y.id : x.begin < y.begin; };
+  if (!std::is_sorted(spans.begin(), spans.end(), before)) std::sort(spans.begin(), spans.end(), before);
   for (size_t i = 1; i < spans.size(); ++i)
     if (spans[i].id == spans[i - 1].id && spans[i].begin < spans[i - 1].end)
       return fail(ctx, BICACHE_ERR_INVALID, "a token is written twice");
@@ -89,7 +92,7 @@ int check_tokens(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
 // The launches of one call: runs are added until the parameter list is full.  launch(list, runs, tokens) is made for
 // every full list and for the rest.
 template <typename F>
-int token_launches(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id, const int32_t* token_off,
+int token_launches(int32_t layer, const std::vector<const PrefixEntry*>& entries, const int32_t* token_off,
                    const int64_t* row_off, const int32_t* seqlen, bool write, F&& launch) {
   alignas(8) int list[kTokenWords];
   std::vector<TokenRun> runs;
@@ -107,8 +110,10 @@ int token_launches(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32
     tokens = 0;
     return st;
   };
-  for (int i = 0; i < R; ++i) {
-    const PrefixEntry& e = *ctx->by_id.at(prefix_id[i]);
+  runs.reserve(entries.size());
+  pages.reserve(2 * entries.size());
+  for (size_t i = 0; i < entries.size(); ++i) {
+    const PrefixEntry& e = *entries[i];
     const std::vector<int32_t>& own = pages_of(e, layer);
     for (int done = 0; done < seqlen[i];) {
       const int token = token_off[i] + done, page = token / kPageSize;
@@ -131,7 +136,7 @@ int token_launches(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32
       runs.push_back(r);
       done += r.n;
       const bool ends = write && page + take == (int)own.size();     // the prefix's last page is among them
-      tokens += r.n + (ends ? (int)own.size() * kPageSize - e.m : 0);
+      tokens += r.n + (ends && e.m % kPageSize ? 1 : 0);
     }
   }
   return flush();
@@ -159,7 +164,8 @@ int append_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   if (!ctx) return BICACHE_ERR_INVALID;
   const bicache_config& cfg = ctx->cfg;
   int64_t rows_end = 0;
-  int st = check_tokens(ctx, layer, R, prefix_id, token_off, row_off, seqlen, true, &rows_end);
+  std::vector<const PrefixEntry*> entries;
+  int st = check_tokens(ctx, layer, R, prefix_id, token_off, row_off, seqlen, true, &rows_end, &entries);
   if (st != BICACHE_OK) return st;
   const int64_t kv_least = (int64_t)cfg.num_kv_heads * cfg.head_dim, q_least = (int64_t)cfg.num_q_heads * cfg.head_dim;
   if (rows_end > 0) {
@@ -198,7 +204,7 @@ int append_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   const bool interleaved = rot && rot->interleaved;
   const bool axes = rot && rot->num_axes > 1;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  return token_launches(ctx, layer, R, prefix_id, token_off, row_off, seqlen, true, [&](const int* list, int words, int runs, int tokens) {
+  return token_launches(layer, entries, token_off, row_off, seqlen, true, [&](const int* list, int words, int runs, int tokens) {
     g.num_runs = runs;
     g.tokens = tokens;
     cudaError_t e = cudaSuccess;
@@ -222,7 +228,8 @@ int read_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* 
   if (!ctx) return BICACHE_ERR_INVALID;
   const bicache_config& cfg = ctx->cfg;
   int64_t rows_end = 0;
-  const int st = check_tokens(ctx, layer, R, prefix_id, token_off, row_off, seqlen, false, &rows_end);
+  std::vector<const PrefixEntry*> entries;
+  const int st = check_tokens(ctx, layer, R, prefix_id, token_off, row_off, seqlen, false, &rows_end, &entries);
   if (st != BICACHE_OK) return st;
   if (rows_end > 0) {
     if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || k_out == v_out)
@@ -237,7 +244,7 @@ int read_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* 
   g.k_out = static_cast<char*>(k_out);
   g.v_out = static_cast<char*>(v_out);
   g.kv_stride = kv_row_stride * ctx->esize;
-  return token_launches(ctx, layer, R, prefix_id, token_off, row_off, seqlen, false, [&](const int* list, int words, int runs, int tokens) {
+  return token_launches(layer, entries, token_off, row_off, seqlen, false, [&](const int* list, int words, int runs, int tokens) {
     g.num_runs = runs;
     g.tokens = tokens;
     cudaError_t e = cudaSuccess;
@@ -434,7 +441,7 @@ class WindowLaunches {
       };
       if (ctx_->cfg.dtype == BICACHE_F32) typed(0.f);
       else typed(__nv_bfloat16());
-    }, WindowSimtLengths());
+    }, WindowLengths());
     return e;
   }
 
