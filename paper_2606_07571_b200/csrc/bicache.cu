@@ -28,7 +28,6 @@
 #include "rope.cuh"
 #include "tc_weights.cuh"
 #include "token_cache.cuh"
-#include "window.cuh"
 #include "tc_window.cuh"
 
 using namespace bicache;

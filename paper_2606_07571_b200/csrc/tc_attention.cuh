@@ -29,6 +29,7 @@
 #include <cuda_bf16.h>
 #include "common.cuh"
 #include "simt_kernels.cuh"
+#include "window.cuh"
 
 namespace bicache {
 
@@ -72,6 +73,11 @@ struct ItemInfo {
   int all_tiles;                         // ceil(m / 128) + sum over the segments of ceil(n / 128)
   SegInfo seg[kMaxSegs];
 };
+// The same of windowed attention (see window.cuh): one segment, the key tiles cut from the item's page sequence.
+struct WindowInfo {
+  WindowPages pages;
+  int req, pos, len;                     // record of the request, position of its first row, cached tokens
+};
 struct alignas(8) Barriers {
   unsigned long long info_full[2];       // item record (double-buffered by item parity) is written
   unsigned long long info_free[2];       // every role is done with the record
@@ -95,6 +101,7 @@ struct alignas(8) Barriers {
   unsigned tmem_base;
   int dead;                              // the context's status word was already set when the CTA started
   ItemInfo info[2];
+  WindowInfo window[2];
 };
 constexpr int kInfoReaders = 8 + 1 + 2;  // arrivals on info_free: softmax warps, the MMA warp, the two load warps
 constexpr int kStageBytes = 8 * 4096;
@@ -582,7 +589,32 @@ __device__ __forceinline__ int seg_of_row(const ItemInfo* inf, int nseg, int p) 
     if (p >= inf->seg[i].begin && p < inf->seg[i].begin + inf->seg[i].count) k = i;
   return k;
 }
-
+// The pages `pieces` of a tile of values (bit p: page p, whose source and slots lane p holds) in 16-byte pieces, the slots
+// that no row sees zeroed.  For a converged warp; the pieces have landed when it returns.
+__device__ __forceinline__ void gather_window_pages(unsigned dst, const char* src, const WindowSlots& slots, unsigned pieces,
+                                                    int lane) {
+#pragma unroll 1
+  for (unsigned left = pieces; left != 0; left &= left - 1) {
+    const int p = __ffs(left) - 1;
+    const char* const from =
+        reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), p));
+    WindowSlots sl;
+    sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
+    sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
+    sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
+    // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
+#pragma unroll
+    for (int i = 0; i < kPageBytes / 512; ++i) {
+      const unsigned at = (unsigned)(i * 512 + lane * 16);
+      cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
+    }
+  }
+  cp_async_commit();
+  cp_async_wait<0>();
+  fence_proxy_async();
+}
+// the first x of 32 bits
+__device__ __forceinline__ unsigned low_bits(int x) { return x >= 32 ? ~0u : x <= 0 ? 0u : (1u << x) - 1u; }
 
 }  // namespace tc
 
@@ -590,13 +622,25 @@ __device__ __forceinline__ int seg_of_row(const ItemInfo* inf, int nseg, int p) 
 // kShared: the schedule holds row tiles with several segments (requests of a prefix group sharing a
 // tile); that instantiation takes its per-tile key counts from the K loader's notes.  The plain one keeps
 // them in registers and carries none of the shared-tile code in its loops.
-template <bool kShared>
+// kWindowed: bicache_attend_window, whose batch travels in the parameters (`win`).  Its items read cached tokens alone: the
+// pages of an item's sequence take the place of a prefix's, a row knows the columns it sees as an interval and a number
+// of first columns, and a tile that some row of a warp does not see in full is masked by bits.
+enum { kPlain = 0, kShared = 1, kWindowed = 2 };
+struct NoWindow {};
+template <int kWords>
+struct WindowBatch {
+  WindowArgs a;
+  ParamList<kWords> list;
+};
+template <int kMode, typename Window>
 __global__ void __launch_bounds__(tc::kThreads, 1)
 tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
                     const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
-                    const __grid_constant__ CUtensorMap tm_q8, int q_tma, int o_tma, long long wait_cycles) {
+                    const __grid_constant__ CUtensorMap tm_q8, int q_tma, int o_tma, long long wait_cycles,
+                    const __grid_constant__ Window win) {
   using namespace tc;
+  constexpr bool kShared = kMode == bicache::kShared, kWindow = kMode == kWindowed;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -679,6 +723,11 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       // reference maximum is finite by then); with one segment padding rows just run along.
       const int vseg = seg_of_row(inf, g.nseg, X * 128 + gt);
       float m_ref = -INFINITY, l_sum = 0.f;
+      WindowColumns col = WindowColumns{0, 0x7fffffff, 0};         // what the row sees; a padding row runs along unmasked
+      if constexpr (kWindow) {
+        const WindowInfo& wi = bars->window[n_it & 1];
+        if (vseg >= 0) col = window_columns(win.a, wi.pages, wi.len, wi.pos + (inf->seg[0].prow0 + X * 128 + gt) / G);
+      }
       for (int j = 0; j < T && active; ++j) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->s_full[X]), c_tile & 1, abort_flag));
         if (!ok) break;
@@ -689,9 +738,18 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         // other rows the reference maximum used below is +inf, which makes every exponential exactly 0
         // (and the row's own maximum -inf, so it never asks for a rescale): no branch, no code of its
         // own in this loop.
-        int cnt;
+        int cnt = kTileKeys;
         bool mine = true;
-        if (!kShared) {
+        unsigned see[4] = {0u, 0u, 0u, 0u};                    // window: the columns of the tile that the row sees
+        bool part = false;                                     // ... if some row of the warp does not see them all
+        if constexpr (kWindow) {
+          mine = vseg >= 0;
+          const int begin = col.begin - j * kTileKeys, end = col.end - j * kTileKeys, sink = col.sink - j * kTileKeys;
+          part = __any_sync(0xffffffffu, begin > 0 || end < kTileKeys);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            see[c] = (low_bits(end - 32 * c) & ~low_bits(begin - 32 * c)) | low_bits(sink - 32 * c);
+        } else if (!kShared) {
           bool dense_unused;
           cnt = tile_keys_single(g, j, dense_unused);
         } else {
@@ -712,7 +770,13 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         unsigned long long acc_a = pack2(0.f, 0.f), acc_b = pack2(0.f, 0.f);
         bool stored = false;                                   // P already stored and signalled
         // A ragged tile: columns past the last key become -inf (their exponentials are exactly 0).
-        if (cnt < kTileKeys) {
+        if constexpr (kWindow) {
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 128; ++i)
+              if (!((see[i >> 5] >> (i & 31)) & 1u)) r[i] = 0xff800000u;
+          }
+        } else if (cnt < kTileKeys) {
 #pragma unroll
           for (int i = 0; i < 128; ++i)
             if (i >= cnt) r[i] = 0xff800000u;
@@ -740,7 +804,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           // slower again: the first part then starts too late).
           // If the row maximum turns out to exceed the reference by more than 2^8 (rare: checked per
           // warp before anything is handed over), the tile is redone below with the new reference.
-          const float neg_m_eff = mine ? -m_ref : -INFINITY;
+          // (a row that has seen no key yet has no reference: 0, and every exponential is that of -inf)
+          const float neg_m_eff = !mine ? -INFINITY : kWindow && m_ref == -INFINITY ? 0.f : -m_ref;
           const unsigned long long neg_m2 = pack2(neg_m_eff, neg_m_eff);
           float mx0 = -INFINITY, mx1 = -INFINITY;
           // the first 64 exponentials, with the maximum over all 128 scores computed alongside
@@ -830,7 +895,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
               m_ref = mx;
             }
             unsigned s4[32];
-            const float neg_m = mine ? -m_ref : -INFINITY;
+            const float neg_m = !mine ? -INFINITY : kWindow && m_ref == -INFINITY ? 0.f : -m_ref;
+            auto seen = [&](int i) { return kWindow ? ((see[i >> 5] >> (i & 31)) & 1u) != 0 : i < cnt; };
             float ps = 0.f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -839,8 +905,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 // (the scores come from TMEM again: columns past the last key of a ragged tile are masked here)
-                const float p0 = c * 32 + 2 * i < cnt ? ex2(fmaf(__uint_as_float(s4[2 * i]), sl2, neg_m)) : 0.f;
-                const float p1 = c * 32 + 2 * i + 1 < cnt ? ex2(fmaf(__uint_as_float(s4[2 * i + 1]), sl2, neg_m)) : 0.f;
+                const float p0 = seen(c * 32 + 2 * i) ? ex2(fmaf(__uint_as_float(s4[2 * i]), sl2, neg_m)) : 0.f;
+                const float p1 = seen(c * 32 + 2 * i + 1) ? ex2(fmaf(__uint_as_float(s4[2 * i + 1]), sl2, neg_m)) : 0.f;
                 ps += p0 + p1;
                 r[c * 16 + i] = pack_bf16(p0, p1);
               }
@@ -901,8 +967,9 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
 #pragma unroll
           for (int i = 0; i < 128; ++i) o[i] = 0u;
         }
-        const float inv = T > 0 ? 1.f / l_sum : 0.f;
-        const float lse = T > 0 ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
+        const bool some = T > 0 && !(kWindow && l_sum == 0.f);     // the row has seen a key
+        const float inv = some ? 1.f / l_sum : 0.f;
+        const float lse = some ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -INFINITY;
         if (s.num_splits > 1) {
           // key-split call: normalised fp32 partial and its lse, merged by a second kernel
           if (row_valid) {
@@ -915,7 +982,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
                               __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
             t.part_lse[pr] = lse;
           }
-        } else if (T > 0) {
+        } else if (kWindow || T > 0) {
           // Each thread holds one output row.  The warp stages its 32 rows, one 64-dim half at a
           // time (128 bytes per row, 16-byte chunks XOR-placed by row: the 128-byte swizzle), and
           // one TMA store writes the half out; a warp whose rows are not all valid, or a head
@@ -984,6 +1051,36 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
     // The record of item `idx` (the whole warp works on it; lane k fills segment k).
     auto write_info = [&](ItemInfo* dst, int idx) {
       if (idx < s.num_items) {
+        if constexpr (kWindow) {
+          if (lane == 0) {
+            const WindowReq& rq = window_req(win.a, win.list.w, idx);
+            const WindowItem it = window_item<kTileKeys>(win.a, rq, idx, kTileRows);
+            WindowInfo& wi = bars->window[dst - bars->info];
+            wi.pages = it.pages;
+            wi.req = (int)(&rq - reinterpret_cast<const WindowReq*>(win.list.w));
+            wi.pos = rq.pos;
+            wi.len = rq.len;
+            SegInfo si;
+            si.row_off = rq.row;
+            si.n = rq.n;
+            si.prow0 = it.row0;
+            si.begin = 0;
+            si.count = min(kTileRows, rq.n * G - it.row0);
+            si.tok_off = 0;
+            si.tile_end = it.tile_end;
+            dst->seg[0] = si;
+            dst->kv_head = it.hk;
+            dst->split = 0;
+            dst->m = it.pages.count * kPageSize;
+            dst->page_off = 0;
+            dst->nseg = 1;
+            dst->nrows = si.count;
+            dst->all_tiles = it.tile_end;
+            dst->valid = 1;
+          }
+          __syncwarp();
+          return;
+        }
         const WorkItem wi = s.items[idx];
         if (s.tiles != nullptr) {
           const RowTile* tl = s.tiles + wi.req;
@@ -1168,6 +1265,46 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       if (!g.valid) break;
       const int kv_head = inf->kv_head;
       const int* pages = s.pages + inf->page_off;
+      if constexpr (kWindow) {
+        // Key tiles of the item's page sequence, 8 pages each.  A page of values in which no row of the item sees some slots
+        // is gathered in 16-byte pieces with these zeroed (they may hold anything, and 0 times a NaN is a NaN); all others
+        // come by one bulk copy.
+        const WindowInfo& wi = bars->window[n_it & 1];
+        const WindowPages wp = wi.pages;
+        const WindowReq& rq = reinterpret_cast<const WindowReq*>(win.list.w)[wi.req];
+        const int* const list = window_page_list(win.a, rq, win.list.w);
+        const char* const pool_base = (is_v ? win.a.pool_v : win.a.pool_k) + (long long)kv_head * win.a.page_bytes;
+        for (int j = 0; j < g.T; ++j) {
+          const int u = U + 2 * j + is_v;
+          const int slot = u % kRing;
+          const unsigned dst = ring_smem + slot * kTileBytes;
+          const unsigned full = smem_u32(&bars->full[slot]);
+          const int npages = min(8, wp.count - 8 * j);
+          const char* src = nullptr;
+          bool bulk = lane < npages;
+          WindowSlots sl = WindowSlots{0, kPageSize, 0};
+          if (bulk) {
+            src = pool_base + window_page(rq, list, wp, 8 * j + lane) * win.a.page_stride;
+            if (is_v) {
+              sl = window_slots(wp, 8 * j + lane);
+              bulk = sl.whole();
+            }
+          }
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->free_[slot]), ((u / kRing) & 1) ^ 1, abort_flag));
+          if (!ok) break;
+          const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
+          if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
+          const unsigned pieces = ~bulks & ((1u << npages) - 1u);
+          if (pieces != 0) gather_window_pages(dst, src, sl, pieces, lane);
+          // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
+          if (lane == 0) {
+            mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
+            armed[slot] = u;
+          } else {
+            mbar_arrive(full);
+          }
+        }
+      } else
       for (int j = 0; j < g.T; ++j) {
         const int u = U + 2 * j + is_v;
         const int slot = u % kRing;
@@ -1509,10 +1646,20 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
   }
 }
 
+// Lists of the windowed form: with the tensor maps beside the longest, a launch stays below the 32,764 bytes of its parameters.
+constexpr int kWindowTileWords = 7424;
+using WindowTileLengths = std::integer_sequence<int, 1216, kWindowTileWords>;
+static_assert(sizeof(ScheduleView) + sizeof(PoolView) + sizeof(TensorArgs) + 6 * sizeof(CUtensorMap) + 64 +
+                  sizeof(WindowBatch<kWindowTileWords>) <= 32764, "launch parameters");
+
 inline cudaError_t configure_tc_attention() {
   cudaFuncAttributes attr;
-  for (int shared = 0; shared < 2; ++shared) {
-    const void* fn = shared ? (const void*)tc_attention_kernel<true> : (const void*)tc_attention_kernel<false>;
+  const void* fns[4] = {(const void*)tc_attention_kernel<kPlain, NoWindow>, (const void*)tc_attention_kernel<kShared, NoWindow>};
+  int num = 2;
+  each_param_length([&](auto words) {
+    fns[num++] = (const void*)tc_attention_kernel<kWindowed, WindowBatch<decltype(words)::value>>;
+  }, WindowTileLengths());
+  for (const void* fn : fns) {
     cudaError_t e = cudaFuncGetAttributes(&attr, fn);
     if (e != cudaSuccess) return e;
     // the register pool the kernel redistributes is the launch allocation of the CTA
@@ -1542,13 +1689,27 @@ inline cudaError_t launch_tc_attention(const ScheduleView& s, const PoolView& po
                                        cudaStream_t stream) {
   const int grid = s.num_items < num_sms ? s.num_items : num_sms;
   if (s.tiles != nullptr && s.shared_tiles)
-    tc_attention_kernel<true><<<grid, tc::kThreads, tc::kSmemBytes, stream>>>(
+    tc_attention_kernel<kShared, NoWindow><<<grid, tc::kThreads, tc::kSmemBytes, stream>>>(
         s, pool, t, status, maps.q, maps.k, maps.v, maps.o, maps.q8, maps.q_tma, maps.o_tma,
-        wait_cycles > 0 ? wait_cycles : tc::kWaitCycles);
+        wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, NoWindow());
   else
-    tc_attention_kernel<false><<<grid, tc::kThreads, tc::kSmemBytes, stream>>>(
+    tc_attention_kernel<kPlain, NoWindow><<<grid, tc::kThreads, tc::kSmemBytes, stream>>>(
         s, pool, t, status, maps.q, maps.k, maps.v, maps.o, maps.q8, maps.q_tma, maps.o_tma,
-        wait_cycles > 0 ? wait_cycles : tc::kWaitCycles);
+        wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, NoWindow());
+  return cudaGetLastError();
+}
+
+// Windowed attention of the batch in `win` (whole items only: no ranges of keys).
+template <int kWords>
+inline cudaError_t launch_tc_window_tiles(const WindowBatch<kWords>& win, const TensorArgs& t, int* status, int num_sms,
+                                          const TcTensorMaps& maps, long long wait_cycles, cudaStream_t stream) {
+  ScheduleView s = ScheduleView();
+  s.num_items = win.a.num_items;
+  s.num_splits = 1;
+  const int grid = s.num_items < num_sms ? s.num_items : num_sms;
+  tc_attention_kernel<kWindowed, WindowBatch<kWords>><<<grid, tc::kThreads, tc::kSmemBytes, stream>>>(
+      s, PoolView(), t, status, maps.q, maps.q, maps.q, maps.o, maps.q, maps.q_tma, maps.o_tma,
+      wait_cycles > 0 ? wait_cycles : tc::kWaitCycles, win);
   return cudaGetLastError();
 }
 

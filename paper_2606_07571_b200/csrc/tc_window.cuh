@@ -19,22 +19,11 @@
 #include "window.cuh"
 
 namespace bicache {
-namespace win {
-
-using namespace dec;
-
-// the first x of 64 bits
-__device__ __forceinline__ unsigned long long low_bits(int x) {
-  return x >= 64 ? ~0ull : x <= 0 ? 0ull : (1ull << x) - 1ull;
-}
-
-}  // namespace win
-
 template <int kWords>
 __global__ void __launch_bounds__(dec::kDecThreads, 2)
 tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wait_cycles,
                  const __grid_constant__ ParamList<kWords> params) {
-  using namespace win;
+  using namespace dec;
   // No room for alignment slack with two CTAs per SM: the kernel has no static shared memory, the
   // dynamic window starts 1024-byte aligned (the swizzled tiles need that), and a CTA that finds
   // otherwise reports an error instead of computing.
@@ -81,26 +70,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
     if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
     const unsigned pieces = ~bulks & ((1u << npages) - 1u);
-    if (pieces != 0) {
-      for (int p = 0; p < npages; ++p) {
-        if (!((pieces >> p) & 1u)) continue;
-        const char* const from =
-            reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), p));
-        WindowSlots sl;
-        sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
-        sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
-        sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
-        // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
-#pragma unroll
-        for (int i = 0; i < kPageBytes / 512; ++i) {
-          const unsigned at = (unsigned)(i * 512 + lane * 16);
-          cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
-        }
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-      fence_proxy_async();
-    }
+    if (pieces != 0) gather_window_pages(dst, src, slots, pieces, lane);
     // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
     if (lane == 0) {
       mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
@@ -194,8 +164,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
         tmem_ld32(tmem + b * 64 + 32 + lane_base, s + 32);
         tmem_wait_ld();
         if (__any_sync(0xffffffffu, begin > 0 || end < kKeys)) {
-          const unsigned long long seen = (low_bits(end) & ~low_bits(begin)) | low_bits(sink);
-          const unsigned lo = (unsigned)seen, hi = (unsigned)(seen >> 32);
+          const unsigned lo = (low_bits(end) & ~low_bits(begin)) | low_bits(sink);
+          const unsigned hi = (low_bits(end - 32) & ~low_bits(begin - 32)) | low_bits(sink - 32);
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             if (!((lo >> i) & 1u)) s[i] = 0xff800000u;             // -inf

@@ -268,6 +268,8 @@ struct WindowForm {
   int slots;                    // work items that run at a time
   int item_cost;                // start and end of a work item
   int join_cost;                // the joining kernel
+  int max_splits;               // ranges of keys
+  int list_words;               // what a launch's list holds
 };
 
 // The launches of one call and one kernel form: requests are added until the parameter list is full.
@@ -298,8 +300,8 @@ class WindowLaunches {
       p.sum_tiles += tiles;
     }
     const int words = kWindowReqWords + w.count;
-    const bool alone = words > kParamWords;               // its page list goes through the workspace
-    if (alone || words_ + words > kParamWords) {
+    const bool alone = words > form_.list_words;          // its page list goes through the workspace
+    if (alone || words_ + words > form_.list_words) {
       const int st = flush();
       if (st != BICACHE_OK) return st;
     }
@@ -315,7 +317,7 @@ class WindowLaunches {
     if (pending_.empty()) return BICACHE_OK;
     WindowArgs a = base_;
     cudaError_t e = cudaSuccess;
-    if (words_ > kParamWords) {
+    if (words_ > form_.list_words) {
       a.staged_pages = ctx_->d_put_pages;
       for (size_t at = 0; at < pages_.size() && e == cudaSuccess; at += kParamWords) {
         const int count = (int)std::min<size_t>(kParamWords, pages_.size() - at);
@@ -388,8 +390,8 @@ class WindowLaunches {
     int max_tiles = 0;          // key tiles of a row tile, at most
     long long sum_tiles = 0;    // of all row tiles
   };
-  static int splits_of(const Pending& p, int tps) {
-    return std::min(kMaxWindowSplits, std::max(1, (p.max_tiles + tps - 1) / tps));
+  int splits_of(const Pending& p, int tps) const {
+    return std::min(form_.max_splits, std::max(1, (p.max_tiles + tps - 1) / tps));
   }
   // How many key tiles an item covers at most.  Counted in key tiles: what a slot has to do on the average, and half
   // an item at the end, or the longest item if there is no more than one to a slot.
@@ -398,7 +400,7 @@ class WindowLaunches {
     for (const Pending& p : pending_) max_tiles = std::max(max_tiles, p.max_tiles);
     int best_tps = max_tiles;
     double best = 1e300;
-    for (int s = 1, before = 0; s <= kMaxWindowSplits && s <= max_tiles; ++s) {
+    for (int s = 1, before = 0; s <= form_.max_splits && s <= max_tiles; ++s) {
       const int tps = (max_tiles + s - 1) / s;
       if (tps == before) continue;
       before = tps;
@@ -474,7 +476,7 @@ class WindowSimtLaunches : public WindowLaunches {
  protected:
   static WindowForm form_of(const bicache_ctx* ctx, int rows) {
     const int blocks = std::max(1, (int)(227 * 1024 / (window_simt_smem(rows, ctx->cfg.head_dim) + 1024)));
-    return WindowForm{rows, kWinKeys, std::min(blocks, rows == 16 ? 4 : 2) * ctx->sm_count, 2, 2};
+    return WindowForm{rows, kWinKeys, std::min(blocks, rows == 16 ? 4 : 2) * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
   }
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
     const size_t smem = window_simt_smem(form_.tile_rows, a.D);
@@ -492,7 +494,7 @@ class WindowSimtLaunches : public WindowLaunches {
 class WindowTensorLaunches : public WindowLaunches {
  public:
   WindowTensorLaunches(bicache_ctx* ctx, const WindowArgs& args, cudaStream_t stream)
-      : WindowLaunches(ctx, args, WindowForm{128, dec::kKeys, 2 * ctx->sm_count, 4, 4}, stream) {}
+      : WindowLaunches(ctx, args, WindowForm{128, dec::kKeys, 2 * ctx->sm_count, 4, 4, kMaxWindowSplits, kParamWords}, stream) {}
 
  protected:
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
@@ -503,6 +505,36 @@ class WindowTensorLaunches : public WindowLaunches {
     return e;
   }
   const int* status() const override { return ctx_->d_status; }
+};
+
+// Row tiles of 256: for requests with more rows than one work item of the other form takes.
+class WindowTileLaunches : public WindowLaunches {
+ public:
+  WindowTileLaunches(bicache_ctx* ctx, const WindowArgs& args, const TcTensorMaps& maps, cudaStream_t stream)
+      : WindowLaunches(ctx, args, WindowForm{kTileRows, kTileKeys, ctx->sm_count, 0, 0, 1, kWindowTileWords}, stream), maps_(maps) {}
+
+ protected:
+  cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
+    TensorArgs t = TensorArgs();
+    t.q = a.q;
+    t.out = a.out;
+    t.lse = a.lse;
+    t.q_stride = a.q_stride;
+    t.out_stride = a.out_stride;
+    t.Hq = a.Hq;
+    t.Hkv = a.Hkv;
+    t.D = a.D;
+    t.scale = a.scale;
+    cudaError_t e = cudaSuccess;
+    with_param_list(list, words, [&](const auto& params) {
+      constexpr int kWords = sizeof(params.w) / sizeof(int);
+      e = launch_tc_window_tiles(WindowBatch<kWords>{a, params}, t, ctx_->d_status, ctx_->sm_count, maps_, ctx_->wait_cycles, stream_);
+    }, WindowTileLengths());
+    return e;
+  }
+
+ private:
+  TcTensorMaps maps_;
 };
 
 int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id, const int32_t* cached_len,
@@ -581,9 +613,28 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   };
   // the tensor-core kernel takes the row maximum before scaling, which needs a positive scale
   if (ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && softmax_scale > 0.f) {
-    ctx->last_kernel = BICACHE_KERNEL_KEY_RANGES;
+    // Requests with more than 128 packed rows go through the kernel with row tiles of 256, which shares every key tile
+    // between two tiles of 128 rows, if there are enough of them to fill the SMs; it does not split the keys.
+    long long tiles = 0, rows_total = 0;
+    for (int i = 0; i < R; ++i) {
+      rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
+      if ((long long)seqlen[i] * G > 128) tiles += ((long long)seqlen[i] * G + kTileRows - 1) / kTileRows * cfg.num_kv_heads;
+    }
+    TcTensorMaps maps;
+    std::memset(&maps, 0, sizeof(maps));
+    maps.q_tma = (128 % G == 0) ? 1 : 0;
+    maps.o_tma = (32 % G == 0) ? 1 : 0;
+    const bool by_256 = tiles >= ctx->sm_count && rows_total < 0x7fffffffLL &&              // box coordinates are 32-bit
+                        encode_map(&maps.q, q, rows_total, cfg.num_q_heads, q_row_stride, maps.q_tma ? G : 1, maps.q_tma ? 128 / G : 128) &&
+                        encode_map(&maps.o, out, rows_total, cfg.num_q_heads, out_row_stride, maps.o_tma ? G : 1, maps.o_tma ? 32 / G : 32);
+    ctx->last_kernel = by_256 ? BICACHE_KERNEL_TENSOR : BICACHE_KERNEL_KEY_RANGES;
+    if (by_256) {
+      WindowTileLaunches launches(ctx, a, maps, stream);
+      const int st = run(launches, [&](int n) { return (long long)n * G > 128; });
+      if (st != BICACHE_OK) return st;
+    }
     WindowTensorLaunches launches(ctx, a, stream);
-    return run(launches, [](int) { return true; });
+    return run(launches, [&](int n) { return !by_256 || (long long)n * G <= 128; });
   }
   ctx->last_kernel = BICACHE_KERNEL_SIMT;
   // a row tile of 16 where that holds a request's rows of a KV head, else of 64

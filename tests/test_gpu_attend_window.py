@@ -34,7 +34,7 @@ def randn(shape, seed, dtype, std=1.0):
     return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
 
 
-HEADS = {"gqa7": (7, 1, 128), "gqa4": (8, 2, 128), "gqa28": (28, 4, 128), "mha2": (2, 2, 128), "gqa150": (150, 1, 128),
+HEADS = {"mha32": (32, 32, 128), "gqa32": (32, 8, 128), "gqa7": (7, 1, 128), "gqa4": (8, 2, 128), "gqa28": (28, 4, 128), "mha2": (2, 2, 128), "gqa150": (150, 1, 128),
          "mha4_64": (4, 4, 64), "gqa2_96": (2, 1, 96), "d256": (3, 1, 256), "d32": (2, 2, 32)}
 
 
@@ -133,6 +133,31 @@ def test_prompts(window, heads, dtype):
     Batch(heads, dtype, lens, [(0, 0, 700), (1, 400, 1131), (2, 0, 256), (1, 1600, 130)]).check(*window)
 
 
+@pytest.mark.parametrize("window", [(0, -1, 0), (4, 700, 0), (0, 127, 128), (0, 300, -1), (33, 64, 17), (0, 0, 0), (129, 200, 0)])
+@pytest.mark.parametrize("heads", ["gqa28", "mha32", "gqa32", "gqa150"])
+def test_row_tiles_of_256(window, heads):
+    """Enough rows for the kernel with row tiles of 256: prompts, rows that see nothing, an empty cache, a few rows."""
+    lens = [700, 901, 257, 0]
+    requests = [(0, 0, 700), (1, 400, 501), (2, 0, 256), (1, 1300, 130), (3, 5, 200), (0, 699, 1), (2, 200, 40), (1, 880, 129)]
+    b = Batch(heads, torch.bfloat16, lens, requests, spare=37)
+    out, _ = b.check(*window)
+    assert b.bc.last_attention_kernel() == binding.KERNEL_TENSOR
+    again, _ = b.call(*window)
+    assert torch.equal(out, again)
+
+
+def test_unseen_tokens_and_row_tiles_of_256():
+    m, n, sinks, left = 2600, 1500, 5, 70
+    b = Batch("gqa28", torch.bfloat16, [m], [(0, m - n, n)])
+    want = b.call(sinks, left, 0)
+    assert b.bc.last_attention_kernel() == binding.KERNEL_TENSOR
+    first = m - n - left
+    bad = torch.full((first - sinks, b.hkv, b.d), math.nan, dtype=torch.bfloat16, device="cuda")
+    b.bc.append_tokens(0, [b.ids[0]], [sinks], [0], [first - sinks], bad, -bad * math.inf)
+    got = b.call(sinks, left, 0)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and want[0].isfinite().all()
+
+
 @pytest.mark.parametrize("m", [1023, 4096, 20000])
 @pytest.mark.parametrize("heads,dtype", [("gqa28", torch.bfloat16), ("mha2", torch.bfloat16), ("mha4_64", torch.float32),
                                          ("gqa2_96", torch.float32)])
@@ -178,10 +203,10 @@ def test_a_nan_that_is_seen_spreads(heads, dtype, n):
     assert out[rows][:-1].isfinite().all() and lse[rows][:-1].isfinite().all()
 
 
-@pytest.mark.parametrize("heads,dtype", [("gqa4", torch.bfloat16), ("mha4_64", torch.float32)])
-def test_steep_scores(heads, dtype):
+@pytest.mark.parametrize("heads,dtype,many", [("gqa4", torch.bfloat16, False), ("gqa32", torch.bfloat16, True), ("mha4_64", torch.float32, False)])
+def test_steep_scores(heads, dtype, many):
     """Scores that grow along the keys by far more than the running reference follows at a time."""
-    b = Batch(heads, dtype, [700], [(0, 690, 10), (0, 0, 300)], std=0.1)
+    b = Batch(heads, dtype, [700], [(0, 690, 10), (0, 0, 300)] * (6 if many else 1), std=0.1)
     ramp = torch.linspace(-30, 30, 700, device="cuda")[:, None, None]
     k = (torch.ones((700, b.hkv, b.d), device="cuda") * ramp).to(dtype)
     b.q[...] = 0.25
