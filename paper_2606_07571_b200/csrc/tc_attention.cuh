@@ -77,6 +77,7 @@ struct ItemInfo {
 struct WindowInfo {
   WindowPages pages;
   int req, pos, len;                     // record of the request, position of its first row, cached tokens
+  int start;                             // the tile to begin with
 };
 struct alignas(8) Barriers {
   unsigned long long info_full[2];       // item record (double-buffered by item parity) is written
@@ -724,8 +725,10 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       const int vseg = seg_of_row(inf, g.nseg, X * 128 + gt);
       float m_ref = -INFINITY, l_sum = 0.f;
       WindowColumns col = WindowColumns{0, 0x7fffffff, 0};         // what the row sees; a padding row runs along unmasked
+      int start = 0;
       if constexpr (kWindow) {
         const WindowInfo& wi = bars->window[n_it & 1];
+        start = wi.start;
         if (vseg >= 0) col = window_columns(win.a, wi.pages, wi.len, wi.pos + (inf->seg[0].prow0 + X * 128 + gt) / G);
       }
       for (int j = 0; j < T && active; ++j) {
@@ -744,7 +747,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         bool part = false;                                     // ... if some row of the warp does not see them all
         if constexpr (kWindow) {
           mine = vseg >= 0;
-          const int begin = col.begin - j * kTileKeys, end = col.end - j * kTileKeys, sink = col.sink - j * kTileKeys;
+          const int col0 = window_tile(start, 0, T, j) * kTileKeys;
+          const int begin = col.begin - col0, end = col.end - col0, sink = col.sink - col0;
           part = __any_sync(0xffffffffu, begin > 0 || end < kTileKeys);
 #pragma unroll
           for (int c = 0; c < 4; ++c)
@@ -1060,6 +1064,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             wi.req = (int)(&rq - reinterpret_cast<const WindowReq*>(win.list.w));
             wi.pos = rq.pos;
             wi.len = rq.len;
+            wi.start = it.start;
             SegInfo si;
             si.row_off = rq.row;
             si.n = rq.n;
@@ -1279,14 +1284,14 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           const int slot = u % kRing;
           const unsigned dst = ring_smem + slot * kTileBytes;
           const unsigned full = smem_u32(&bars->full[slot]);
-          const int npages = min(8, wp.count - 8 * j);
+          const int page0 = 8 * window_tile(wi.start, 0, g.T, j), npages = min(8, wp.count - page0);
           const char* src = nullptr;
           bool bulk = lane < npages;
           WindowSlots sl = WindowSlots{0, kPageSize, 0};
           if (bulk) {
-            src = pool_base + window_page(rq, list, wp, 8 * j + lane) * win.a.page_stride;
+            src = pool_base + window_page(rq, list, wp, page0 + lane) * win.a.page_stride;
             if (is_v) {
-              sl = window_slots(wp, 8 * j + lane);
+              sl = window_slots(wp, page0 + lane);
               bulk = sl.whole();
             }
           }
@@ -1455,6 +1460,12 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       auto read_meta = [&](unsigned uu) -> int {
         return __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&bars->tile_meta[(uu >> 1) & 7]), 0);
       };
+      // keys of the j-th key tile of an item, whose tiles begin with `start` under a window
+      int start = 0, start_next = 0;
+      auto tile_keys = [&](const Geo& g, int first, int j, bool& dense) {
+        return tile_keys_single(g, kWindow ? window_tile(first, 0, g.T, j) : j, dense);
+      };
+      if constexpr (kWindow) start = __shfl_sync(0xffffffffu, bars->window[0].start, 0);
       bool dn = false;           // layout of the current key tile
       int ksteps = 8;            // its keys, in steps of 16
       bool pre = false;          // the first S of the current item was issued at the end of the previous one
@@ -1471,7 +1482,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             if (!ok) break;
             tc_fence_after();
             if (!kShared) {
-              ksteps = (tile_keys_single(cur, 0, dn) + 15) >> 4;
+              ksteps = (tile_keys(cur, start, 0, dn) + 15) >> 4;
             } else {
               const int meta = read_meta(u);
               dn = (meta & 256) != 0;
@@ -1515,7 +1526,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             bool dn_next = false;
             int ks_next = 8;
             if (!last) {
-              if (!kShared) ks_next = (tile_keys_single(cur, j + 1, dn_next) + 15) >> 4;
+              if (!kShared) ks_next = (tile_keys(cur, start, j + 1, dn_next) + 15) >> 4;
             } else {
               // the next item (fetched long ago): its first S follows this item's last O
               const int nn = n_it + 1;
@@ -1527,7 +1538,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
               s_on0 = can_pre;
               s_on1 = can_pre && nxt.b_active;
               q_last = nxt.T == 1;
-              if (!kShared && can_pre) ks_next = (tile_keys_single(nxt, 0, dn_next) + 15) >> 4;
+              if constexpr (kWindow) start_next = __shfl_sync(0xffffffffu, bars->window[nn & 1].start, 0);
+              if (!kShared && can_pre) ks_next = (tile_keys(nxt, start_next, 0, dn_next) + 15) >> 4;
             }
             if (s_on0) {
               ok = BICACHE_WAIT(bar_full + sn * 8, ((u + 2) >> 2) & 1);
@@ -1613,11 +1625,13 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           ok = BICACHE_WAIT(smem_u32(&bars->info_full[nn & 1]), (nn >> 1) & 1);
           if (!ok) break;
           nxt = read_geo_uniform(&bars->info[nn & 1], s.num_splits, s.tiles_per_split);
+          if constexpr (kWindow) start_next = __shfl_sync(0xffffffffu, bars->window[nn & 1].start, 0);
         }
         if (elect_one()) mbar_arrive(smem_u32(&bars->info_free[n_it & 1]));
         __syncwarp();
         pre = can_pre;
         cur = nxt;
+        start = start_next;
         ++n_it;
       }
 #undef BICACHE_WAIT

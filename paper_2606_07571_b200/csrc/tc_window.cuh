@@ -43,7 +43,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   const int T = it.tile_end - it.tile_begin;
   const int rows = min(128, r.n * G - it.row0);                // rows of the item; the warps beyond them do nothing
   const int active = (rows + 31) >> 5;
-  auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - (it.tile_begin + j) * (kKeys / kPageSize)); };
+  auto tile_of = [&](int j) { return window_tile(it.start, it.tile_begin, it.tile_end, j); };
+  auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - tile_of(j) * (kKeys / kPageSize)); };
 
   // Set-up, all of it side by side: thread 0 its barriers, warp 4 TMEM, warps 5 and 6 their own barriers and the first
   // tiles, for which they need nobody.
@@ -55,7 +56,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     const int b = j % stages;
     const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
     const unsigned dst = (is_v ? v_ring : k_ring) + b * kKvTileBytes;
-    const int npages = tile_pages(j), s = (it.tile_begin + j) * (kKeys / kPageSize) + lane;
+    const int npages = tile_pages(j), s = tile_of(j) * (kKeys / kPageSize) + lane;
     const char* src = nullptr;
     bool bulk = lane < npages;
     WindowSlots slots = WindowSlots{0, kPageSize, 0};
@@ -152,10 +153,9 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
       const bool mine = row < rows;
       WindowColumns col = WindowColumns{0, 0x7fffffff, 0};
       if (mine) col = window_columns(a, it.pages, r.len, r.pos + (it.row0 + row) / G);
-      const int col0 = it.tile_begin * kKeys;
       for (int j = 0; j < T && ok; ++j) {
         const int b = j & 1;
-        const int begin = col.begin - col0 - j * kKeys, end = col.end - col0 - j * kKeys, sink = col.sink - col0 - j * kKeys;
+        const int col0 = tile_of(j) * kKeys, begin = col.begin - col0, end = col.end - col0, sink = col.sink - col0;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->s_full[b]), (j >> 1) & 1, abort_flag));
         if (!ok) break;
         tc_fence_after();
