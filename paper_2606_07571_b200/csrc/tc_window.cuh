@@ -46,8 +46,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   auto tile_of = [&](int j) { return window_tile(it.start, it.tile_begin, it.tile_end, j); };
   auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - tile_of(j) * (kKeys / kPageSize)); };
 
-  // Set-up, all of it side by side: thread 0 its barriers, warp 4 TMEM, warps 5 and 6 their own barriers and the first
-  // tiles, for which they need nobody.
+  // Set-up, all of it side by side: warps 0-3 request the Q tile, thread 0 sets flags and barriers, warp 4 fetches TMEM, warps 5
+  // and 6 set their own barriers and issue the first tiles, for which they need nobody.
   const int is_v = warp - 5;
   const int stages = is_v ? kVStages : kKStages;
   int armed[kKStages] = {-1, -1, -1};        // load warps: the last tile armed with bulk copies, per stage
@@ -82,24 +82,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   };
   const int ahead = min(T, stages);          // tiles that find their slots free
   bool begun = false;
-  if (tid == 0) {
-    sy->wait_cycles = wait_cycles;
-    if ((q_smem & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
-    sy->dead = status_now != 0 || (q_smem & 1023u) != 0 ? 1 : 0;
-    sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
-    mbar_init(smem_u32(&sy->q_full), 32 * active);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sy->s_full[i]), 1);
-      mbar_init(smem_u32(&sy->p_full[i]), 32 * active);
-    }
-    mbar_init(smem_u32(&sy->pv_done), 1);
-    mbar_init(smem_u32(&sy->o_done), 1);
-    mbar_init(smem_u32(&sy->drain), 1);
-    fence_barrier_init();
-  } else if (warp == 4) {
-    tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
-    tmem_relinquish();
-  } else if (warp >= 5) {
+  bool dead;
+  if (warp >= 5) {
     if (lane == 0) {
       for (int i = 0; i < stages; ++i) {
         mbar_init(smem_u32(is_v ? &sy->v_full[i] : &sy->k_full[i]), 32);
@@ -108,33 +92,24 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
       fence_barrier_init();
     }
     __syncwarp();
+    asm volatile("barrier.cta.arrive 1, 224;" ::: "memory");       // the others may use the barriers
     begun = status_now == 0 && (q_smem & 1023u) == 0;
     if (begun)
       for (int j = 0; j < ahead; ++j) load_tile(j);
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&sy->tmem_base);
-  const bool dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
-  const unsigned tmem_o = tmem + 128;
-
-  if (warp < 4) {
-    // ================================ softmax and epilogue =================================
-    const int row = warp * 32 + lane;                        // row of the tile = TMEM lane
-    const unsigned lane_base = (unsigned)(warp * 32) << 16;
-    const float sl2 = a.scale * 1.4426950408889634f;         // scores are handled in the log2 domain
-    float m_ref = -INFINITY, l_sum = 0.f;
-    bool ok = !dead;
-    if (warp < active) {
-      if (ok && T > 0) {
+    asm volatile("barrier.cta.sync 2, 96;" ::: "memory");          // the flags that thread 0 sets
+    dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
+  } else {
+    if (warp == 4) {
+      tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
+      tmem_relinquish();
+    } else {
+      if (warp < active && T > 0) {
         // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i.
         // Rows past the end stay what they are: a row of Q meets no other row's results.
-        const int r0 = warp * 32 + (lane >> 4), c16 = lane & 15;
+        const int c16 = lane & 15, here = min(32, rows - warp * 32);
         const char* const q_head = a.q + (r.row * a.q_stride + (long long)it.hk * G * 128) * 2 + c16 * 16;
-        const int prow = it.row0 + r0;
+        const int prow = it.row0 + warp * 32 + (lane >> 4);
         int t = prow / G, jj = prow - t * G;
-        const int here = min(32, rows - warp * 32);
 #pragma unroll 4
         for (int i = lane >> 4; i < here; i += 2) {
           cp_async16(q_smem + tile_chunk_offset(warp * 32 + i, c16), q_head + ((long long)t * a.q_stride + jj * 128) * 2, 16u);
@@ -145,9 +120,45 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
           }
         }
         cp_async_commit();
+      }
+      if (tid == 0) {
+        sy->wait_cycles = wait_cycles;
+        if ((q_smem & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
+        sy->dead = status_now != 0 || (q_smem & 1023u) != 0 ? 1 : 0;
+        sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
+        mbar_init(smem_u32(&sy->q_full), 32 * active);
+        for (int i = 0; i < 2; ++i) {
+          mbar_init(smem_u32(&sy->s_full[i]), 1);
+          mbar_init(smem_u32(&sy->p_full[i]), 32 * active);
+        }
+        mbar_init(smem_u32(&sy->pv_done), 1);
+        mbar_init(smem_u32(&sy->o_done), 1);
+        mbar_init(smem_u32(&sy->drain), 1);
+        fence_barrier_init();
+      }
+      __syncwarp();
+      if (warp == 0) asm volatile("barrier.cta.arrive 2, 96;" ::: "memory");
+    }
+    tc_fence_before();
+    asm volatile("barrier.cta.sync 1, 224;" ::: "memory");
+    tc_fence_after();
+    dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
+  }
+  const unsigned tmem = warp < 5 ? *reinterpret_cast<volatile unsigned*>(&sy->tmem_base) : 0;
+  const unsigned tmem_o = tmem + 128;
+
+  if (warp < 4) {
+    // ================================ softmax and epilogue =================================
+    const int row = warp * 32 + lane;                        // row of the tile = TMEM lane
+    const unsigned lane_base = (unsigned)(warp * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f;         // scores are handled in the log2 domain
+    float m_ref = -INFINITY, l_sum = 0.f;
+    bool ok = !dead;
+    if (warp < active) {
+      if (T > 0) {
         cp_async_wait<0>();
         fence_proxy_async();
-        mbar_arrive(smem_u32(&sy->q_full));
+        if (ok) mbar_arrive(smem_u32(&sy->q_full));
       }
       // the columns this row sees, from the first tile on; a row past the end runs along unmasked and asks for nothing
       const bool mine = row < rows;

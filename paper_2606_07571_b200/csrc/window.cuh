@@ -208,10 +208,11 @@ __device__ __forceinline__ long long window_part(const WindowArgs& a, const Wind
 
 // ---------------------------------------------------------------------------------------------
 // CUDA-core kernel.  256 threads take a row tile against key tiles of 64: queries, keys and values lie in shared memory
-// as fp32 (a row's end padded by 16 bytes, so that lanes on neighbouring rows read other banks), the values where the
-// keys were.  A row tile of 64 is a grid of 16 x 16 threads, each with 4 rows x 4 keys of the scores and 4 rows x
-// D / 16 dims of the output.  A row tile of 16, for few rows, is four groups of 4 x 16 threads, each group with a quarter
-// of the keys of a tile and a running softmax of its own; they are put together at the end.  All sums in fp32.
+// as fp32 (a row's end padded by 16 bytes, so that lanes on neighbouring rows read other banks).  A row tile of 64 is a grid
+// of 16 x 16 threads, each with 4 rows x 4 keys of the scores (two dims to a packed product) and 4 rows x D / 16 dims of the
+// output.  A row tile of 16, for few rows, is four groups of 4 x 16 threads, each group with a quarter of the keys of a
+// tile and a running softmax of its own; they are put together at the end.  All sums in fp32.  Values arrive while the scores
+// are computed, the next tile's keys during the rest.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWinThreads = 256;
 constexpr int kWinKeys = 64;
@@ -219,7 +220,7 @@ constexpr int kWinPer = 4;                      // rows of a thread
 constexpr int kWinLanes = 16;                   // threads that share a row
 
 inline size_t window_simt_smem(int rows, int D) {
-  return sizeof(float) * ((size_t)(rows + kWinKeys) * (D + 4) + (size_t)kWinKeys * (rows + 4));
+  return sizeof(float) * ((size_t)(rows + 2 * kWinKeys) * (D + 4) + (size_t)kWinKeys * (rows + 4));
 }
 
 __device__ __forceinline__ float lanes16_max(float x) {
@@ -245,8 +246,9 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
   extern __shared__ __align__(16) float win_smem[];
   const int D = a.D, pitch = D + 4, chunks = D / kPer;
   float* const qs = win_smem;                                      // [kRows][pitch]
-  float* const ks = qs + kRows * pitch;                            // [kWinKeys][pitch]: keys, then values
-  float* const ps = ks + kWinKeys * pitch;                         // [kWinKeys][kPPitch]
+  float* const ks = qs + kRows * pitch;                            // [kWinKeys][pitch]
+  float* const vs = ks + kWinKeys * pitch;
+  float* const ps = vs + kWinKeys * pitch;                         // [kWinKeys][kPPitch]
   const WindowReq& r = window_req(a, list.w, blockIdx.x);
   const WindowItem it = window_item<kWinKeys>(a, r, blockIdx.x, kRows);
   const int* const pages = window_page_list(a, r, list.w);
@@ -282,68 +284,92 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
     for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] = 0.f;
   }
-  auto stage = [&](const char* pool, int tile) {
-    for (int i = tid; i < kWinKeys * chunks; i += kWinThreads) {
-      const int key = i / chunks, c = i - key * chunks, s = tile * (kWinKeys / kPageSize) + key / kPageSize;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (s < it.pages.count && window_slots(it.pages, s).has(key % kPageSize))
-        v = *reinterpret_cast<const uint4*>(pool + window_page(r, pages, it.pages, s) * a.page_stride +
-                                            (long long)it.hk * a.page_bytes +
-                                            page_chunk_offset(a.swizzled != 0, key % kPageSize, c, chunks * 16));
-      float f[kPer];
-      Tr::unpack(v, f);
+  // One tile of keys or values; slots that no row of the item sees become zero.  fp32 is copied asynchronously.
+  const int key_first = tid / chunks, c_first = tid - key_first * chunks, key_step = kWinThreads / chunks, c_step = kWinThreads - key_step * chunks;
+  auto stage = [&](float* dst, const char* pool, int tile) {
+    pool += (long long)it.hk * a.page_bytes;
+    for (int key = key_first, c = c_first; key < kWinKeys;) {
+      const int s = tile * (kWinKeys / kPageSize) + key / kPageSize;
+      const bool has = s < it.pages.count && window_slots(it.pages, s).has(key % kPageSize);
+      const char* src = pool;
+      if (has)
+        src += window_page(r, pages, it.pages, s) * a.page_stride + page_chunk_offset(a.swizzled != 0, key % kPageSize, c, chunks * 16);
+      float* const to = &dst[key * pitch + c * kPer];
+      if constexpr (kEsize == 4) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                     ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(src), "r"(has ? 16u : 0u) : "memory");
+      } else {
+        float f[kPer];
+        Tr::unpack(has ? *reinterpret_cast<const uint4*>(src) : make_uint4(0, 0, 0, 0), f);
 #pragma unroll
-      for (int e = 0; e < kPer; e += 4)
-        *reinterpret_cast<float4*>(&ks[key * pitch + c * kPer + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        for (int e = 0; e < kPer; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+      }
+      key += key_step;
+      c += c_step;
+      if (c >= chunks) {
+        c -= chunks;
+        ++key;
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto landed = [](bool all) {                                     // all copies of this thread, or all but the last
+    if (all) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;" ::: "memory");
   };
 
-  for (int tile = it.tile_begin; tile < it.tile_end; ++tile) {
-    __syncthreads();
-    stage(a.pool_k, tile);
-    __syncthreads();
-    float s[kWinPer][kMine];
+  const float sl2 = a.scale * 1.4426950408889634f;                 // scores are handled in the log2 domain
+  const int num_tiles = it.tile_end - it.tile_begin;
+  if (num_tiles > 0) stage(ks, a.pool_k, it.start);
+  for (int j = 0; j < num_tiles; ++j) {
+    const int tile = window_tile(it.start, it.tile_begin, it.tile_end, j);
+    landed(true);                                                  // the keys
+    __syncthreads();                                               // ... and the last tile's values have been read
+    stage(vs, a.pool_v, tile);
+    unsigned long long s2[kWinPer][kMine];                         // sums over even and odd dims
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i)
 #pragma unroll
-      for (int j = 0; j < kMine; ++j) s[i][j] = 0.f;
+      for (int k = 0; k < kMine; ++k) s2[i][k] = 0ull;
+#pragma unroll 2
     for (int d = 0; d < D; d += 4) {
-      float4 qv[kWinPer], kv[kMine];
+      ulonglong2 qv[kWinPer], kv[kMine];
 #pragma unroll
-      for (int i = 0; i < kWinPer; ++i) qv[i] = *reinterpret_cast<const float4*>(&qs[(ty * kWinPer + i) * pitch + d]);
+      for (int i = 0; i < kWinPer; ++i) qv[i] = *reinterpret_cast<const ulonglong2*>(&qs[(ty * kWinPer + i) * pitch + d]);
 #pragma unroll
-      for (int j = 0; j < kMine; ++j)
-        kv[j] = *reinterpret_cast<const float4*>(&ks[(part * kPartKeys + tx + j * kWinLanes) * pitch + d]);
+      for (int k = 0; k < kMine; ++k)
+        kv[k] = *reinterpret_cast<const ulonglong2*>(&ks[(part * kPartKeys + tx + k * kWinLanes) * pitch + d]);
 #pragma unroll
       for (int i = 0; i < kWinPer; ++i)
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-          s[i][j] = fmaf(qv[i].x, kv[j].x, s[i][j]);
-          s[i][j] = fmaf(qv[i].y, kv[j].y, s[i][j]);
-          s[i][j] = fmaf(qv[i].z, kv[j].z, s[i][j]);
-          s[i][j] = fmaf(qv[i].w, kv[j].w, s[i][j]);
+        for (int k = 0; k < kMine; ++k) {
+          asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(s2[i][k]) : "l"(qv[i].x), "l"(kv[k].x));
+          asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(s2[i][k]) : "l"(qv[i].y), "l"(kv[k].y));
         }
     }
     __syncthreads();                                               // the keys have been read
-    stage(a.pool_v, tile);
+    if (j + 1 < num_tiles) stage(ks, a.pool_k, window_tile(it.start, it.tile_begin, it.tile_end, j + 1));
+    float s[kWinPer][kMine];
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i) {
+      const int c0 = tile * kWinKeys + part * kPartKeys;           // the group's first column
+      const bool whole = col[i].begin <= c0 && col[i].end >= c0 + kPartKeys;
       float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int c = tile * kWinKeys + part * kPartKeys + tx + j * kWinLanes;
-        const bool seen = (c >= col[i].begin && c < col[i].end) || c < col[i].sink;
-        s[i][j] = seen ? s[i][j] * a.scale : -INFINITY;
-        mx = fmaxf(mx, s[i][j]);
+      for (int k = 0; k < kMine; ++k) {
+        const int c = c0 + tx + k * kWinLanes;
+        const float x = (__uint_as_float((unsigned)s2[i][k]) + __uint_as_float((unsigned)(s2[i][k] >> 32))) * sl2;
+        s[i][k] = whole || (c >= col[i].begin && c < col[i].end) || c < col[i].sink ? x : -INFINITY;
+        mx = fmaxf(mx, s[i][k]);
       }
       const float m_new = fmaxf(m_run[i], lanes16_max(mx));
       const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen so far: every weight is 0
-      const float alpha = expf(m_run[i] - m_use);
+      const float alpha = exp2f(m_run[i] - m_use);
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        s[i][j] = expf(s[i][j] - m_use);
-        sum += s[i][j];
+      for (int k = 0; k < kMine; ++k) {
+        s[i][k] = exp2f(s[i][k] - m_use);
+        sum += s[i][k];
       }
       l_run[i] = l_run[i] * alpha + sum;                           // of this thread's keys; added up at the end
       m_run[i] = m_new;
@@ -351,9 +377,10 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
       for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] *= alpha;
     }
 #pragma unroll
-    for (int j = 0; j < kMine; ++j)
-      *reinterpret_cast<float4*>(&ps[(part * kPartKeys + tx + j * kWinLanes) * kPPitch + ty * kWinPer]) =
-          make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+    for (int k = 0; k < kMine; ++k)
+      *reinterpret_cast<float4*>(&ps[(part * kPartKeys + tx + k * kWinLanes) * kPPitch + ty * kWinPer]) =
+          make_float4(s[0][k], s[1][k], s[2][k], s[3][k]);
+    landed(j + 1 == num_tiles);                                            // the values
     __syncthreads();
 #pragma unroll 4
     for (int key = part * kPartKeys; key < (part + 1) * kPartKeys; ++key) {
@@ -363,7 +390,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
         if (d < D) {
-          const float2 v = *reinterpret_cast<const float2*>(&ks[key * pitch + d]);
+          const float2 v = *reinterpret_cast<const float2*>(&vs[key * pitch + d]);
 #pragma unroll
           for (int i = 0; i < kWinPer; ++i) {
             acc[i][2 * g] = fmaf(pr[i], v.x, acc[i][2 * g]);
@@ -377,7 +404,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
   for (int i = 0; i < kWinPer; ++i) l_run[i] = lanes16_sum(l_run[i]);
   if (kParts > 1) {
-    // the groups' results: accumulators where the keys and values were, statistics where the weights were
+    // the groups' results: accumulators where the keys were, statistics where the weights were
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i) {
@@ -406,7 +433,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
       for (int g = 0; g < 2 * kPairs; ++g) acc[i][g] = 0.f;
 #pragma unroll
       for (int o = 0; o < kParts; ++o) {
-        const float w = expf(ps[o * kRows + row] - m_use);
+        const float w = exp2f(ps[o * kRows + row] - m_use);
         l_all += w * ps[(kParts + o) * kRows + row];
 #pragma unroll
         for (int g = 0; g < kPairs; ++g) {
@@ -428,7 +455,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
     if (p >= packed) break;
     const WindowRow w(a, it.hk, p);
     const float inv = l_run[i] == 0.f ? 0.f : 1.f / l_run[i];
-    const float lse = l_run[i] == 0.f ? -INFINITY : m_run[i] + logf(l_run[i]);
+    const float lse = l_run[i] == 0.f ? -INFINITY : m_run[i] * 0.6931471805599453f + logf(l_run[i]);
     if (r.splits > 1) {
       const long long at = window_part(a, r, it.split, w);
       if (tx == 0) a.part_lse[at] = lse;

@@ -306,8 +306,9 @@ class WindowLaunches {
       if (st != BICACHE_OK) return st;
     }
     p.r.page_word = (int)pages_.size();
-    for (int s = 0; s < w.count; ++s)
-      pages_.push_back(pages[s < w.sink_pages ? s : s + p.r.gap]);
+    const auto behind = pages.begin() + w.sink_pages + p.r.gap;
+    pages_.insert(pages_.end(), pages.begin(), pages.begin() + w.sink_pages);
+    pages_.insert(pages_.end(), behind, behind + (w.count - w.sink_pages));
     pending_.push_back(p);
     words_ += words;
     return alone ? flush() : BICACHE_OK;
@@ -369,7 +370,7 @@ class WindowLaunches {
     e = launch(a, list, used);
     ctx_->launches++;
     if (e == cudaSuccess && row_heads > 0) {
-      e = join(a, list, used, row_heads, most_splits);
+      e = join(a, list, words, row_heads, most_splits);     // needs no pages
       ctx_->launches++;
     }
     return cuda_status(ctx_, e, "attend_window");
@@ -412,6 +413,7 @@ class WindowLaunches {
         if (sp > 1) part += (long long)sp * p.r.n * base_.Hq;
       }
       if (part > ctx_->part_capacity_rowheads) break;
+      if (s > 1 && items > 4LL * form_.slots) break;         // enough to even out: more would only start more often
       const double longest = tps + form_.item_cost;
       const double mean = (double)(tiles + items * form_.item_cost) / form_.slots;
       const double cost = (items <= form_.slots ? longest : std::max(longest, mean + longest / 2)) + (part > 0 ? form_.join_cost : 0);
@@ -475,8 +477,8 @@ class WindowSimtLaunches : public WindowLaunches {
 
  protected:
   static WindowForm form_of(const bicache_ctx* ctx, int rows) {
-    const int blocks = std::max(1, (int)(227 * 1024 / (window_simt_smem(rows, ctx->cfg.head_dim) + 1024)));
-    return WindowForm{rows, kWinKeys, std::min(blocks, rows == 16 ? 4 : 2) * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
+    const int blocks = std::max(1, std::min(2, (int)(227 * 1024 / (window_simt_smem(rows, ctx->cfg.head_dim) + 1024))));
+    return WindowForm{rows, kWinKeys, blocks * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
   }
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
     const size_t smem = window_simt_smem(form_.tile_rows, a.D);
@@ -614,7 +616,9 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   // the tensor-core kernel takes the row maximum before scaling, which needs a positive scale
   if (ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && softmax_scale > 0.f) {
     // Requests with more than 128 packed rows go through the kernel with row tiles of 256, which shares every key tile
-    // between two tiles of 128 rows, if there are enough of them to fill the SMs; it does not split the keys.
+    // between two tiles of 128 rows, if there are three of them to an SM; it does not split the keys.  (28 query heads, window
+    // of 500 + 201: 224 items take 71 us, as ranges and tiles of 128 rows 59; 32 query heads, window of 1023: 512 items take
+    // 114 us against 122, 2048 items 406 against 436.)
     long long tiles = 0, rows_total = 0;
     for (int i = 0; i < R; ++i) {
       rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
@@ -624,7 +628,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     std::memset(&maps, 0, sizeof(maps));
     maps.q_tma = (128 % G == 0) ? 1 : 0;
     maps.o_tma = (32 % G == 0) ? 1 : 0;
-    const bool by_256 = tiles >= ctx->sm_count && rows_total < 0x7fffffffLL &&              // box coordinates are 32-bit
+    const bool by_256 = tiles >= 3LL * ctx->sm_count && rows_total < 0x7fffffffLL &&              // box coordinates are 32-bit
                         encode_map(&maps.q, q, rows_total, cfg.num_q_heads, q_row_stride, maps.q_tma ? G : 1, maps.q_tma ? 128 / G : 128) &&
                         encode_map(&maps.o, out, rows_total, cfg.num_q_heads, out_row_stride, maps.o_tma ? G : 1, maps.o_tma ? 32 / G : 32);
     ctx->last_kernel = by_256 ? BICACHE_KERNEL_TENSOR : BICACHE_KERNEL_KEY_RANGES;

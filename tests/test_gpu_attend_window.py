@@ -139,7 +139,7 @@ def test_row_tiles_of_256(window, heads):
     """Enough rows for the kernel with row tiles of 256: prompts, rows that see nothing, an empty cache, a few rows."""
     lens = [700, 901, 257, 0]
     requests = [(0, 0, 700), (1, 400, 501), (2, 0, 256), (1, 1300, 130), (3, 5, 200), (0, 699, 1), (2, 200, 40), (1, 880, 129)]
-    b = Batch(heads, torch.bfloat16, lens, requests, spare=37)
+    b = Batch(heads, torch.bfloat16, lens, requests * 2, spare=37)
     out, _ = b.check(*window)
     assert b.bc.last_attention_kernel() == binding.KERNEL_TENSOR
     again, _ = b.call(*window)
@@ -148,7 +148,7 @@ def test_row_tiles_of_256(window, heads):
 
 def test_unseen_tokens_and_row_tiles_of_256():
     m, n, sinks, left = 2600, 1500, 5, 70
-    b = Batch("gqa28", torch.bfloat16, [m], [(0, m - n, n)])
+    b = Batch("gqa28", torch.bfloat16, [m], [(0, m - n, n)] * 3)
     want = b.call(sinks, left, 0)
     assert b.bc.last_attention_kernel() == binding.KERNEL_TENSOR
     first = m - n - left
@@ -206,7 +206,7 @@ def test_a_nan_that_is_seen_spreads(heads, dtype, n):
 @pytest.mark.parametrize("heads,dtype,many", [("gqa4", torch.bfloat16, False), ("gqa32", torch.bfloat16, True), ("mha4_64", torch.float32, False)])
 def test_steep_scores(heads, dtype, many):
     """Scores that grow along the keys by far more than the running reference follows at a time."""
-    b = Batch(heads, dtype, [700], [(0, 690, 10), (0, 0, 300)] * (6 if many else 1), std=0.1)
+    b = Batch(heads, dtype, [700], [(0, 690, 10), (0, 0, 300)] * (12 if many else 1), std=0.1)
     ramp = torch.linspace(-30, 30, 700, device="cuda")[:, None, None]
     k = (torch.ones((700, b.hkv, b.d), device="cuda") * ramp).to(dtype)
     b.q[...] = 0.25
