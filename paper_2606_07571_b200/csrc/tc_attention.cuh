@@ -1277,7 +1277,6 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         const WindowInfo& wi = bars->window[n_it & 1];
         const WindowPages wp = wi.pages;
         const WindowReq& rq = reinterpret_cast<const WindowReq*>(win.list.w)[wi.req];
-        const int* const list = window_page_list(win.a, rq, win.list.w);
         const char* const pool_base = (is_v ? win.a.pool_v : win.a.pool_k) + (long long)kv_head * win.a.page_bytes;
         for (int j = 0; j < g.T; ++j) {
           const int u = U + 2 * j + is_v;
@@ -1289,7 +1288,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           bool bulk = lane < npages;
           WindowSlots sl = WindowSlots{0, kPageSize, 0};
           if (bulk) {
-            src = pool_base + window_page(rq, list, wp, page0 + lane) * win.a.page_stride;
+            src = pool_base + window_page(win.a, rq, win.list.w, wp, page0 + lane) * win.a.page_stride;
             if (is_v) {
               sl = window_slots(wp, page0 + lane);
               bulk = sl.whole();

@@ -62,7 +62,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     WindowSlots slots = WindowSlots{0, kPageSize, 0};
     if (bulk) {
       src = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes +
-            window_page(r, window_page_list(a, r, params.w), it.pages, s) * a.page_stride;
+            window_page(a, r, params.w, it.pages, s) * a.page_stride;
       if (is_v) {
         slots = window_slots(it.pages, s);
         bulk = slots.whole();

@@ -158,8 +158,8 @@ __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const Win
   const int per_head = r.row_tiles * r.splits;
   it.hk = at / per_head;
   at -= it.hk * per_head;
-  const int tile = at / r.splits;
-  it.split = at - tile * r.splits;
+  const int from_end = at / r.splits, tile = r.row_tiles - 1 - from_end;         // the last rows see most: they go first
+  it.split = at - from_end * r.splits;
   it.row0 = tile * tile_rows;
   const int last = min(it.row0 + tile_rows, r.n * G) - 1;
   it.pages = window_pages(a.sinks, a.left, a.right, r.len, r.pos + it.row0 / G, r.pos + last / G);
@@ -174,13 +174,12 @@ __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const Win
   it.start = max(it.tile_begin, min(it.start, it.tile_end - 1));
   return it;
 }
-// The pool page of page `s` of an item's sequence.
-__device__ __forceinline__ int window_page(const WindowReq& r, const int* pages, const WindowPages& w, int s) {
+// The pool page of page `s` of an item's sequence.  (Two loads and a branch, not one load through either pointer: that would
+// read the parameters by way of memory, in 0.4 us instead of 0.1.)
+__device__ __forceinline__ int window_page(const WindowArgs& a, const WindowReq& r, const int* list, const WindowPages& w, int s) {
   const int page = s < w.sink_pages ? s : s - w.sink_pages + w.lo_page;          // of the prefix
-  return pages[page < r.sink_pages ? page : page - r.gap];
-}
-__device__ __forceinline__ const int* window_page_list(const WindowArgs& a, const WindowReq& r, const int* list) {
-  return a.staged_pages ? a.staged_pages : list + r.page_word;
+  const int at = page < r.sink_pages ? page : page - r.gap;
+  return a.staged_pages ? a.staged_pages[at] : list[r.page_word + at];
 }
 // The slots of page `s` of the sequence that some row of the item sees: [lo, hi), and [0, sink) besides.  What lies
 // in the others must not reach a sum, not even with weight 0: it may be no number.
@@ -207,22 +206,27 @@ __device__ __forceinline__ long long window_part(const WindowArgs& a, const Wind
 }
 
 // ---------------------------------------------------------------------------------------------
-// CUDA-core kernel.  256 threads take a row tile against key tiles of 64: queries, keys and values lie in shared memory
+// CUDA-core kernel.  128 threads take a row tile against key tiles of 64: queries, keys and values lie in shared memory
 // as fp32 (a row's end padded by 16 bytes, so that lanes on neighbouring rows read other banks).  A row tile of 64 is a grid
-// of 16 x 16 threads, each with 4 rows x 4 keys of the scores (two dims to a packed product) and 4 rows x D / 16 dims of the
-// output.  A row tile of 16, for few rows, is four groups of 4 x 16 threads, each group with a quarter of the keys of a
+// of 8 x 16 threads, each with 8 rows x 4 keys of the scores (two dims to a packed product) and 8 rows x D / 16 dims of the
+// output.  A row tile of 16, for few rows, is four groups of 2 x 16 threads, each group with a quarter of the keys of a
 // tile and a running softmax of its own; they are put together at the end.  All sums in fp32.  Values arrive while the scores
 // are computed, the next tile's keys during the rest.
 // ---------------------------------------------------------------------------------------------
-constexpr int kWinThreads = 256;
+constexpr int kWinThreads = 128;
 constexpr int kWinKeys = 64;
-constexpr int kWinPer = 4;                      // rows of a thread
+constexpr int kWinPer = 8;                      // rows of a thread
 constexpr int kWinLanes = 16;                   // threads that share a row
 
 inline size_t window_simt_smem(int rows, int D) {
   return sizeof(float) * ((size_t)(rows + 2 * kWinKeys) * (D + 4) + (size_t)kWinKeys * (rows + 4));
 }
 
+__device__ __forceinline__ float win_exp2(float x) {               // 2 ulp, results below 2^-126 are 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float lanes16_max(float x) {
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
@@ -234,8 +238,14 @@ __device__ __forceinline__ float lanes16_sum(float x) {
   return x;
 }
 
+// kMaxD 64 and 128: head dims of exactly that; 256: any.
+constexpr int kWinAnyD = 256;
+inline int window_simt_blocks(int rows, int D) {                   // that fit an SM, by shared memory and registers
+  const int fit = (int)(227 * 1024 / (window_simt_smem(rows, D) + 1280));
+  return std::max(1, std::min(fit, D == 64 ? 3 : 2));
+}
 template <typename T, int kRows, int kMaxD, int kWords>
-__global__ void __launch_bounds__(kWinThreads)
+__global__ void __launch_bounds__(kWinThreads, kMaxD == 64 ? 3 : kMaxD == 128 ? 2 : 1)
 window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__ ParamList<kWords> list) {
   using Tr = ElemTraits<T>;
   constexpr int kPer = Tr::kPerChunk, kEsize = (int)sizeof(T);
@@ -243,15 +253,19 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
   constexpr int kPartKeys = kWinKeys / kParts, kMine = kPartKeys / kWinLanes;                    // of a group, of a thread
   constexpr int kPairs = kMaxD / (2 * kWinLanes);                  // pairs of dims of a thread
   constexpr int kPPitch = kRows + 4;
+  struct PagePlace {
+    long long at;                                                  // bytes from the layer's pool
+    unsigned slots;                                                // those that some row of the item sees
+  };
+  __shared__ PagePlace places[2][kWinKeys / kPageSize];            // of a tile's pages, the next tile's beside
   extern __shared__ __align__(16) float win_smem[];
-  const int D = a.D, pitch = D + 4, chunks = D / kPer;
+  const int D = kMaxD == kWinAnyD ? a.D : kMaxD, pitch = D + 4, chunks = D / kPer;
   float* const qs = win_smem;                                      // [kRows][pitch]
   float* const ks = qs + kRows * pitch;                            // [kWinKeys][pitch]
   float* const vs = ks + kWinKeys * pitch;
   float* const ps = vs + kWinKeys * pitch;                         // [kWinKeys][kPPitch]
   const WindowReq& r = window_req(a, list.w, blockIdx.x);
   const WindowItem it = window_item<kWinKeys>(a, r, blockIdx.x, kRows);
-  const int* const pages = window_page_list(a, r, list.w);
   const int G = a.Hq / a.Hkv, packed = r.n * G;
   const int tid = threadIdx.x, tx = tid % kWinLanes, ty = tid / kWinLanes % kRowGroups, part = tid / (kWinLanes * kRowGroups);
 
@@ -284,16 +298,27 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
     for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] = 0.f;
   }
+  // Where a tile's pages lie, for the tiles to be staged after the next barrier.
+  auto look_up = [&](int tile, PagePlace* to) {
+    if (tid >= kWinKeys / kPageSize) return;
+    const int s = tile * (kWinKeys / kPageSize) + tid;
+    PagePlace p = PagePlace{0, 0u};
+    if (s < it.pages.count) {
+      const WindowSlots sl = window_slots(it.pages, s);
+#pragma unroll
+      for (int i = 0; i < kPageSize; ++i) p.slots |= (sl.has(i) ? 1u : 0u) << i;
+      p.at = window_page(a, r, list.w, it.pages, s) * a.page_stride + (long long)it.hk * a.page_bytes;
+    }
+    to[tid] = p;
+  };
   // One tile of keys or values; slots that no row of the item sees become zero.  fp32 is copied asynchronously.
   const int key_first = tid / chunks, c_first = tid - key_first * chunks, key_step = kWinThreads / chunks, c_step = kWinThreads - key_step * chunks;
-  auto stage = [&](float* dst, const char* pool, int tile) {
-    pool += (long long)it.hk * a.page_bytes;
+  auto stage = [&](float* dst, const char* pool, const PagePlace* from) {
+#pragma unroll 4
     for (int key = key_first, c = c_first; key < kWinKeys;) {
-      const int s = tile * (kWinKeys / kPageSize) + key / kPageSize;
-      const bool has = s < it.pages.count && window_slots(it.pages, s).has(key % kPageSize);
-      const char* src = pool;
-      if (has)
-        src += window_page(r, pages, it.pages, s) * a.page_stride + page_chunk_offset(a.swizzled != 0, key % kPageSize, c, chunks * 16);
+      const PagePlace& p = from[key / kPageSize];
+      const bool has = (p.slots >> (key % kPageSize)) & 1u;
+      const char* const src = has ? pool + p.at + page_chunk_offset(a.swizzled != 0, key % kPageSize, c, chunks * 16) : pool;
       float* const to = &dst[key * pitch + c * kPer];
       if constexpr (kEsize == 4) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
@@ -320,18 +345,22 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 
   const float sl2 = a.scale * 1.4426950408889634f;                 // scores are handled in the log2 domain
   const int num_tiles = it.tile_end - it.tile_begin;
-  if (num_tiles > 0) stage(ks, a.pool_k, it.start);
+  if (num_tiles > 0) {
+    look_up(it.start, places[0]);
+    __syncthreads();
+    stage(ks, a.pool_k, places[0]);
+  }
   for (int j = 0; j < num_tiles; ++j) {
     const int tile = window_tile(it.start, it.tile_begin, it.tile_end, j);
     landed(true);                                                  // the keys
     __syncthreads();                                               // ... and the last tile's values have been read
-    stage(vs, a.pool_v, tile);
+    stage(vs, a.pool_v, places[j & 1]);
+    if (j + 1 < num_tiles) look_up(window_tile(it.start, it.tile_begin, it.tile_end, j + 1), places[(j + 1) & 1]);
     unsigned long long s2[kWinPer][kMine];                         // sums over even and odd dims
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i)
 #pragma unroll
       for (int k = 0; k < kMine; ++k) s2[i][k] = 0ull;
-#pragma unroll 2
     for (int d = 0; d < D; d += 4) {
       ulonglong2 qv[kWinPer], kv[kMine];
 #pragma unroll
@@ -348,27 +377,38 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
         }
     }
     __syncthreads();                                               // the keys have been read
-    if (j + 1 < num_tiles) stage(ks, a.pool_k, window_tile(it.start, it.tile_begin, it.tile_end, j + 1));
+    if (j + 1 < num_tiles) stage(ks, a.pool_k, places[(j + 1) & 1]);
     float s[kWinPer][kMine];
+    const int c0 = tile * kWinKeys + part * kPartKeys;             // the group's first column
+    bool whole = true;                                             // the rows see the group's keys in full
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i) {
-      const int c0 = tile * kWinKeys + part * kPartKeys;           // the group's first column
-      const bool whole = col[i].begin <= c0 && col[i].end >= c0 + kPartKeys;
-      float mx = -INFINITY;
+      whole = whole && col[i].begin <= c0 && col[i].end >= c0 + kPartKeys;
 #pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-        const int c = c0 + tx + k * kWinLanes;
-        const float x = (__uint_as_float((unsigned)s2[i][k]) + __uint_as_float((unsigned)(s2[i][k] >> 32))) * sl2;
-        s[i][k] = whole || (c >= col[i].begin && c < col[i].end) || c < col[i].sink ? x : -INFINITY;
-        mx = fmaxf(mx, s[i][k]);
-      }
+      for (int k = 0; k < kMine; ++k)
+        s[i][k] = (__uint_as_float((unsigned)s2[i][k]) + __uint_as_float((unsigned)(s2[i][k] >> 32))) * sl2;
+    }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < kWinPer; ++i)
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+          const int c = c0 + tx + k * kWinLanes;
+          if (!((c >= col[i].begin && c < col[i].end) || c < col[i].sink)) s[i][k] = -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kWinPer; ++i) {
+      float mx = s[i][0];
+#pragma unroll
+      for (int k = 1; k < kMine; ++k) mx = fmaxf(mx, s[i][k]);
       const float m_new = fmaxf(m_run[i], lanes16_max(mx));
       const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen so far: every weight is 0
-      const float alpha = exp2f(m_run[i] - m_use);
+      const float alpha = win_exp2(m_run[i] - m_use);
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < kMine; ++k) {
-        s[i][k] = exp2f(s[i][k] - m_use);
+        s[i][k] = win_exp2(s[i][k] - m_use);
         sum += s[i][k];
       }
       l_run[i] = l_run[i] * alpha + sum;                           // of this thread's keys; added up at the end
@@ -378,18 +418,27 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
     }
 #pragma unroll
     for (int k = 0; k < kMine; ++k)
-      *reinterpret_cast<float4*>(&ps[(part * kPartKeys + tx + k * kWinLanes) * kPPitch + ty * kWinPer]) =
-          make_float4(s[0][k], s[1][k], s[2][k], s[3][k]);
+#pragma unroll
+      for (int i = 0; i < kWinPer; i += 4)
+        *reinterpret_cast<float4*>(&ps[(part * kPartKeys + tx + k * kWinLanes) * kPPitch + ty * kWinPer + i]) =
+            make_float4(s[i][k], s[i + 1][k], s[i + 2][k], s[i + 3][k]);
     landed(j + 1 == num_tiles);                                            // the values
     __syncthreads();
 #pragma unroll 4
     for (int key = part * kPartKeys; key < (part + 1) * kPartKeys; ++key) {
-      const float4 p = *reinterpret_cast<const float4*>(&ps[key * kPPitch + ty * kWinPer]);
-      const float pr[kWinPer] = {p.x, p.y, p.z, p.w};
+      float pr[kWinPer];
+#pragma unroll
+      for (int i = 0; i < kWinPer; i += 4) {
+        const float4 p = *reinterpret_cast<const float4*>(&ps[key * kPPitch + ty * kWinPer + i]);
+        pr[i] = p.x;
+        pr[i + 1] = p.y;
+        pr[i + 2] = p.z;
+        pr[i + 3] = p.w;
+      }
 #pragma unroll
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
-        if (d < D) {
+        if (kMaxD != kWinAnyD || d < D) {
           const float2 v = *reinterpret_cast<const float2*>(&vs[key * pitch + d]);
 #pragma unroll
           for (int i = 0; i < kWinPer; ++i) {
@@ -416,7 +465,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
-        if (d < D) *reinterpret_cast<float2*>(&ks[(part * kRows + row) * pitch + d]) = make_float2(acc[i][2 * g], acc[i][2 * g + 1]);
+        if (kMaxD != kWinAnyD || d < D) *reinterpret_cast<float2*>(&ks[(part * kRows + row) * pitch + d]) = make_float2(acc[i][2 * g], acc[i][2 * g + 1]);
       }
     }
     __syncthreads();
@@ -433,12 +482,12 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
       for (int g = 0; g < 2 * kPairs; ++g) acc[i][g] = 0.f;
 #pragma unroll
       for (int o = 0; o < kParts; ++o) {
-        const float w = exp2f(ps[o * kRows + row] - m_use);
+        const float w = win_exp2(ps[o * kRows + row] - m_use);
         l_all += w * ps[(kParts + o) * kRows + row];
 #pragma unroll
         for (int g = 0; g < kPairs; ++g) {
           const int d = (g * kWinLanes + tx) * 2;
-          if (d < D) {
+          if (kMaxD != kWinAnyD || d < D) {
             const float2 v = *reinterpret_cast<const float2*>(&ks[(o * kRows + row) * pitch + d]);
             acc[i][2 * g] += w * v.x;
             acc[i][2 * g + 1] += w * v.y;
@@ -462,7 +511,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
-        if (d < D) *reinterpret_cast<float2*>(a.part_o + at * D + d) = make_float2(acc[i][2 * g] * inv, acc[i][2 * g + 1] * inv);
+        if (kMaxD != kWinAnyD || d < D) *reinterpret_cast<float2*>(a.part_o + at * D + d) = make_float2(acc[i][2 * g] * inv, acc[i][2 * g + 1] * inv);
       }
     } else {
       const long long row = r.row + w.t;
@@ -471,7 +520,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
 #pragma unroll
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
-        if (d < D) {
+        if (kMaxD != kWinAnyD || d < D) {
           Tr::store(o + d * kEsize, acc[i][2 * g] * inv);
           Tr::store(o + (d + 1) * kEsize, acc[i][2 * g + 1] * inv);
         }

@@ -458,9 +458,9 @@ class WindowLaunches {
 template <typename F>
 void with_window_simt(int dtype, int rows, int D, F&& f) {
   auto dims = [&](auto zero, auto r) {
-    if (D <= 64) f(zero, r, std::integral_constant<int, 64>());
-    else if (D <= 128) f(zero, r, std::integral_constant<int, 128>());
-    else f(zero, r, std::integral_constant<int, 256>());
+    if (D == 64) f(zero, r, std::integral_constant<int, 64>());
+    else if (D == 128) f(zero, r, std::integral_constant<int, 128>());
+    else f(zero, r, std::integral_constant<int, kWinAnyD>());
   };
   auto tiles = [&](auto zero) {
     if (rows == 16) dims(zero, std::integral_constant<int, 16>());
@@ -477,8 +477,7 @@ class WindowSimtLaunches : public WindowLaunches {
 
  protected:
   static WindowForm form_of(const bicache_ctx* ctx, int rows) {
-    const int blocks = std::max(1, std::min(2, (int)(227 * 1024 / (window_simt_smem(rows, ctx->cfg.head_dim) + 1024))));
-    return WindowForm{rows, kWinKeys, blocks * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
+    return WindowForm{rows, kWinKeys, window_simt_blocks(rows, ctx->cfg.head_dim) * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
   }
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
     const size_t smem = window_simt_smem(form_.tile_rows, a.D);
