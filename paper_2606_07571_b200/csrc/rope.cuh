@@ -9,6 +9,7 @@
 // long argument reduction; here it is one 64-bit integer multiplication.  The part of a turn is reduced to
 // an eighth before it becomes fp32, so cos and sin are off by no more than about 1.2e-7.
 #pragma once
+#include <type_traits>
 #include <cuda_bf16.h>
 #include "common.cuh"
 #include "simt_kernels.cuh"
@@ -213,9 +214,9 @@ rope_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ RopeRows
 // Rows, any rotated width: one thread per pair (and per dim beyond the rotated ones), element by element.
 // A block takes one row at a time.
 // ---------------------------------------------------------------------------------------------
-template <typename T, typename A>
+template <typename T>
 __global__ void __launch_bounds__(kRopeThreads)
-rope_rows_kernel(const __grid_constant__ A a, const __grid_constant__ RopeRows r, int interleaved) {
+rope_rows_kernel(const __grid_constant__ RopeAngles a, const __grid_constant__ RopeRows r, int interleaved) {
   using Tr = ElemTraits<T>;
   constexpr int kEsize = (int)sizeof(T);
   __shared__ float2 cs[kRopeMaxPairs];
@@ -249,6 +250,106 @@ rope_rows_kernel(const __grid_constant__ A a, const __grid_constant__ RopeRows r
   }
 }
 
+// ---------------------------------------------------------------------------------------------
+// Rows of any rotated width in 16-byte chunks, with several position axes.  Where the halves of a pair lie in chunks that do
+// not line up (half-split pairs, rot_dim / 2 not a multiple of the chunk), a thread loads the other halves of its chunk
+// besides, by 4 bytes (by single elements for an odd number of pairs), which the L1 has; interleaved pairs lie in one chunk.
+// A block takes a row, and a batch of whole heads of it at a time: a row may be rotated in place, so what a batch loads
+// is there before what it stores.
+// ---------------------------------------------------------------------------------------------
+constexpr int kRopeHeld = 4;               // chunks of a batch that a thread holds
+
+// dims kPer * c .. of a head at `head`, rotated; cs: cosine and sine of every pair
+template <typename T>
+__device__ __forceinline__ uint4 rope_any_chunk(const char* head, int c, int pairs, bool interleaved, const float2* cs) {
+  using Tr = ElemTraits<T>;
+  constexpr int kPer = Tr::kPerChunk, kEsize = (int)sizeof(T), kWord = 4 / kEsize;
+  const uint4 own = *reinterpret_cast<const uint4*>(head + c * 16);
+  const int d0 = c * kPer;
+  if (d0 >= 2 * pairs) return own;
+  float x[kPer], y[kPer];
+  Tr::unpack(own, x);
+  if (interleaved) {
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) {
+      const int pair = (d0 + e) >> 1;
+      if (pair < pairs) {
+        const float2 w = cs[pair];
+        const float a = x[e], b = x[e + 1];
+        x[e] = fmaf(a, w.x, -(b * w.y));
+        x[e + 1] = fmaf(b, w.x, a * w.y);
+      }
+    }
+    return rope_pack<T>(x);
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; e += kWord) {
+    const int d = d0 + e, other = d < pairs ? d + pairs : d - pairs;
+    if (pairs % kWord == 0) {
+      unsigned w = 0;
+      if (d < 2 * pairs) w = *reinterpret_cast<const unsigned*>(head + other * kEsize);
+      if constexpr (kWord == 2) {
+        y[e] = __uint_as_float(w << 16);
+        y[e + 1] = __uint_as_float(w & 0xffff0000u);
+      } else {
+        y[e] = __uint_as_float(w);
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < kWord; ++f) {
+        const int df = d + f;
+        y[e + f] = df < 2 * pairs ? Tr::load(head + (df < pairs ? df + pairs : df - pairs) * kEsize) : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int d = d0 + e;
+    if (d < pairs) {
+      const float2 w = cs[d];
+      x[e] = fmaf(x[e], w.x, -(y[e] * w.y));
+    } else if (d < 2 * pairs) {
+      const float2 w = cs[d - pairs];
+      x[e] = fmaf(x[e], w.x, y[e] * w.y);
+    }
+  }
+  return rope_pack<T>(x);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRopeThreads)
+rope_any_kernel(const __grid_constant__ RopeAxes a, const __grid_constant__ RopeRows r, int interleaved) {
+  __shared__ float2 cs[kRopeMaxPairs];
+  const int chunks = r.head_bytes / 16, batch = kRopeHeld * kRopeThreads / chunks * chunks;     // units of whole heads
+  const int units = chunks * (r.t[0].heads + r.t[1].heads);
+  for (long long row = blockIdx.x; row < r.rows; row += gridDim.x) {
+    __syncthreads();
+    if ((int)threadIdx.x < a.pairs)
+      cs[threadIdx.x] = rope_cos_sin(a, rope_position(a, row, threadIdx.x), a.turn[threadIdx.x]);
+    __syncthreads();
+    for (int u0 = 0; u0 < units; u0 += batch) {
+      uint4 x[kRopeHeld];
+      const int end = min(units, u0 + batch);
+      auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < kRopeHeld; ++i) {
+          const int u = u0 + (int)threadIdx.x + i * kRopeThreads;
+          if (u >= end) continue;
+          const int h = u / chunks, which = h >= r.t[0].heads ? 1 : 0;
+          f(i, r.t[which], (long long)(h - (which ? r.t[0].heads : 0)) * r.head_bytes, u - h * chunks);
+        }
+      };
+      each([&](int i, const RopeTensor& t, long long head, int c) {
+        x[i] = rope_any_chunk<T>(t.in + row * t.in_stride + head, c, a.pairs, interleaved != 0, cs);
+      });
+      __syncthreads();
+      each([&](int i, const RopeTensor& t, long long head, int c) {
+        *reinterpret_cast<uint4*>(t.out + row * t.out_stride + head + c * 16) = x[i];
+      });
+    }
+  }
+}
+
 // Four rows to a block once that still gives every SM two blocks (it quarters the index arithmetic and the loads
 // in flight are what hides the latency); one row to a block below that.
 template <typename T, typename A>
@@ -271,7 +372,10 @@ cudaError_t launch_rope(const A& a, const RopeRows& r, bool interleaved, int sm_
     }
   } else {
     const long long blocks = r.rows < 16LL * sm_count ? r.rows : 16LL * sm_count;
-    rope_rows_kernel<T, A><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
+    if constexpr (std::is_same<A, RopeAxes>::value)
+      rope_any_kernel<T><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
+    else
+      rope_rows_kernel<T><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a, r, interleaved ? 1 : 0);
   }
   return cudaGetLastError();
 }

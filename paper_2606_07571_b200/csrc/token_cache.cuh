@@ -165,17 +165,15 @@ append_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ TokenA
   }
 }
 
-// Any rotated width: one thread per pair (and per dim beyond the rotated ones), element by element, a token at a time.
+// Any rotated width, chunk by chunk as in rope_any_kernel, a token at a time.
 template <typename T, typename A, int kWords>
 __global__ void __launch_bounds__(kRopeThreads)
-append_elements_kernel(const __grid_constant__ A a, const __grid_constant__ TokenArgs g, int interleaved,
-                       const __grid_constant__ ParamList<kWords> list) {
-  using Tr = ElemTraits<T>;
-  constexpr int kEsize = (int)sizeof(T), kPer = Tr::kPerChunk;
+append_any_kernel(const __grid_constant__ A a, const __grid_constant__ TokenArgs g, int interleaved,
+                  const __grid_constant__ ParamList<kWords> list) {
   __shared__ float2 cs[kRopeMaxPairs];
-  const int dims = g.head_bytes / kEsize, rest = dims - 2 * g.pairs;
-  const int per_q = g.q ? g.pairs + (g.q_in_place ? 0 : rest) : 0, per_k = g.pairs + rest;
-  const int q_units = per_q * g.Hq, k_units = per_k * g.Hkv, units = q_units + k_units + dims * g.Hkv;
+  const int chunks = g.head_bytes / 16, batch = kRopeHeld * kRopeThreads / chunks * chunks;     // units of whole heads
+  const int q_heads = g.q ? g.Hq : 0, units = chunks * (q_heads + 2 * g.Hkv);
+  const bool swz = g.swizzled != 0;
   for (int t = blockIdx.x; t < g.tokens; t += gridDim.x) {
     const TokenPlace pl = token_place(g, list.w, a.positions == nullptr, t);
     const bool data = pl.row >= 0;
@@ -183,39 +181,36 @@ append_elements_kernel(const __grid_constant__ A a, const __grid_constant__ Toke
     if (data && (int)threadIdx.x < g.pairs)
       cs[threadIdx.x] = rope_cos_sin(a, rope_position(a, pl.at, threadIdx.x), a.turn[threadIdx.x]);
     __syncthreads();
-    for (int u = threadIdx.x; u < units; u += blockDim.x) {
-      const int which = u < q_units ? 0 : u < q_units + k_units ? 1 : 2;
-      if (which == 0 && !data) continue;
-      const int v = which == 0 ? u : which == 1 ? u - q_units : u - q_units - k_units;
-      const int per = which == 0 ? per_q : which == 1 ? per_k : dims;
-      const int h = v / per, i = v - h * per;
-      const bool turns = which != 2 && i < g.pairs;
-      const int d0 = which == 2 ? i : turns ? (interleaved ? 2 * i : i) : i + g.pairs;
-      const int d1 = turns ? (interleaved ? 2 * i + 1 : i + g.pairs) : d0;
-      const long long head = (long long)h * g.head_bytes;
-      T x0 = T(0.f), x1 = T(0.f);
-      if (data) {
-        const char* const in = (which == 0 ? g.q + pl.row * g.q_stride : (which == 1 ? g.k : g.v) + pl.row * g.kv_stride) + head;
-        x0 = *reinterpret_cast<const T*>(in + d0 * kEsize);
-        if (turns) {
-          const float x = Tr::load(in + d0 * kEsize), y = Tr::load(in + d1 * kEsize);
-          const float2 w = cs[i];
-          Tr::store(reinterpret_cast<char*>(&x0), x * w.x - y * w.y);
-          Tr::store(reinterpret_cast<char*>(&x1), y * w.x + x * w.y);
+    for (int u0 = data ? 0 : chunks * q_heads; u0 < units; u0 += batch) {
+      uint4 x[kRopeHeld];
+      const int end = min(units, u0 + batch);
+      auto each = [&](auto&& f) {                                  // f(held, 0 query 1 key 2 value, head, chunk)
+#pragma unroll
+        for (int i = 0; i < kRopeHeld; ++i) {
+          const int u = u0 + (int)threadIdx.x + i * kRopeThreads;
+          if (u >= end) continue;
+          const int h = u / chunks, which = h < q_heads ? 0 : h < q_heads + g.Hkv ? 1 : 2;
+          f(i, which, h - (which == 0 ? 0 : which == 1 ? q_heads : q_heads + g.Hkv), u - h * chunks);
         }
-      }
-      if (which == 0) {
-        char* const out = g.q_out + pl.row * g.q_out_stride + head;
-        *reinterpret_cast<T*>(out + d0 * kEsize) = x0;
-        if (turns) *reinterpret_cast<T*>(out + d1 * kEsize) = x1;
-      } else {
-        char* const out = (which == 1 ? g.pool_k : g.pool_v) + pl.page + (long long)h * g.page_bytes;
-        for (int s = pl.slot, end = data ? s + 1 : kPageSize; s < end; ++s) {
-          auto at = [&](int d) { return out + page_chunk_offset(g.swizzled != 0, s, d / kPer, g.head_bytes) + d % kPer * kEsize; };
-          *reinterpret_cast<T*>(at(d0)) = x0;
-          if (turns) *reinterpret_cast<T*>(at(d1)) = x1;
+      };
+      each([&](int i, int which, int h, int c) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (!data) return;
+        const char* const head = (which == 0 ? g.q + pl.row * g.q_stride : (which == 1 ? g.k : g.v) + pl.row * g.kv_stride) +
+                                 (long long)h * g.head_bytes;
+        x[i] = which == 2 ? *reinterpret_cast<const uint4*>(head + c * 16)
+                          : rope_any_chunk<T>(head, c, g.pairs, interleaved != 0, cs);
+      });
+      __syncthreads();                                             // queries may be rotated in place
+      each([&](int i, int which, int h, int c) {
+        if (which == 0) {
+          *reinterpret_cast<uint4*>(g.q_out + pl.row * g.q_out_stride + (long long)h * g.head_bytes + c * 16) = x[i];
+        } else {
+          char* const to = (which == 1 ? g.pool_k : g.pool_v) + pl.page + (long long)h * g.page_bytes;
+          for (int s = pl.slot, last = data ? s + 1 : kPageSize; s < last; ++s)
+            *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, s, c, g.head_bytes)) = x[i];
         }
-      }
+      });
     }
   }
 }
@@ -275,7 +270,7 @@ cudaError_t launch_append(const A& a, const TokenArgs& g, bool interleaved, cons
     }
   } else {
     const int blocks = (int)std::min<long long>(g.tokens, 16LL * sm_count);
-    append_elements_kernel<T><<<blocks, kRopeThreads, 0, stream>>>(a, g, interleaved ? 1 : 0, list);
+    append_any_kernel<T><<<blocks, kRopeThreads, 0, stream>>>(a, g, interleaved ? 1 : 0, list);
   }
   return cudaGetLastError();
 }

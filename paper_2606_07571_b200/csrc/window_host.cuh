@@ -640,10 +640,17 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     return run(launches, [&](int n) { return !by_256 || (long long)n * G <= 128; });
   }
   ctx->last_kernel = BICACHE_KERNEL_SIMT;
-  // a row tile of 16 where that holds a request's rows of a KV head, else of 64
+  // A row tile of 16 where that holds a request's rows of a KV head, else of 64; of 16 for all if the call has no more than
+  // two tiles of 64 rows x 64 keys to an SM (such a tile takes 4 us, one of 16 rows a third of that).
+  long long steps = 0;
+  for (int i = 0; i < R; ++i)
+    if (seqlen[i] > 0)
+      steps += ((long long)seqlen[i] * G + 63) / 64 * cfg.num_kv_heads *
+               (1 + window_pages(sinks, left, right, cached_len[i], query_pos[i], query_pos[i] + seqlen[i] - 1).count * kPageSize / kWinKeys);
+  const bool small = steps <= 2LL * ctx->sm_count;
   WindowSimtLaunches few(ctx, a, 16, stream), many(ctx, a, 64, stream);
-  const int st = run(few, [&](int n) { return (long long)n * G <= 16; });
-  return st != BICACHE_OK ? st : run(many, [&](int n) { return (long long)n * G > 16; });
+  const int st = run(few, [&](int n) { return small || (long long)n * G <= 16; });
+  return st != BICACHE_OK ? st : run(many, [&](int n) { return !small && (long long)n * G > 16; });
 }
 
 cudaError_t configure_window(const bicache_config& cfg, bool tensor_ok) {
