@@ -590,10 +590,13 @@ __device__ __forceinline__ int seg_of_row(const ItemInfo* inf, int nseg, int p) 
     if (p >= inf->seg[i].begin && p < inf->seg[i].begin + inf->seg[i].count) k = i;
   return k;
 }
-// The pages `pieces` of a tile of values (bit p: page p, whose source and slots lane p holds) in 16-byte pieces, the slots
-// that no row sees zeroed.  For a converged warp; the pieces have landed when it returns.
-__device__ __forceinline__ void gather_window_pages(unsigned dst, const char* src, const WindowSlots& slots, unsigned pieces,
-                                                    int lane) {
+// The pages `pieces` of a tile of values (bit p: page p, whose source and slots lane p holds) without the slots that no row
+// sees, which become zero: they may hold anything, and 0 times a NaN is a NaN.  A run of slots is contiguous in each of the
+// page image's four blocks (8 slots x 64 dims), so it takes four bulk copies; nobody waits for them.  For a converged warp;
+// returns the bytes to come.
+__device__ __forceinline__ unsigned copy_window_pages(unsigned dst, const char* src, const WindowSlots& slots, unsigned pieces,
+                                                      unsigned bar, int lane) {
+  unsigned bytes = 0;
 #pragma unroll 1
   for (unsigned left = pieces; left != 0; left &= left - 1) {
     const int p = __ffs(left) - 1;
@@ -603,16 +606,24 @@ __device__ __forceinline__ void gather_window_pages(unsigned dst, const char* sr
     sl.lo = __shfl_sync(0xffffffffu, slots.lo, p);
     sl.hi = __shfl_sync(0xffffffffu, slots.hi, p);
     sl.sink = __shfl_sync(0xffffffffu, slots.sink, p);
-    // the page image in order: two halves of 8 slots, each two blocks of 64 dims with 128 bytes a slot
+    // two halves of 8 slots, in each two blocks of 64 dims with 128 bytes a slot
 #pragma unroll
     for (int i = 0; i < kPageBytes / 512; ++i) {
       const unsigned at = (unsigned)(i * 512 + lane * 16);
-      cp_async16(dst + p * kPageBytes + at, from + at, sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))) ? 16u : 0u);
+      if (!sl.has((int)((at >> 11) * 8 + ((at & 1023u) >> 7))))
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + p * kPageBytes + at), "r"(0u) : "memory");
     }
+    // lane: run of slots (the first tokens', the window's behind them), half, block
+    const int g = (lane >> 1) & 1;
+    const int first = (lane >> 2) ? max(max(sl.lo, sl.sink), 8 * g) : 8 * g;
+    const int last = min((lane >> 2) ? sl.hi : sl.sink, 8 * g + 8);
+    const unsigned mine = lane < 8 && last > first ? (unsigned)(last - first) * 128u : 0u;
+    const unsigned at = (unsigned)(g * 2048 + (lane & 1) * 1024 + (first - 8 * g) * 128);
+    if (mine) bulk_copy_g2s(dst + p * kPageBytes + at, from + at, mine, bar);
+    bytes += __reduce_add_sync(0xffffffffu, mine);
   }
-  cp_async_commit();
-  cp_async_wait<0>();
-  fence_proxy_async();
+  fence_proxy_async();                       // the zeros, for the MMA
+  return bytes;
 }
 // the first x of 32 bits
 __device__ __forceinline__ unsigned low_bits(int x) { return x >= 32 ? ~0u : x <= 0 ? 0u : (1u << x) - 1u; }
@@ -1271,9 +1282,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       const int kv_head = inf->kv_head;
       const int* pages = s.pages + inf->page_off;
       if constexpr (kWindow) {
-        // Key tiles of the item's page sequence, 8 pages each.  A page of values in which no row of the item sees some slots
-        // is gathered in 16-byte pieces with these zeroed (they may hold anything, and 0 times a NaN is a NaN); all others
-        // come by one bulk copy.
+        // Key tiles of the item's page sequence, 8 pages each: one bulk copy per page, but for pages of values of which no row
+        // of the item sees some slots.
         const WindowInfo& wi = bars->window[n_it & 1];
         const WindowPages wp = wi.pages;
         const WindowReq& rq = reinterpret_cast<const WindowReq*>(win.list.w)[wi.req];
@@ -1299,10 +1309,11 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
           if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
           const unsigned pieces = ~bulks & ((1u << npages) - 1u);
-          if (pieces != 0) gather_window_pages(dst, src, sl, pieces, lane);
+          unsigned bytes = __popc(bulks) * kPageBytes;
+          if (pieces != 0) bytes += copy_window_pages(dst, src, sl, pieces, full, lane);
           // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
           if (lane == 0) {
-            mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
+            mbar_arrive_expect_tx(full, bytes);
             armed[slot] = u;
           } else {
             mbar_arrive(full);

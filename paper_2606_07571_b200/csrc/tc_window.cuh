@@ -10,8 +10,8 @@
 //     does not see in full is masked with the bits of a 64-bit word, and a row that has seen nothing yet keeps -inf as
 //     its reference and 0 for it in the exponent;
 //   - slots that no row of the item sees may hold anything.  Their scores are masked one way or another; as values they would
-//     meet weight 0, and 0 times a NaN is a NaN: a page of values with such slots is gathered in 16-byte pieces with
-//     these zeroed, where whole pages come by one bulk copy;
+//     meet weight 0, and 0 times a NaN is a NaN: a page of values with such slots comes by a copy per run of seen slots, the
+//     others zeroed, where whole pages come by one bulk copy;
 //   - an item that has all the keys of its rows writes the output itself, in bf16; ranges write normalised partial
 //     results for window_join_kernel.
 #pragma once
@@ -71,10 +71,11 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
     if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
     const unsigned pieces = ~bulks & ((1u << npages) - 1u);
-    if (pieces != 0) gather_window_pages(dst, src, slots, pieces, lane);
+    unsigned bytes = __popc(bulks) * kPageBytes;
+    if (pieces != 0) bytes += copy_window_pages(dst, src, slots, pieces, full, lane);
     // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
     if (lane == 0) {
-      mbar_arrive_expect_tx(full, (unsigned)(__popc(bulks) * kPageBytes));
+      mbar_arrive_expect_tx(full, bytes);
       armed[b] = j;
     } else {
       mbar_arrive(full);
@@ -359,7 +360,6 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
       ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
       if (ok) load_tile(j);
     }
-    cp_async_wait<0>();
     // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
     if ((!ok || *abort_flag) && lane == 0) {
       for (int b = 0; b < stages; ++b)

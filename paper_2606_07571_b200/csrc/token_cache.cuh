@@ -165,53 +165,58 @@ append_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ TokenA
   }
 }
 
-// Any rotated width, chunk by chunk as in rope_any_kernel, a token at a time.
-template <typename T, typename A, int kWords>
+// Any rotated width, chunk by chunk as in rope_any_kernel; kRows tokens at a time, so that a batch fills the block also
+// where there are few heads.
+template <typename T, typename A, int kRows, int kWords>
 __global__ void __launch_bounds__(kRopeThreads)
 append_any_kernel(const __grid_constant__ A a, const __grid_constant__ TokenArgs g, int interleaved,
                   const __grid_constant__ ParamList<kWords> list) {
-  __shared__ float2 cs[kRopeMaxPairs];
+  __shared__ float2 cs[kRows][kRopeMaxPairs];
+  __shared__ TokenPlace place[kRows];
   const int chunks = g.head_bytes / 16, batch = kRopeHeld * kRopeThreads / chunks * chunks;     // units of whole heads
-  const int q_heads = g.q ? g.Hq : 0, units = chunks * (q_heads + 2 * g.Hkv);
+  const int q_heads = g.q ? g.Hq : 0, per_token = chunks * (q_heads + 2 * g.Hkv);
   const bool swz = g.swizzled != 0;
-  for (int t = blockIdx.x; t < g.tokens; t += gridDim.x) {
-    const TokenPlace pl = token_place(g, list.w, a.positions == nullptr, t);
-    const bool data = pl.row >= 0;
-    __syncthreads();
-    if (data && (int)threadIdx.x < g.pairs)
-      cs[threadIdx.x] = rope_cos_sin(a, rope_position(a, pl.at, threadIdx.x), a.turn[threadIdx.x]);
-    __syncthreads();
-    for (int u0 = data ? 0 : chunks * q_heads; u0 < units; u0 += batch) {
-      uint4 x[kRopeHeld];
-      const int end = min(units, u0 + batch);
-      auto each = [&](auto&& f) {                                  // f(held, 0 query 1 key 2 value, head, chunk)
+  const int t0 = blockIdx.x * kRows, rows = min(kRows, g.tokens - t0), units = rows * per_token;
+  if ((int)threadIdx.x < rows) place[threadIdx.x] = token_place(g, list.w, a.positions == nullptr, t0 + threadIdx.x);
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * g.pairs; i += kRopeThreads) {
+    const int row = i / g.pairs, pair = i - row * g.pairs;
+    if (place[row].row >= 0) cs[row][pair] = rope_cos_sin(a, rope_position(a, place[row].at, pair), a.turn[pair]);
+  }
+  __syncthreads();
+  for (int u0 = 0; u0 < units; u0 += batch) {
+    uint4 x[kRopeHeld];
+    const int end = min(units, u0 + batch);
+    auto each = [&](auto&& f) {                                    // f(held, token, 0 query 1 key 2 value, head, chunk)
 #pragma unroll
-        for (int i = 0; i < kRopeHeld; ++i) {
-          const int u = u0 + (int)threadIdx.x + i * kRopeThreads;
-          if (u >= end) continue;
-          const int h = u / chunks, which = h < q_heads ? 0 : h < q_heads + g.Hkv ? 1 : 2;
-          f(i, which, h - (which == 0 ? 0 : which == 1 ? q_heads : q_heads + g.Hkv), u - h * chunks);
-        }
-      };
-      each([&](int i, int which, int h, int c) {
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (!data) return;
-        const char* const head = (which == 0 ? g.q + pl.row * g.q_stride : (which == 1 ? g.k : g.v) + pl.row * g.kv_stride) +
-                                 (long long)h * g.head_bytes;
-        x[i] = which == 2 ? *reinterpret_cast<const uint4*>(head + c * 16)
-                          : rope_any_chunk<T>(head, c, g.pairs, interleaved != 0, cs);
-      });
-      __syncthreads();                                             // queries may be rotated in place
-      each([&](int i, int which, int h, int c) {
-        if (which == 0) {
-          *reinterpret_cast<uint4*>(g.q_out + pl.row * g.q_out_stride + (long long)h * g.head_bytes + c * 16) = x[i];
-        } else {
-          char* const to = (which == 1 ? g.pool_k : g.pool_v) + pl.page + (long long)h * g.page_bytes;
-          for (int s = pl.slot, last = data ? s + 1 : kPageSize; s < last; ++s)
-            *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, s, c, g.head_bytes)) = x[i];
-        }
-      });
-    }
+      for (int i = 0; i < kRopeHeld; ++i) {
+        const int u = u0 + (int)threadIdx.x + i * kRopeThreads;
+        if (u >= end) continue;
+        const int row = kRows == 1 ? 0 : u / per_token, v = u - row * per_token;
+        const int h = v / chunks, which = h < q_heads ? 0 : h < q_heads + g.Hkv ? 1 : 2;
+        f(i, row, which, h - (which == 0 ? 0 : which == 1 ? q_heads : q_heads + g.Hkv), v - h * chunks);
+      }
+    };
+    each([&](int i, int row, int which, int h, int c) {
+      const TokenPlace& pl = place[row];
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (pl.row < 0) return;
+      const char* const head = (which == 0 ? g.q + pl.row * g.q_stride : (which == 1 ? g.k : g.v) + pl.row * g.kv_stride) +
+                               (long long)h * g.head_bytes;
+      x[i] = which == 2 ? *reinterpret_cast<const uint4*>(head + c * 16)
+                        : rope_any_chunk<T>(head, c, g.pairs, interleaved != 0, cs[row]);
+    });
+    __syncthreads();                                               // queries may be rotated in place
+    each([&](int i, int row, int which, int h, int c) {
+      const TokenPlace& pl = place[row];
+      if (which == 0) {
+        if (pl.row >= 0) *reinterpret_cast<uint4*>(g.q_out + pl.row * g.q_out_stride + (long long)h * g.head_bytes + c * 16) = x[i];
+      } else {
+        char* const to = (which == 1 ? g.pool_k : g.pool_v) + pl.page + (long long)h * g.page_bytes;
+        for (int s = pl.slot, last = pl.row >= 0 ? s + 1 : kPageSize; s < last; ++s)
+          *reinterpret_cast<uint4*>(to + page_chunk_offset(swz, s, c, g.head_bytes)) = x[i];
+      }
+    });
   }
 }
 
@@ -269,8 +274,12 @@ cudaError_t launch_append(const A& a, const TokenArgs& g, bool interleaved, cons
       else append_chunks_kernel<T, false, 1><<<blocks, threads, 0, stream>>>(a, g, list);
     }
   } else {
-    const int blocks = (int)std::min<long long>(g.tokens, 16LL * sm_count);
-    append_any_kernel<T><<<blocks, kRopeThreads, 0, stream>>>(a, g, interleaved ? 1 : 0, list);
+    // as many tokens as make a batch, once that still gives every SM eight blocks
+    const int units = g.head_bytes / 16 * ((g.q ? g.Hq : 0) + 2 * g.Hkv);
+    if (units <= kRopeHeld * kRopeThreads / 4 && g.tokens >= 64LL * sm_count)
+      append_any_kernel<T, A, 8><<<(unsigned)((g.tokens + 7LL) / 8), kRopeThreads, 0, stream>>>(a, g, interleaved ? 1 : 0, list);
+    else
+      append_any_kernel<T, A, 1><<<(unsigned)g.tokens, kRopeThreads, 0, stream>>>(a, g, interleaved ? 1 : 0, list);
   }
   return cudaGetLastError();
 }

@@ -559,24 +559,32 @@ window_join_kernel(const __grid_constant__ WindowArgs a, int row_heads, const in
   const int at = rh - r.row_heads_before, t = at / a.Hq, h = at - t * a.Hq;
   const long long stride = (long long)r.n * a.Hq, p0 = r.part_off + at;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (status && *status != kDevOk) return;                         // some ranges were not computed
+  // everything is requested before anything is used: the first ranges' rows, the status, the log-sum-exps
+  constexpr int kStep = kWarps == 1 ? 1 : kJoinWarps;
+  const int s_first = kWarps == 1 ? 0 : warp;
+  float4 v[8];
+  auto load = [&](int s0, int d) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (d < a.D && s0 + u * kStep < r.splits)
+        v[u] = *reinterpret_cast<const float4*>(a.part_o + (p0 + (s0 + u * kStep) * stride) * a.D + d);
+  };
+  load(s_first, lane * 4);
+  const int state = status ? *status : kDevOk;
   const float l0 = lane < r.splits ? a.part_lse[p0 + lane * stride] : -INFINITY;
   const float l1 = lane + 32 < r.splits ? a.part_lse[p0 + (lane + 32) * stride] : -INFINITY;
+  if (state != kDevOk) return;                                     // some ranges were not computed
   const float mx = warp_max(fmaxf(l0, l1));
   const bool any = mx > -INFINITY || __any_sync(0xffffffffu, l0 != l0 || l1 != l1);      // a NaN spreads
   const float w0 = any ? expf(l0 - mx) : 0.f, w1 = any ? expf(l1 - mx) : 0.f;
   const float total = warp_sum(w0 + w1), inv = any ? 1.f / total : 0.f;
   const long long row = r.row + t;
-  constexpr int kStep = kWarps == 1 ? 1 : kJoinWarps;
   for (int d0 = 0; d0 < a.D; d0 += 128) {
     const int d = d0 + lane * 4;
     const bool mine = d < a.D;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = kWarps == 1 ? 0 : warp; s0 < r.splits; s0 += 8 * kStep) {
-      float4 v[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (mine) v[u] = *reinterpret_cast<const float4*>(a.part_o + (p0 + min(s0 + u * kStep, r.splits - 1) * stride) * a.D + d);
+    for (int s0 = s_first; s0 < r.splits; s0 += 8 * kStep) {
+      if (d0 > 0 || s0 > s_first) load(s0, d);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int s = s0 + u * kStep;

@@ -266,8 +266,9 @@ static_assert(sizeof(WindowArgs) + 64 + 4 * kParamWords <= 32764, "launch parame
 struct WindowForm {
   int tile_rows, tile_keys;
   int slots;                    // work items that run at a time
-  int item_cost;                // start and end of a work item
-  int join_cost;                // the joining kernel
+  double item_cost;             // start and end of a work item
+  double join_cost;             // the joining kernel, and what it takes for a row-head of a range
+  double join_row_head_cost;
   int max_splits;               // ranges of keys
   int list_words;               // what a launch's list holds
 };
@@ -416,7 +417,7 @@ class WindowLaunches {
       if (s > 1 && items > 4LL * form_.slots) break;         // enough to even out: more would only start more often
       const double longest = tps + form_.item_cost;
       const double mean = (double)(tiles + items * form_.item_cost) / form_.slots;
-      const double cost = (items <= form_.slots ? longest : std::max(longest, mean + longest / 2)) + (part > 0 ? form_.join_cost : 0);
+      const double cost = (items <= form_.slots ? longest : std::max(longest, mean + longest / 2)) + (part > 0 ? form_.join_cost + form_.join_row_head_cost * part : 0.0);
       if (cost < best) {
         best = cost;
         best_tps = tps;
@@ -477,7 +478,7 @@ class WindowSimtLaunches : public WindowLaunches {
 
  protected:
   static WindowForm form_of(const bicache_ctx* ctx, int rows) {
-    return WindowForm{rows, kWinKeys, window_simt_blocks(rows, ctx->cfg.head_dim) * ctx->sm_count, 2, 2, kMaxWindowSplits, kParamWords};
+    return WindowForm{rows, kWinKeys, window_simt_blocks(rows, ctx->cfg.head_dim) * ctx->sm_count, 2, 2, 1e-4, kMaxWindowSplits, kParamWords};
   }
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
     const size_t smem = window_simt_smem(form_.tile_rows, a.D);
@@ -495,7 +496,7 @@ class WindowSimtLaunches : public WindowLaunches {
 class WindowTensorLaunches : public WindowLaunches {
  public:
   WindowTensorLaunches(bicache_ctx* ctx, const WindowArgs& args, cudaStream_t stream)
-      : WindowLaunches(ctx, args, WindowForm{128, dec::kKeys, 2 * ctx->sm_count, 4, 4, kMaxWindowSplits, kParamWords}, stream) {}
+      : WindowLaunches(ctx, args, WindowForm{128, dec::kKeys, 2 * ctx->sm_count, 4, 5, 2e-4, kMaxWindowSplits, kParamWords}, stream) {}
 
  protected:
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
@@ -512,7 +513,7 @@ class WindowTensorLaunches : public WindowLaunches {
 class WindowTileLaunches : public WindowLaunches {
  public:
   WindowTileLaunches(bicache_ctx* ctx, const WindowArgs& args, const TcTensorMaps& maps, cudaStream_t stream)
-      : WindowLaunches(ctx, args, WindowForm{kTileRows, kTileKeys, ctx->sm_count, 0, 0, 1, kWindowTileWords}, stream), maps_(maps) {}
+      : WindowLaunches(ctx, args, WindowForm{kTileRows, kTileKeys, ctx->sm_count, 0, 0, 0, 1, kWindowTileWords}, stream), maps_(maps) {}
 
  protected:
   cudaError_t launch(const WindowArgs& a, const int* list, int words) override {
@@ -615,9 +616,11 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   // the tensor-core kernel takes the row maximum before scaling, which needs a positive scale
   if (ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && softmax_scale > 0.f) {
     // Requests with more than 128 packed rows go through the kernel with row tiles of 256, which shares every key tile
-    // between two tiles of 128 rows, if there are three of them to an SM; it does not split the keys.  (28 query heads, window
-    // of 500 + 201: 224 items take 71 us, as ranges and tiles of 128 rows 59; 32 query heads, window of 1023: 512 items take
-    // 114 us against 122, 2048 items 406 against 436.)
+    // between two tiles of 128 rows, if there are three of them to an SM and the query heads of a KV head divide 128 (else
+    // one warp gathers the query tiles, and short items wait for it); it does not split the keys.  Both sides measured: 32
+    // query heads, 16,384 rows, window of 4096: 865 us, as tiles of 128 rows 920; window of 1024: 407 and 425; 8 KV heads,
+    // 4096 rows, window of 1024 (512 items): 111 and 115.  28 query heads, window of 500 + 201: 224 items 71 us against 57, 550
+    // items 115 against 102.
     long long tiles = 0, rows_total = 0;
     for (int i = 0; i < R; ++i) {
       rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
@@ -627,7 +630,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     std::memset(&maps, 0, sizeof(maps));
     maps.q_tma = (128 % G == 0) ? 1 : 0;
     maps.o_tma = (32 % G == 0) ? 1 : 0;
-    const bool by_256 = tiles >= 3LL * ctx->sm_count && rows_total < 0x7fffffffLL &&              // box coordinates are 32-bit
+    const bool by_256 = tiles >= 3LL * ctx->sm_count && maps.q_tma && rows_total < 0x7fffffffLL &&              // box coordinates are 32-bit
                         encode_map(&maps.q, q, rows_total, cfg.num_q_heads, q_row_stride, maps.q_tma ? G : 1, maps.q_tma ? 128 / G : 128) &&
                         encode_map(&maps.o, out, rows_total, cfg.num_q_heads, out_row_stride, maps.o_tma ? G : 1, maps.o_tma ? 32 / G : 32);
     ctx->last_kernel = by_256 ? BICACHE_KERNEL_TENSOR : BICACHE_KERNEL_KEY_RANGES;
