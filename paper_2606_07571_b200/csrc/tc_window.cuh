@@ -46,8 +46,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   auto tile_of = [&](int j) { return window_tile(it.start, it.tile_begin, it.tile_end, j); };
   auto tile_pages = [&](int j) { return min(kKeys / kPageSize, it.pages.count - tile_of(j) * (kKeys / kPageSize)); };
 
-  // Set-up, all of it side by side: warps 0-3 request the Q tile, thread 0 sets flags and barriers, warp 4 fetches TMEM, warps 5
-  // and 6 set their own barriers and issue the first tiles, for which they need nobody.
+  // Set-up, all of it side by side: warps 0-3 request the Q tile, warp 4 sets flags and barriers and fetches TMEM, warps
+  // 5 and 6 set their own barriers and issue the first tiles, for which they need nobody.
   const int is_v = warp - 5;
   const int stages = is_v ? kVStages : kKStages;
   int armed[kKStages] = {-1, -1, -1};        // load warps: the last tile armed with bulk copies, per stage
@@ -97,32 +97,11 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     begun = status_now == 0 && (q_smem & 1023u) == 0;
     if (begun)
       for (int j = 0; j < ahead; ++j) load_tile(j);
-    asm volatile("barrier.cta.sync 2, 96;" ::: "memory");          // the flags that thread 0 sets
+    asm volatile("barrier.cta.sync 2, 96;" ::: "memory");          // the flags that warp 4 sets
     dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
   } else {
     if (warp == 4) {
-      tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
-      tmem_relinquish();
-    } else {
-      if (warp < active && T > 0) {
-        // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i.
-        // Rows past the end stay what they are: a row of Q meets no other row's results.
-        const int c16 = lane & 15, here = min(32, rows - warp * 32);
-        const char* const q_head = a.q + (r.row * a.q_stride + (long long)it.hk * G * 128) * 2 + c16 * 16;
-        const int prow = it.row0 + warp * 32 + (lane >> 4);
-        int t = prow / G, jj = prow - t * G;
-#pragma unroll 4
-        for (int i = lane >> 4; i < here; i += 2) {
-          cp_async16(q_smem + tile_chunk_offset(warp * 32 + i, c16), q_head + ((long long)t * a.q_stride + jj * 128) * 2, 16u);
-          jj += 2;
-          while (jj >= G) {                         // at most twice (G >= 1)
-            jj -= G;
-            ++t;
-          }
-        }
-        cp_async_commit();
-      }
-      if (tid == 0) {
+      if (lane == 0) {
         sy->wait_cycles = wait_cycles;
         if ((q_smem & 1023u) != 0) atomicCAS(status, kDevOk, kDevInternal);
         sy->dead = status_now != 0 || (q_smem & 1023u) != 0 ? 1 : 0;
@@ -138,7 +117,35 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
         fence_barrier_init();
       }
       __syncwarp();
-      if (warp == 0) asm volatile("barrier.cta.arrive 2, 96;" ::: "memory");
+      asm volatile("barrier.cta.arrive 2, 96;" ::: "memory");
+      tmem_alloc(smem_u32(&sy->tmem_base), kDecTmemCols);
+      tmem_relinquish();
+    } else {
+      if (warp < active && T > 0) {
+        // The Q tile: warp w fetches rows 32 w .. 32 w + 31, lane l the 16-byte chunk (l & 15) of rows 32 w + (l >> 4) + 2 i.
+        // Rows past the end stay what they are: a row of Q meets no other row's results.
+        const int c16 = lane & 15, r0 = lane >> 4, here = min(32, rows - warp * 32);
+        const int prow = it.row0 + warp * 32 + r0, t = prow / G;
+        int jj = prow - t * G;
+        // two packed rows on: two heads, and from one token's last to the next's first at most once
+        const int step = G == 1 ? 0 : 2;
+        const long long step_bytes = G == 1 ? 4 * a.q_stride : 512, wrap_bytes = a.q_stride * 2 - G * 256;
+        const char* src = a.q + ((r.row + t) * a.q_stride + (long long)(it.hk * G + jj) * 128) * 2 + c16 * 16;
+        unsigned dst[4];                             // of rows r0 + 2 i, i < 4; 8 rows on: 2048 bytes
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[i] = q_smem + tile_chunk_offset(warp * 32 + r0 + 2 * i, c16);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (r0 + 2 * i < here) cp_async16(dst[i & 3] + (i >> 2) * 2048, src, 16u);
+          jj += step;
+          src += step_bytes;
+          if (jj >= G) {
+            jj -= G;
+            src += wrap_bytes;
+          }
+        }
+        cp_async_commit();
+      }
     }
     tc_fence_before();
     asm volatile("barrier.cta.sync 1, 224;" ::: "memory");
@@ -254,47 +261,57 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
         const bool whole = r.splits == 1;
         const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
         const float lse = l_sum == 0.f ? -INFINITY : (m_ref + log2f(l_sum)) * 0.6931471805599453f;
-        // A thread holds a row (128 values).  It goes to shared memory first (the K/V rings are free by now: every tile has been
-        // consumed; rows 528 bytes apart keep the 16-byte stores conflict-free) and leaves as one bulk copy.
-        unsigned char* const stage_row = smem + kQBytes + row * 528;
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          unsigned o[32];
-          if (T > 0) {
-            tmem_ld32(tmem_o + c * 32 + lane_base, o);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = 0u;
-          }
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint4 v;
-              v.x = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-              v.y = pack_bf16(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-              v.z = pack_bf16(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-              v.w = pack_bf16(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-              *reinterpret_cast<uint4*>(stage_row + (c * 32 + i) * 2) = v;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<float4*>(stage_row + (c * 32 + i) * 4) =
-                  make_float4(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv,
-                              __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-          }
-        }
-        fence_proxy_async();
         if (mine) {
-          const void* const dst = whole ? (const void*)(a.out + (out_row * a.out_stride + (long long)w.h * 128) * 2)
-                                        : (const void*)(a.part_o + at * 128);
-          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                       ::"l"(dst), "r"(smem_u32(stage_row)), "r"(whole ? 256u : 512u) : "memory");
-          bulk_commit_group();
           if (!whole) a.part_lse[at] = lse;
           else if (a.lse) a.lse[out_row * a.Hq + w.h] = lse;
-          bulk_wait_read();                                        // the rows have left shared memory
+        }
+        // A thread holds a row (128 values).  It goes to shared memory first (the K/V rings are free by now: every tile has been
+        // consumed; rows 272 bytes apart keep the 16-byte stores conflict-free), half a row at a time if it is a partial
+        // result; then the warp writes whole rows.  (A bulk copy per row took three times as long.)
+        unsigned char* const stage = smem + kQBytes + warp * 32 * 272;
+        char* const mine_to = whole ? a.out + (out_row * a.out_stride + (long long)w.h * 128) * 2 : reinterpret_cast<char*>(a.part_o + at * 128);
+        const int here = min(32, rows - warp * 32);
+#pragma unroll 1
+        for (int half = 0; half < (whole ? 1 : 2); ++half) {
+#pragma unroll 1
+          for (int c = 0; c < (whole ? 2 : 1); ++c) {
+            unsigned o[64];
+            if (T > 0) {
+              tmem_ld32(tmem_o + (half + c) * 64 + lane_base, o);
+              tmem_ld32(tmem_o + (half + c) * 64 + 32 + lane_base, o + 32);
+              tmem_wait_ld();
+            } else {
+#pragma unroll
+              for (int i = 0; i < 64; ++i) o[i] = 0u;
+            }
+            if (whole) {
+#pragma unroll
+              for (int i = 0; i < 64; i += 8) {
+                uint4 v;
+                v.x = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                v.y = pack_bf16(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                v.z = pack_bf16(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                v.w = pack_bf16(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                *reinterpret_cast<uint4*>(stage + lane * 272 + (c * 64 + i) * 2) = v;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 64; i += 4)
+                *reinterpret_cast<float4*>(stage + lane * 272 + i * 4) =
+                    make_float4(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv,
+                                __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+            }
+          }
+          __syncwarp();
+          // 256 bytes a row, two rows at a time
+#pragma unroll 4
+          for (int i = lane >> 4; i < 32; i += 2) {
+            char* const to = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine_to), i));
+            if (i < here)
+              *reinterpret_cast<uint4*>(to + half * 256 + (lane & 15) * 16) =
+                  *reinterpret_cast<const uint4*>(stage + i * 272 + (lane & 15) * 16);
+          }
+          __syncwarp();
         }
       }
       tc_fence_before();
