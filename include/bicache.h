@@ -486,7 +486,7 @@ int32_t bicache_rope_axes_table(bicache_ctx* ctx, int64_t rows, const bicache_ro
  * position is its index in the prefix.
  * q, q_out: device, rows [Hq][D], or both NULL: the queries of the same rows, rotated to the same positions in the same
  * launch; rows that belong to no request are left as they are.  q_out may be q itself with the same stride, else must
- * not overlap an input.
+ * not overlap an input.  With queries, a row belongs to one request; keys and values alone may go to several.
  * NOTFOUND for an unknown or evicted id; INVALID for tokens past the end of the prefix, a layer that it does not own,
  * queries without a rotation, bad pointers, strides or rotations. */
 int32_t bicache_append_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
@@ -496,7 +496,8 @@ int32_t bicache_append_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const 
                               int64_t position_axis_stride, void* stream);
 
 /* The way back: token token_off[i] + a of prefix prefix_id[i] to row row_off[i] + a of k_out and v_out, bit-exact.
- * Tokens may be read more than once.  Arguments and errors as for bicache_append_tokens. */
+ * Tokens may be read more than once, a row is written once (INVALID).  Arguments and errors as for
+ * bicache_append_tokens. */
 int32_t bicache_read_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
                             const int32_t* token_off, const int64_t* row_off, const int32_t* seqlen, void* k_out,
                             void* v_out, int64_t kv_row_stride, void* stream);
@@ -512,12 +513,18 @@ int32_t bicache_read_tokens(bicache_ctx* ctx, int32_t layer, int32_t R, const in
  *   cached_len[i]  tokens that are there, 0 .. the prefix's length; what lies behind them is not read as a number.
  *   query_pos[i]   position of the first row, >= 0; rows may stand behind the cached tokens.
  *   row_off[i], seqlen[i], q, out, their strides, lse_out, softmax_scale: as for bicache_attend; lse_out is over the visible
- * tokens.  A row that sees no token gets out = 0 and lse = -inf.  Rows that belong to no request are left as they are.
+ * tokens.  A row belongs to one request (INVALID).  A row that sees no token gets out = 0 and lse = -inf.  Rows that belong
+ * to no request are left as they are.  bf16 with head_dim 128 and a positive scale runs on the tensor cores, where weights
+ * are rounded to bf16 before they meet the values; sums are fp32, their order is fixed: the same call gives the same bits.
+ * bicache_last_attention_kernel answers KERNEL_TENSOR for row tiles of 256 (many rows), KERNEL_KEY_RANGES for row tiles of
+ * 128 and ranges of keys, KERNEL_SIMT for the CUDA cores.  A tensor-core call that finds the device status raised
+ * leaves its outputs as they are.
  * A stored value that is not finite spreads to the rows that see its token, and may spread to others of the same request; a
  * token that no row of the request sees has no effect, whatever it holds.
  * Uses the context's workspace as scratch: two calls, or replays of graphs that hold such calls, must not overlap.
  * NOTFOUND for an unknown or evicted id; INVALID for negative sizes, left or right below -1, cached_len beyond the
- * prefix, a scale that is not finite, out being q, bad pointers or strides. */
+ * prefix, a scale that is not finite, out being q (other overlap of the two is not looked for, and not allowed), bad
+ * pointers or strides. */
 int32_t bicache_attend_window(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* prefix_id,
                               const int32_t* cached_len, const int32_t* query_pos, const int64_t* row_off,
                               const int32_t* seqlen, const void* q, int64_t q_row_stride, void* out,
@@ -586,7 +593,7 @@ int64_t bicache_schedule_uploads(const bicache_ctx* ctx);
  * 0 none yet; BICACHE_KERNEL_SIMT the CUDA-core kernel (fp32, head dims other than 128, forced);
  * BICACHE_KERNEL_TENSOR the tensor-core kernel over two 128-row query tiles per work item;
  * BICACHE_KERNEL_KEY_RANGES the tensor-core kernel for few query rows against a long cached prefix
- * (bicache_attend only; chosen when every request has a cached prefix of at least 1024 tokens and at
+ * (for bicache_attend, and see bicache_attend_window; there chosen when every request has a cached prefix of at least 1024 tokens and at
  * most 128 * Hkv / Hq suffix tokens, and the call is small enough for the kernel's tables): the group's
  * rows share tiles, the prefix keys are split into ranges over the CTAs, each request's own keys are
  * one more range, and a merge kernel applies the log-sum-exp merge (exact up to rounding);

@@ -225,20 +225,27 @@ def _host(a, code):
     return a, address, n
 
 
+_PACK = {(n, code): struct.Struct("%d%s" % (n, code)).pack for n in range(65) for code in "iq"}
+
+
 def _host_list(a, code):
-    """_host for the calls that take a list entry per request: struct.pack converts long lists a third faster."""
+    """_host for the calls that take an entry per request, as (bytes, length): packing converts a list in two thirds of
+    the time, a short one in half."""
     if isinstance(a, np.ndarray):
-        return _host(a, code)
+        a = np.ascontiguousarray(a, dtype=_TYPE_CODES[code])
+        return a.tobytes(), a.size
     n = len(a)
-    packed = struct.pack("%d%s" % (n, code), *a)
-    return packed, packed, n
+    return (_PACK[n, code](*a) if n <= 64 else struct.pack("%d%s" % (n, code), *a)), n
 
 
-def _rows_within(off, n, count, rows):
-    """Does no run of rows, packed by _host_list, end past `rows`?"""
-    if count > 8:
+def _rows_within(row_off, seqlen, off, n, rows):
+    """Does no run of rows end past `rows`?  off, n: row_off and seqlen as _host_list packs them."""
+    if len(n) > 32:
         return int((np.frombuffer(off, np.int64) + np.frombuffer(n, np.int32)).max()) <= rows
-    return all(o + k <= rows for o, k in zip(struct.unpack("%dq" % count, off), struct.unpack("%di" % count, n)))
+    for o, k in zip(row_off, seqlen):
+        if o + k > rows:
+            return False
+    return True
 
 
 # torch.cuda.current_stream builds a Stream object (2 us); the bare handle is what the library takes
@@ -622,17 +629,17 @@ class BiCache:
     # -- a cache that grows -------------------------------------------------------------------
     def _token_args(self, prefix_id, token_off, row_off, seqlen, k, v):
         """Number of requests, the host arrays of a batch of tokens, rows of the tensors and their stride."""
-        _, ppid, count = _host_list(prefix_id, "i")
-        _, ptok, n_tok = _host_list(token_off, "i")
-        _, poff, n_off = _host_list(row_off, "q")
-        _, pn, n_len = _host_list(seqlen, "i")
+        ppid, count = _host_list(prefix_id, "i")
+        ptok, n_tok = _host_list(token_off, "i")
+        poff, n_off = _host_list(row_off, "q")
+        pn, n_len = _host_list(seqlen, "i")
         assert count == n_tok == n_off == n_len
         dtype, device = self.dtype, self.device
         assert k.dtype == v.dtype == dtype and k.device == v.device == device, "%s tensors on %s are needed" % (dtype, device)
         (rows, heads, d), strides = k.shape, k.stride()
         assert v.shape == k.shape and v.stride() == strides and heads == self.Hkv and d == self.D
         assert strides[2] == 1 and strides[1] == d
-        assert _rows_within(poff, pn, count, rows), "a request's rows reach past the tensors"
+        assert _rows_within(row_off, seqlen, poff, pn, rows), "a request's rows reach past the tensors"
         return count, ppid, ptok, poff, pn, rows, strides[0]
 
     def append_tokens(self, layer, prefix_id, token_off, row_off, seqlen, k, v, q=None, q_out=None, rotation=None,
@@ -659,15 +666,15 @@ class BiCache:
                       right=-1, scale=None):
         """Rows row_off[i] .. + seqlen[i] of q [rows, Hq, D], at positions query_pos[i] .., attend over the tokens
         t < cached_len[i] of prefix prefix_id[i] with t <= p + right and (t < sinks or t >= p - left); -1: no bound."""
-        _, ppid, count = _host_list(prefix_id, "i")
-        _, pcl, n_cl = _host_list(cached_len, "i")
-        _, pqp, n_qp = _host_list(query_pos, "i")
-        _, poff, n_off = _host_list(row_off, "q")
-        _, pn, n_len = _host_list(seqlen, "i")
+        ppid, count = _host_list(prefix_id, "i")
+        pcl, n_cl = _host_list(cached_len, "i")
+        pqp, n_qp = _host_list(query_pos, "i")
+        poff, n_off = _host_list(row_off, "q")
+        pn, n_len = _host_list(seqlen, "i")
         assert count == n_cl == n_qp == n_off == n_len
         q_at, q_row, out_at, out_row = self._rope_pair(q, out, self.Hq)
         rows = q.shape[0]
-        assert _rows_within(poff, pn, count, rows), "a request's rows reach past q"
+        assert _rows_within(row_off, seqlen, poff, pn, rows), "a request's rows reach past q"
         lp = None
         if lse is not None:
             self._own(lse, torch.float32)

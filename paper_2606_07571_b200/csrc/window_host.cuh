@@ -7,7 +7,7 @@ namespace {
 
 // ---- rotations ----------------------------------------------------------------------------------
 
-// The part of a rotation that does not depend on the rows.  `axes` receives the pairs' axes.
+// A rotation as the kernels take it; what is wrong with it is recorded in the context.
 int rotation_angles(const bicache_ctx* ctx, const bicache_rotation* rot, int max_dim, const int32_t* positions,
                     int64_t axis_stride, int64_t rows, bool inverse, RopeAxes* a) {
   if (rot->rot_dim < 2 || rot->rot_dim > max_dim || rot->rot_dim % 2)
@@ -46,6 +46,18 @@ int rope_axes_impl(bicache_ctx* ctx, int64_t rows, const bicache_rotation* rot, 
 }
 
 // ---- tokens in and out --------------------------------------------------------------------------
+
+// Does a row of a tensor belong to two requests?  (Rows that are written must not.)
+bool rows_overlap(int32_t R, const int64_t* row_off, const int32_t* seqlen) {
+  std::vector<std::pair<int64_t, int64_t>> spans;
+  spans.reserve(R);
+  for (int i = 0; i < R; ++i)
+    if (seqlen[i] > 0) spans.emplace_back(row_off[i], row_off[i] + seqlen[i]);
+  if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return true;
+  return false;
+}
 
 // Lists of three lengths; with the angles beside the longest, a launch stays below the 32,764 bytes of its parameters.
 constexpr int kTokenWords = 7552;
@@ -174,6 +186,7 @@ int append_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     if (!q != !q_out) return fail(ctx, BICACHE_ERR_INVALID, "queries without their output, or the reverse");
     if (q) {
       if (!rot) return fail(ctx, BICACHE_ERR_INVALID, "queries without a rotation");
+      if (rows_overlap(R, row_off, seqlen)) return fail(ctx, BICACHE_ERR_INVALID, "a query row belongs to two requests");
       if (!aligned16(q) || !aligned16(q_out)) return fail(ctx, BICACHE_ERR_INVALID, "tensor pointer not 16-byte aligned");
       if (q_row_stride < q_least || q_out_row_stride < q_least || (q_row_stride * ctx->esize) % 16 ||
           (q_out_row_stride * ctx->esize) % 16)
@@ -234,6 +247,7 @@ int read_tokens_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t* 
   if (rows_end > 0) {
     if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || k_out == v_out)
       return fail(ctx, BICACHE_ERR_INVALID, "bad k/v pointer");
+    if (rows_overlap(R, row_off, seqlen)) return fail(ctx, BICACHE_ERR_INVALID, "a row belongs to two requests");
     if (kv_row_stride < (int64_t)cfg.num_kv_heads * cfg.head_dim || (kv_row_stride * ctx->esize) % 16)
       return fail(ctx, BICACHE_ERR_INVALID, "bad row stride");
   }
@@ -573,6 +587,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     if (!q || !out || !aligned16(q) || !aligned16(out) || !aligned4(lse_out))
       return fail(ctx, BICACHE_ERR_INVALID, "bad tensor pointer");
     if (q == out) return fail(ctx, BICACHE_ERR_INVALID, "the output must not be the queries");
+    if (rows_overlap(R, row_off, seqlen)) return fail(ctx, BICACHE_ERR_INVALID, "a row belongs to two requests");
     const int64_t least = (int64_t)cfg.num_q_heads * cfg.head_dim;
     if (q_row_stride < least || out_row_stride < least || (q_row_stride * ctx->esize) % 16 || (out_row_stride * ctx->esize) % 16)
       return fail(ctx, BICACHE_ERR_INVALID, "bad row stride");

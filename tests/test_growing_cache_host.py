@@ -58,7 +58,7 @@ def append(lib, ctx, layer=0, pid=(0, 2), tok=(30, 0), off=(0, 10), n=(10, 16), 
 @pytest.mark.parametrize("change", [
     {}, {"q": C16, "qo": C16}, {"q": C16, "qo": 0x40000, "qs": 1024}, {"rot": None}, {"pos": A4}, {"n": (0, 0), "k": None, "v": None},
     {"pid": (), "tok": (), "off": (), "n": ()}, {"tok": (0, 0), "n": (40, 16)}, {"pid": (0, 0), "tok": (30, 20), "n": (10, 10)},
-    {"pid": (0, 0), "tok": (30, 30), "n": (10, 0)}, {"layer": 2, "pid": (1, 2), "tok": (7, 0)}, {"ks": 264},
+    {"pid": (0, 0), "tok": (30, 30), "n": (10, 0)}, {"layer": 2, "pid": (1, 2), "tok": (7, 0)}, {"ks": 264}, {"off": (0, 0)},
     {"rot": rotation(axes=3, axis=[0, 1, 2, 0] * 16), "pos": A16, "axis_stride": 26}, {"rot": rotation(pairs=1)}])
 def test_append_arguments_in_order(lib, ctx, change):
     assert append(lib, ctx, **change) == b.ERR_UNSUPPORTED
@@ -78,7 +78,8 @@ def test_append_arguments_in_order(lib, ctx, change):
     {"rot": rotation(scale=INF)}, {"rot": rotation(pairs=2, freq=[1.0, NAN])}, {"rot": rotation(pairs=2, freq=[1.0, 2.0 ** 21])},
     {"rot": rotation(axes=2, axis=[0, 2] * 32), "pos": A16, "axis_stride": 26}, {"rot": rotation(axis=[1] + [0] * 63)},
     {"rot": rotation(axes=2, axis=[0, -1] * 32), "pos": A16, "axis_stride": 26},
-    {"rot": rotation(axes=2), "axis_stride": 26}, {"rot": rotation(axes=2), "pos": A16, "axis_stride": 25}])
+    {"rot": rotation(axes=2), "axis_stride": 26}, {"rot": rotation(axes=2), "pos": A16, "axis_stride": 25},
+    {"off": (0, 9), "q": C16, "qo": 0x40000}])
 def test_append_refusals(lib, ctx, change):
     assert append(lib, ctx, **change) == b.ERR_INVALID
 
@@ -97,7 +98,7 @@ def read(lib, ctx, layer=0, pid=(0, 0), tok=(30, 30), off=(0, 10), n=(10, 10), k
 def test_read(lib, ctx):
     assert read(lib, ctx) == b.ERR_UNSUPPORTED                # the same token twice may be read
     for change in ({"layer": 3}, {"n": (11, 1)}, {"n": (-1, 1)}, {"k": None}, {"v": A4}, {"k": A16, "v": A16}, {"ks": 248},
-                   {"ks": 257}, {"pid": (1, 1), "tok": (0, 0)}, {"tok": None}):
+                   {"ks": 257}, {"pid": (1, 1), "tok": (0, 0)}, {"tok": None}, {"off": (0, 9)}):
         assert read(lib, ctx, **change) == b.ERR_INVALID
     assert read(lib, ctx, pid=(0, 9)) == b.ERR_NOTFOUND
 
@@ -125,7 +126,7 @@ def test_window_arguments_in_order(lib, ctx, change):
     {"sinks": -1}, {"left": -2}, {"right": -2}, {"scale": NAN}, {"scale": INF}, {"n": (-1, 0, 0)}, {"off": (0, -1, 0)},
     {"pos": (0, 0, -1)}, {"cached": (-1, 0, 0)}, {"cached": (41, 0, 0)}, {"pos": (BIG - 9, 0, 0)}, {"pid": (-2, 2, 0)},
     {"pid": (-1, 2, 0)}, {"pid": (1, 2, 0), "cached": (1, 0, 0)}, {"q": None}, {"out": None}, {"q": A4}, {"out": ODD},
-    {"lse": ODD}, {"out": A16}, {"qs": 504}, {"os": 508}, {"qs": 516}, {"n": (0x60000000, 3, 2)}])
+    {"lse": ODD}, {"out": A16}, {"qs": 504}, {"os": 508}, {"qs": 516}, {"n": (0x60000000, 3, 2)}, {"off": (0, 11, 10)}])
 def test_window_refusals(lib, ctx, change):
     assert window(lib, ctx, **change) == b.ERR_INVALID
 
