@@ -150,16 +150,18 @@ __device__ __forceinline__ int window_tile(int start, int begin, int end, int j)
   return t < end ? t : t - (end - begin);
 }
 // kTile: tokens of a key tile.  Row tiles of a request have the same number of ranges; a range past a tile's end is empty.
-template <int kTile>
+// Row tiles go from the last, whose rows see most, to the first; neighbours are those of one KV head, which share keys in L2,
+// or, with kHeadsTogether, the KV heads of one row tile, so that all long items come first.
+template <int kTile, bool kHeadsTogether = false>
 __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const WindowReq& r, int item, int tile_rows) {
   WindowItem it;
   const int G = a.Hq / a.Hkv;
   int at = item - r.item_begin;
-  const int per_head = r.row_tiles * r.splits;
-  it.hk = at / per_head;
-  at -= it.hk * per_head;
-  const int from_end = at / r.splits, tile = r.row_tiles - 1 - from_end;         // the last rows see most: they go first
-  it.split = at - from_end * r.splits;
+  const int outer = (kHeadsTogether ? a.Hkv : r.row_tiles) * r.splits, o = at / outer;
+  at -= o * outer;
+  const int inner = at / r.splits, tile = r.row_tiles - 1 - (kHeadsTogether ? o : inner);
+  it.hk = kHeadsTogether ? inner : o;
+  it.split = at - inner * r.splits;
   it.row0 = tile * tile_rows;
   const int last = min(it.row0 + tile_rows, r.n * G) - 1;
   it.pages = window_pages(a.sinks, a.left, a.right, r.len, r.pos + it.row0 / G, r.pos + last / G);
@@ -265,7 +267,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
   float* const vs = ks + kWinKeys * pitch;
   float* const ps = vs + kWinKeys * pitch;                         // [kWinKeys][kPPitch]
   const WindowReq& r = window_req(a, list.w, blockIdx.x);
-  const WindowItem it = window_item<kWinKeys>(a, r, blockIdx.x, kRows);
+  const WindowItem it = window_item<kWinKeys, true>(a, r, blockIdx.x, kRows);
   const int G = a.Hq / a.Hkv, packed = r.n * G;
   const int tid = threadIdx.x, tx = tid % kWinLanes, ty = tid / kWinLanes % kRowGroups, part = tid / (kWinLanes * kRowGroups);
 
