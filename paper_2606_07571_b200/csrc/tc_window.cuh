@@ -51,23 +51,33 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
   const int is_v = warp - 5;
   const int stages = is_v ? kVStages : kKStages;
   int armed[kKStages] = {-1, -1, -1};        // load warps: the last tile armed with bulk copies, per stage
+  // Where lanes 0-3 find the pages of a tile.
+  struct TilePage {
+    const char* src;
+    WindowSlots slots;
+    bool bulk;                               // to be copied as a whole
+  };
+  auto find_tile = [&](int j) {
+    TilePage p = TilePage{nullptr, WindowSlots{0, kPageSize, 0}, lane < tile_pages(j)};
+    if (p.bulk) {
+      const int s = tile_of(j) * (kKeys / kPageSize) + lane;
+      p.src = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes + window_page(a, r, params.w, it.pages, s) * a.page_stride;
+      if (is_v) {
+        p.slots = window_slots(it.pages, s);
+        p.bulk = p.slots.whole();
+      }
+    }
+    return p;
+  };
   // One tile into its slot, which is free.
-  auto load_tile = [&](int j) {
+  auto load_tile = [&](int j, const TilePage& p) {
     const int b = j % stages;
     const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
     const unsigned dst = (is_v ? v_ring : k_ring) + b * kKvTileBytes;
-    const int npages = tile_pages(j), s = tile_of(j) * (kKeys / kPageSize) + lane;
-    const char* src = nullptr;
-    bool bulk = lane < npages;
-    WindowSlots slots = WindowSlots{0, kPageSize, 0};
-    if (bulk) {
-      src = (is_v ? a.pool_v : a.pool_k) + (long long)it.hk * a.page_bytes +
-            window_page(a, r, params.w, it.pages, s) * a.page_stride;
-      if (is_v) {
-        slots = window_slots(it.pages, s);
-        bulk = slots.whole();
-      }
-    }
+    const int npages = tile_pages(j);
+    const char* const src = p.src;
+    const WindowSlots& slots = p.slots;
+    const bool bulk = p.bulk;
     const unsigned bulks = __ballot_sync(0xffffffffu, bulk);
     if (bulk) bulk_copy_g2s(dst + lane * kPageBytes, src, kPageBytes, full);
     const unsigned pieces = ~bulks & ((1u << npages) - 1u);
@@ -96,7 +106,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     asm volatile("barrier.cta.arrive 1, 224;" ::: "memory");       // the others may use the barriers
     begun = status_now == 0 && (q_smem & 1023u) == 0;
     if (begun)
-      for (int j = 0; j < ahead; ++j) load_tile(j);
+      for (int j = 0; j < ahead; ++j) load_tile(j, find_tile(j));
     asm volatile("barrier.cta.sync 2, 96;" ::: "memory");          // the flags that warp 4 sets
     dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
   } else {
@@ -373,9 +383,10 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     // Warp 5 stages the K tiles, warp 6 the V tiles.
     bool ok = !dead;
     for (int j = begun ? ahead : 0; j < T && ok; ++j) {
+      const TilePage p = find_tile(j);                             // while the slot is still in use
       const unsigned free_bar = smem_u32(is_v ? &sy->v_free[j % stages] : &sy->k_free[j % stages]);
       ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
-      if (ok) load_tile(j);
+      if (ok) load_tile(j, p);
     }
     // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
     if ((!ok || *abort_flag) && lane == 0) {

@@ -26,7 +26,7 @@ struct WindowReq {
   int len;                      // cached tokens
   int sink_pages;               // pages of the list that come before the gap (0: no gap)
   int gap;                      // pages left out behind them
-  int page_word;                // page list in the parameter words
+  int page_word;                // page list in the parameter words, or among the staged pages
   int item_begin;               // first work item
   int splits, tiles_per_split;  // ranges of key tiles
   int part_off;                 // first partial result in row-heads (splits > 1)
@@ -42,7 +42,7 @@ struct WindowArgs {
   float* lse;                   // or nullptr
   long long q_stride, out_stride;          // elements between rows
   const char *pool_k, *pool_v;  // of the layer
-  const int* staged_pages;      // page list of the only request, if it did not fit the parameters
+  const int* staged_pages;      // the page lists, if they did not fit the parameters
   long long page_stride;        // bytes of a page of all heads
   int page_bytes, swizzled;
   int Hq, Hkv, D;
@@ -53,7 +53,7 @@ struct WindowArgs {
 };
 
 // The last of `num` records whose start (`start` of it) is not above x.  A guess by proportion comes first, since batches are
-// mostly even: every step of a search is a parameter read that waits for the one before (about 0.2 us).
+// mostly even: every step of a search is a parameter read that waits for the one before.
 template <typename R, typename F>
 __device__ __forceinline__ const R& last_start(const int* list, int num, int total, int x, F&& start) {
   const R* const recs = reinterpret_cast<const R*>(list);
@@ -177,11 +177,11 @@ __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const Win
   return it;
 }
 // The pool page of page `s` of an item's sequence.  (Two loads and a branch, not one load through either pointer: that would
-// read the parameters by way of memory, in 0.4 us instead of 0.1.)
+// read the parameters by way of memory.)
 __device__ __forceinline__ int window_page(const WindowArgs& a, const WindowReq& r, const int* list, const WindowPages& w, int s) {
   const int page = s < w.sink_pages ? s : s - w.sink_pages + w.lo_page;          // of the prefix
   const int at = page < r.sink_pages ? page : page - r.gap;
-  return a.staged_pages ? a.staged_pages[at] : list[r.page_word + at];
+  return a.staged_pages ? a.staged_pages[r.page_word + at] : list[r.page_word + at];
 }
 // The slots of page `s` of the sequence that some row of the item sees: [lo, hi), and [0, sink) besides.  What lies
 // in the others must not reach a sum, not even with weight 0: it may be no number.
@@ -531,7 +531,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
   }
 }
 
-// A page list that does not fit the parameters goes through the workspace, written by launches of this kernel.
+// Page lists that do not fit the parameters stand in the workspace, written by launches of this kernel.
 template <int kWords>
 __global__ void stage_pages_kernel(int* __restrict__ dst, int count, const __grid_constant__ ParamList<kWords> list) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;

@@ -287,7 +287,9 @@ struct WindowForm {
   int list_words;               // what a launch's list holds
 };
 
-// The launches of one call and one kernel form: requests are added until the parameter list is full.
+// The launches of one call and one kernel form.  Requests are added until the parameter list holds no more records; their
+// page lists stand behind the records, or, if they are too long for that, in the workspace, where launches of
+// their own write them.  (64 tokens over 31,000 pages: four launches of what a list holds, each with its join, took 283 us.)
 class WindowLaunches {
  public:
   WindowLaunches(bicache_ctx* ctx, const WindowArgs& args, const WindowForm& form, cudaStream_t stream)
@@ -314,10 +316,9 @@ class WindowLaunches {
       p.max_tiles = std::max(p.max_tiles, tiles);
       p.sum_tiles += tiles;
     }
-    const int words = kWindowReqWords + w.count;
-    const bool alone = words > form_.list_words;          // its page list goes through the workspace
-    if (alone || words_ + words > form_.list_words) {
-      const int st = flush();
+    const long long records = (long long)(pending_.size() + 1) * kWindowReqWords, all = (long long)pages_.size() + w.count;
+    if (records > form_.list_words || (records + all > form_.list_words && all > ctx_->cfg.num_pages)) {
+      const int st = flush();                             // one request alone has no more pages than the pool
       if (st != BICACHE_OK) return st;
     }
     p.r.page_word = (int)pages_.size();
@@ -325,15 +326,15 @@ class WindowLaunches {
     pages_.insert(pages_.end(), pages.begin(), pages.begin() + w.sink_pages);
     pages_.insert(pages_.end(), behind, behind + (w.count - w.sink_pages));
     pending_.push_back(p);
-    words_ += words;
-    return alone ? flush() : BICACHE_OK;
+    return BICACHE_OK;
   }
 
   int flush() {
     if (pending_.empty()) return BICACHE_OK;
     WindowArgs a = base_;
     cudaError_t e = cudaSuccess;
-    if (words_ > form_.list_words) {
+    const int words = (int)pending_.size() * kWindowReqWords;
+    if (words + (long long)pages_.size() > form_.list_words) {
       a.staged_pages = ctx_->d_put_pages;
       for (size_t at = 0; at < pages_.size() && e == cudaSuccess; at += kParamWords) {
         const int count = (int)std::min<size_t>(kParamWords, pages_.size() - at);
@@ -351,14 +352,13 @@ class WindowLaunches {
     std::stable_sort(pending_.begin(), pending_.end(), [](const Pending& x, const Pending& y) { return x.max_tiles > y.max_tiles; });
     const int tps = choose_tiles_per_split();
     long long items = 0, part = 0;
-    const int words = (int)pending_.size() * kWindowReqWords;
     for (size_t i = 0; i < pending_.size(); ++i) {
       Pending& p = pending_[i];
       p.r.splits = splits_of(p, tps);
       p.r.tiles_per_split = std::max(1, (p.max_tiles + p.r.splits - 1) / p.r.splits);
       p.r.item_begin = (int)items;
       p.r.part_off = p.r.row_heads_before = 0;
-      p.r.page_word = a.staged_pages ? 0 : p.r.page_word + words;
+      p.r.page_word += a.staged_pages ? 0 : words;
       items += (long long)p.r.row_tiles * a.Hkv * p.r.splits;
     }
     int row_heads = 0;
@@ -380,7 +380,6 @@ class WindowLaunches {
     for (const Pending& p : pending_) most_splits = std::max(most_splits, p.r.splits);
     pending_.clear();
     pages_.clear();
-    words_ = 0;
     if (items > 0x7fffffffLL) return fail(ctx_, BICACHE_ERR_INVALID, "batch too large");
     e = launch(a, list, used);
     ctx_->launches++;
@@ -466,7 +465,6 @@ class WindowLaunches {
 
   std::vector<Pending> pending_;
   std::vector<int32_t> pages_;
-  int words_ = 0;
 };
 
 // f(T, rows, largest head dim) as integral constants, of the CUDA-core kernel that serves a type, row tile and head dim
