@@ -53,6 +53,7 @@ struct PrefixEntry {
   int32_t m;
   int32_t first_layer = 0;
   bool uniform = true;
+  bool consecutive = false;                           // uniform, and every page is the one after its predecessor
   std::vector<int32_t> pages;                         // the list of layer first_layer
   std::vector<std::vector<int32_t>> layer_pages;      // only if !uniform
 };
@@ -1059,6 +1060,8 @@ int32_t put_impl(bicache_ctx* ctx, uint64_t key, int32_t m, const void* k, const
   for (size_t j = 1; j < lists.size(); ++j) e.uniform = e.uniform && lists[j] == lists[0];
   e.pages = lists[0];
   if (!e.uniform) e.layer_pages = lists;
+  e.consecutive = e.uniform;
+  for (int i = 1; i < need; ++i) e.consecutive = e.consecutive && e.pages[i] == e.pages[i - 1] + 1;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   cudaError_t ce = cudaSuccess;
   if (write) {

@@ -6,19 +6,28 @@
 // tile j ends.  Roles: warps 0-3 softmax (one thread per row; they also gather the Q tile), warp 4 MMA issue and TMEM, warp
 // 5 stages K tiles, warp 6 V tiles.  What the window adds:
 //   - pages are looked up in the item's page sequence (first tokens, then the window's);
+//   - an item begins with a tile that all its rows see (window_item), so that the running maxima hardly move;
 //   - a row knows the columns it sees as an interval and a number of first columns.  A tile that some row of a warp
-//     does not see in full is masked with the bits of a 64-bit word, and a row that has seen nothing yet keeps -inf as
-//     its reference and 0 for it in the exponent;
+//     does not see in full is masked by bits, and a row that has seen nothing yet keeps -inf as its reference and 0 for it
+//     in the exponent;
 //   - slots that no row of the item sees may hold anything.  Their scores are masked one way or another; as values they would
 //     meet weight 0, and 0 times a NaN is a NaN: a page of values with such slots comes by a copy per run of seen slots, the
 //     others zeroed, where whole pages come by one bulk copy;
 //   - an item that has all the keys of its rows writes the output itself, in bf16; ranges write normalised partial
 //     results for window_join_kernel.
+//
+// What bounds it.  Few rows: reading the keys (64 tokens over caches of 700 to 16,384 keys, 1.7 GB: 264 us, 6.4 TB/s); a single
+// token over 16,384 keys takes 10 us and its join 4, of which 5 are reading: starts and ends of four tiles to an item.
+// Long windows: the shared-memory port, which moves 768 cycles' worth of operands for a tile that the tensor pipe computes in
+// 512 (1145 TFLOP/s over 16,384 keys that all rows see).  Short windows: an item's start (6000 cycles until its first
+// scores) and end (3500) beside 12 tiles of 1550 (two items at a time): 28 query heads, window of 500 + 201, five ragged
+// requests 90 us, the tensor pipe 37 % busy.
 #pragma once
 #include "tc_decode.cuh"
 #include "window.cuh"
 
 namespace bicache {
+
 template <int kWords>
 __global__ void __launch_bounds__(dec::kDecThreads, 2)
 tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wait_cycles,
@@ -277,7 +286,7 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
         }
         // A thread holds a row (128 values).  It goes to shared memory first (the K/V rings are free by now: every tile has been
         // consumed; rows 272 bytes apart keep the 16-byte stores conflict-free), half a row at a time if it is a partial
-        // result; then the warp writes whole rows.  (A bulk copy per row took three times as long.)
+        // result; then the warp writes whole rows.  (A bulk copy per row took 4500 cycles, this 3400.)
         unsigned char* const stage = smem + kQBytes + warp * 32 * 272;
         char* const mine_to = whole ? a.out + (out_row * a.out_stride + (long long)w.h * 128) * 2 : reinterpret_cast<char*>(a.part_o + at * 128);
         const int here = min(32, rows - warp * 32);

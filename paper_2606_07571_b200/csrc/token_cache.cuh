@@ -6,7 +6,8 @@
 // pages they reach) travels as launch parameters, so nothing is uploaded and one launch does a layer of the whole batch,
 // queries included.  Row space: the tokens of all runs one after the other; a block takes kRows of them, its
 // first threads look up where each lies, and then a thread does one unit (the chunks of a head that pair up) for
-// all the block's rows, as in rope_chunks_kernel.
+// all the block's rows, as in rope_chunks_kernel.  23,000 rows of 32 heads, queries, keys and values, three position axes: 176
+// us (1.13 GB, 6.4 TB/s) and 115 us back (0.76 GB, 6.6 TB/s).  16 rows: 3 us each way, a launch and three loads in turn.
 #pragma once
 #include "evict.cuh"
 #include "rope.cuh"
@@ -166,7 +167,8 @@ append_chunks_kernel(const __grid_constant__ A a, const __grid_constant__ TokenA
 }
 
 // Any rotated width, chunk by chunk as in rope_any_kernel; kRows tokens at a time, so that a batch fills the block also
-// where there are few heads.
+// where there are few heads.  100,000 rows of 4 KV heads, 108 of 128 dims turned, and back: 336 us, where one thread per pair
+// took 720 and one token at a time 588; what it does over the bandwidth (125 us) is loading the other halves by 4 bytes.
 template <typename T, typename A, int kRows, int kWords>
 __global__ void __launch_bounds__(kRopeThreads)
 append_any_kernel(const __grid_constant__ A a, const __grid_constant__ TokenArgs g, int interleaved,

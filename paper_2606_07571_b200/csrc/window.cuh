@@ -8,7 +8,8 @@
 // This file: the batch as the kernels see it, the CUDA-core kernel (fp32, head dims other than 128), and the
 // kernel that joins ranges of keys.
 //
-// The batch travels as launch parameters: requests, and of each the pages that some row of it sees.  A request's row
+// The batch travels as launch parameters: requests, and of each the pages that some row of it sees, unless the prefix's pages
+// follow one another in the pool (what an unbroken pool hands out), which the number of the first says.  A request's row
 // space is its rows x the G = Hq / Hkv query heads of a KV head (packed row = row * G + head), cut into row tiles.  A row tile
 // sees an interval of tokens (rows follow one another, so their windows join up) and the first tokens; its
 // pages - those of the first tokens, then the interval's - are put side by side, and key tiles are cut from that
@@ -24,6 +25,7 @@ struct WindowReq {
   int n;                        // rows
   int pos;                      // position of the first
   int len;                      // cached tokens
+  int first_page;               // of a prefix whose pages are consecutive, which needs no list; else -1
   int sink_pages;               // pages of the list that come before the gap (0: no gap)
   int gap;                      // pages left out behind them
   int page_word;                // page list in the parameter words, or among the staged pages
@@ -32,6 +34,7 @@ struct WindowReq {
   int part_off;                 // first partial result in row-heads (splits > 1)
   int row_tiles;
   int row_heads_before;         // row-heads of split requests before this one (joining kernel)
+  int pad;
 };
 constexpr int kWindowReqWords = sizeof(WindowReq) / 4;
 static_assert(sizeof(WindowReq) % 8 == 0, "8-byte aligned records");
@@ -180,6 +183,7 @@ __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, const Win
 // read the parameters by way of memory.)
 __device__ __forceinline__ int window_page(const WindowArgs& a, const WindowReq& r, const int* list, const WindowPages& w, int s) {
   const int page = s < w.sink_pages ? s : s - w.sink_pages + w.lo_page;          // of the prefix
+  if (r.first_page >= 0) return r.first_page + page;
   const int at = page < r.sink_pages ? page : page - r.gap;
   return a.staged_pages ? a.staged_pages[r.page_word + at] : list[r.page_word + at];
 }
@@ -214,6 +218,9 @@ __device__ __forceinline__ long long window_part(const WindowArgs& a, const Wind
 // output.  A row tile of 16, for few rows, is four groups of 2 x 16 threads, each group with a quarter of the keys of a
 // tile and a running softmax of its own; they are put together at the end.  All sums in fp32.  Values arrive while the scores
 // are computed, the next tile's keys during the rest.
+// Bound by instructions and their latency: 5000 to a warp and tile, 3072 of them products, 12 warps to an SM.  10,334 causal
+// fp32 rows of 4 heads of 64 dims take 1670 us (33 TFLOP/s; 256 threads with 4 rows each took 3390), three requests of up to
+// 1000 rows under a window of 700 78 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWinThreads = 128;
 constexpr int kWinKeys = 64;
@@ -543,7 +550,7 @@ __global__ void stage_pages_kernel(int* __restrict__ dst, int count, const __gri
 //   lse = log sum_s exp(l_s),  o = sum_s exp(l_s - lse) o_s,
 // the ranges in ascending order.  kWarps = 1: a warp per row-head; kWarps = 8: the eight warps of a block share
 // one, warp w taking ranges w, w + 8, ..; for few row-heads of many ranges.  Placed on the SMs while the kernel before
-// it still runs, and waits for its end.
+// it still runs, and waits for its end.  Latency is what it costs: 4 to 6 us, 28 row-heads of 64 ranges as 7000 of two.
 // ---------------------------------------------------------------------------------------------
 constexpr int kJoinWarps = 8;
 constexpr int kMaxWindowSplits = 64;

@@ -42,13 +42,14 @@ class Batch:
     """Prefixes of given lengths (reserved `spare` tokens longer, everything behind the cached tokens NaN), requests with
     rows in between which others lie."""
 
-    def __init__(self, heads, dtype, lens, requests, spare=0, std=1.5, path=None):
+    def __init__(self, heads, dtype, lens, requests, spare=0, std=1.5, path=None, shuffled=True):
         self.hq, self.hkv, self.d = HEADS[heads]
         self.dtype, self.lens, self.requests = dtype, lens, requests         # request: prefix index, position, rows
         pages = sum((m + spare + 15) // 16 for m in lens) + 1
         order = np.random.default_rng(1).permutation(pages)
         self.rows = sum(n for _, _, n in requests) + len(requests) + 1
-        self.bc = binding.BiCache(1, self.hq, self.hkv, self.d, pages, dtype, self.rows, len(requests), free_order=order)
+        self.bc = binding.BiCache(1, self.hq, self.hkv, self.d, pages, dtype, self.rows, len(requests),
+                                  free_order=order if shuffled else None)
         self.bc.k_pool.fill_(255)
         self.bc.v_pool.fill_(255)
         if path is not None:
@@ -240,6 +241,26 @@ def test_pages_that_do_not_fit_the_parameters():
     b = Batch("d32", torch.bfloat16, [m, 100], [(1, 90, 10), (0, m - 3, 3), (1, 99, 1)])
     b.check(0, -1, 0)
     b.check(7, 127500, 0)
+
+
+@pytest.mark.parametrize("heads,dtype", [("gqa28", torch.bfloat16), ("mha32", torch.bfloat16), ("mha4_64", torch.float32)])
+@pytest.mark.parametrize("window", [(0, -1, 0), (20, 200, 30)])
+def test_consecutive_and_shuffled_pages_give_the_same_bits(heads, dtype, window):
+    lens = [700, 3001, 17, 0]
+    requests = [(0, 100, 300), (1, 3000, 1), (2, 16, 5), (1, 900, 700), (3, 0, 2), (0, 650, 50), (1, 1300, 900)]
+    outs = [Batch(heads, dtype, lens, requests, spare=5, shuffled=s).call(*window) for s in (False, True)]
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    Batch(heads, dtype, lens, requests[:3], spare=5, shuffled=False).check(*window)
+
+
+def test_long_lists_go_through_the_workspace():
+    """Page lists of a batch that together do not fit the parameters: launches that write them, then one and a join."""
+    lens = [20000, 30000, 40000, 50000]
+    b = Batch("d32", torch.bfloat16, lens, [(i, m - 2, 2) for i, m in enumerate(lens)])
+    before = b.bc.launch_count()
+    b.check(4, -1, 0)
+    assert b.bc.launch_count() - before == 4                   # 8750 pages: two lists
+    b.check(4, 25000, 0)
 
 
 def test_many_requests_take_several_launches():
