@@ -16,7 +16,7 @@
 //   - an item that has all the keys of its rows writes the output itself, in bf16; ranges write normalised partial
 //     results for window_join_kernel.
 //
-// What bounds it.  Few rows: reading the keys (64 tokens over caches of 700 to 16,384 keys, 1.7 GB: 264 us, 6.4 TB/s); a single
+// What bounds it.  Few rows: reading the keys (64 tokens over caches of 700 to 16,384 keys, 1.7 GB: 260 us, 6.5 TB/s); a single
 // token over 16,384 keys takes 10 us and its join 4, of which 5 are reading: starts and ends of four tiles to an item.
 // Long windows: the shared-memory port, which moves 768 cycles' worth of operands for a tile that the tensor pipe computes in
 // 512 (1145 TFLOP/s over 16,384 keys that all rows see).  Short windows: an item's start (6000 cycles until its first
