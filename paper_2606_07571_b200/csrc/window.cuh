@@ -215,12 +215,12 @@ __device__ __forceinline__ long long window_part(const WindowArgs& a, const Wind
 // CUDA-core kernel.  128 threads take a row tile against key tiles of 64: queries, keys and values lie in shared memory
 // as fp32 (a row's end padded by 16 bytes, so that lanes on neighbouring rows read other banks).  A row tile of 64 is a grid
 // of 8 x 16 threads, each with 8 rows x 4 keys of the scores (two dims to a packed product) and 8 rows x D / 16 dims of the
-// output.  A row tile of 16, for few rows, is four groups of 2 x 16 threads, each group with a quarter of the keys of a
+// output (two rows to a packed product).  A row tile of 16, for few rows, is four groups of 2 x 16 threads, each group with a quarter of the keys of a
 // tile and a running softmax of its own; they are put together at the end.  All sums in fp32.  Values arrive while the scores
 // are computed, the next tile's keys during the rest.
-// Bound by instructions and their latency: 5000 to a warp and tile, 3072 of them products, 12 warps to an SM.  10,334 causal
-// fp32 rows of 4 heads of 64 dims take 1670 us (33 TFLOP/s; 256 threads with 4 rows each took 3390), three requests of up to
-// 1000 rows under a window of 700 78 us.
+// Bound by instructions and their latency: 4500 to a warp and tile, less than half of them products, 12 warps to an SM.
+// 10,334 causal fp32 rows of 4 heads of 64 dims take 1555 us (35 TFLOP/s; 256 threads with 4 rows each took 3390, products of
+// the output by single rows 1670), three requests of up to 1000 rows under a window of 700 78 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWinThreads = 128;
 constexpr int kWinKeys = 64;
@@ -235,6 +235,11 @@ __device__ __forceinline__ float win_exp2(float x) {               // 2 ulp, res
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+__device__ __forceinline__ unsigned long long win_pack(float lo, float hi) {
+  unsigned long long d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
 }
 __device__ __forceinline__ float lanes16_max(float x) {
 #pragma unroll
@@ -299,13 +304,14 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
     if (p < packed) col[i] = window_columns(a, it.pages, r.len, r.pos + p / G);
   }
 
-  float m_run[kWinPer], l_run[kWinPer], acc[kWinPer][2 * kPairs];
+  float m_run[kWinPer], l_run[kWinPer];
+  unsigned long long acc2[kWinPer / 2][2 * kPairs];                // output, two rows to a register pair
 #pragma unroll
   for (int i = 0; i < kWinPer; ++i) {
     m_run[i] = -INFINITY;
     l_run[i] = 0.f;
 #pragma unroll
-    for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] = 0.f;
+    for (int d = 0; d < 2 * kPairs; ++d) acc2[i / 2][d] = 0ull;
   }
   // Where a tile's pages lie, for the tiles to be staged after the next barrier.
   auto look_up = [&](int tile, PagePlace* to) {
@@ -406,6 +412,7 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
           if (!((c >= col[i].begin && c < col[i].end) || c < col[i].sink)) s[i][k] = -INFINITY;
         }
     }
+    float alpha[kWinPer];
 #pragma unroll
     for (int i = 0; i < kWinPer; ++i) {
       float mx = s[i][0];
@@ -413,17 +420,21 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
       for (int k = 1; k < kMine; ++k) mx = fmaxf(mx, s[i][k]);
       const float m_new = fmaxf(m_run[i], lanes16_max(mx));
       const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen so far: every weight is 0
-      const float alpha = win_exp2(m_run[i] - m_use);
+      alpha[i] = win_exp2(m_run[i] - m_use);
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < kMine; ++k) {
         s[i][k] = win_exp2(s[i][k] - m_use);
         sum += s[i][k];
       }
-      l_run[i] = l_run[i] * alpha + sum;                           // of this thread's keys; added up at the end
+      l_run[i] = l_run[i] * alpha[i] + sum;                        // of this thread's keys; added up at the end
       m_run[i] = m_new;
+    }
 #pragma unroll
-      for (int d = 0; d < 2 * kPairs; ++d) acc[i][d] *= alpha;
+    for (int i = 0; i < kWinPer / 2; ++i) {
+      const unsigned long long both = win_pack(alpha[2 * i], alpha[2 * i + 1]);
+#pragma unroll
+      for (int d = 0; d < 2 * kPairs; ++d) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(acc2[i][d]) : "l"(both));
     }
 #pragma unroll
     for (int k = 0; k < kMine; ++k)
@@ -435,30 +446,35 @@ window_simt_kernel(const __grid_constant__ WindowArgs a, const __grid_constant__
     __syncthreads();
 #pragma unroll 4
     for (int key = part * kPartKeys; key < (part + 1) * kPartKeys; ++key) {
-      float pr[kWinPer];
+      unsigned long long pr[kWinPer / 2];                          // the weights of two rows
 #pragma unroll
-      for (int i = 0; i < kWinPer; i += 4) {
-        const float4 p = *reinterpret_cast<const float4*>(&ps[key * kPPitch + ty * kWinPer + i]);
+      for (int i = 0; i < kWinPer / 2; i += 2) {
+        const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(&ps[key * kPPitch + ty * kWinPer + 2 * i]);
         pr[i] = p.x;
         pr[i + 1] = p.y;
-        pr[i + 2] = p.z;
-        pr[i + 3] = p.w;
       }
 #pragma unroll
       for (int g = 0; g < kPairs; ++g) {
         const int d = (g * kWinLanes + tx) * 2;
         if (kMaxD != kWinAnyD || d < D) {
           const float2 v = *reinterpret_cast<const float2*>(&vs[key * pitch + d]);
+          const unsigned long long vx = win_pack(v.x, v.x), vy = win_pack(v.y, v.y);
 #pragma unroll
-          for (int i = 0; i < kWinPer; ++i) {
-            acc[i][2 * g] = fmaf(pr[i], v.x, acc[i][2 * g]);
-            acc[i][2 * g + 1] = fmaf(pr[i], v.y, acc[i][2 * g + 1]);
+          for (int i = 0; i < kWinPer / 2; ++i) {
+            asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc2[i][2 * g]) : "l"(pr[i]), "l"(vx));
+            asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc2[i][2 * g + 1]) : "l"(pr[i]), "l"(vy));
           }
         }
       }
     }
   }
 
+  float acc[kWinPer][2 * kPairs];
+#pragma unroll
+  for (int i = 0; i < kWinPer; ++i)
+#pragma unroll
+    for (int d = 0; d < 2 * kPairs; ++d)
+      acc[i][d] = __uint_as_float((unsigned)(i & 1 ? acc2[i / 2][d] >> 32 : acc2[i / 2][d]));
 #pragma unroll
   for (int i = 0; i < kWinPer; ++i) l_run[i] = lanes16_sum(l_run[i]);
   if (kParts > 1) {
