@@ -1321,8 +1321,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             mbar_arrive(full);
           }
         }
-      } else
-      for (int j = 0; j < g.T; ++j) {
+      }
+      for (int j = 0; !kWindow && j < g.T; ++j) {
         const int u = U + 2 * j + is_v;
         const int slot = u % kRing;
         const int jg = g.tile_begin + j;

@@ -180,6 +180,56 @@ def test_many_rows(tokens):
     assert same(kb, want_k) and same(q_out, want_q) and same(vb, v)
 
 
+@pytest.mark.parametrize("seed", range(16))
+def test_random_runs(seed):
+    """Disjoint runs of tokens of several prefixes in any order, against what the rotary call makes of the same rows."""
+    rng = np.random.default_rng(seed)
+    hq, hkv, d = [(7, 1, 128), (4, 4, 64), (2, 2, 96), (32, 8, 128)][seed % 4]
+    dtype = torch.float32 if seed % 3 == 0 else torch.bfloat16
+    lens = [int(x) for x in np.exp(rng.uniform(0, 7, rng.integers(1, 7)))]
+    pages = sum((m + 15) // 16 for m in lens)
+    bc = binding.BiCache(2, hq, hkv, d, pages, dtype, 16, 1, free_order=rng.permutation(pages) if seed % 2 else None)
+    garbage(bc)
+    ids = [bc.reserve_prefix(i, m)[0] for i, m in enumerate(lens)]
+    runs = []
+    for i, m in enumerate(lens):
+        cuts = sorted(set([0, m] + rng.integers(0, m + 1, 4).tolist()))
+        runs += [(i, a, b - a) for a, b in zip(cuts, cuts[1:]) if rng.random() < 0.8]
+    rng.shuffle(runs)
+    runs = [tuple(int(x) for x in r) for r in runs] or [(0, 0, lens[0])]
+    pid, tok, n = [ids[i] for i, _, _ in runs], [t for _, t, _ in runs], [k for _, _, k in runs]
+    off = (np.concatenate([[0], np.cumsum(n)[:-1]]) + np.arange(len(n))).tolist()          # a row between two runs
+    rows = off[-1] + n[-1]
+    q, k, v = (randn((rows, h, d), seed * 3 + j, dtype) for j, h in enumerate((hq, hkv, hkv)))
+    where = torch.zeros(rows, dtype=torch.int32)
+    for o, t, c in zip(off, tok, n):
+        where[o:o + c] = torch.arange(t, t + c)
+    rot = int(rng.choice([d, d // 2, 2 * rng.integers(1, d // 2 + 1)]))
+    inter, freq = bool(rng.integers(0, 2)), binding.rope_frequencies(rot, 10000.0)
+    q_out, kb, vb = torch.full_like(q, 3.0), torch.full_like(k, 3.0), torch.full_like(v, 3.0)
+    bc.append_tokens(1, pid, tok, off, n, k, v, q, q_out, binding.Rotation(freq, inter))
+    bc.read_tokens(1, pid, tok, off, n, kb, vb)
+    mine = torch.zeros(rows, dtype=torch.bool)
+    for o, c in zip(off, n):
+        mine[o:o + c] = True
+    mine = mine.cuda()
+    axis, p = [0] * (rot // 2), [where[mine.cpu()].tolist()]
+    check_rotated(q_out[mine], q[mine], p, freq, axis, inter, 1.0, dtype)
+    check_rotated(kb[mine], k[mine], p, freq, axis, inter, 1.0, dtype)
+    assert same(vb[mine], v[mine])
+    for x in (q_out, kb, vb):
+        assert (x[~mine] == 3).all()
+    for i, m in enumerate(lens):                               # by the call that reads whole layers
+        a, b = torch.empty((m, hkv, d), dtype=dtype, device="cuda"), torch.empty((m, hkv, d), dtype=dtype, device="cuda")
+        bc.read_prefix_layer(ids[i], 1, a, b)
+        rest = torch.ones(m, dtype=torch.bool)
+        for (j, t, c), o in zip(runs, off):
+            if j == i:
+                assert same(a[t:t + c], kb[o:o + c]) and same(b[t:t + c], vb[o:o + c])
+                rest[t:t + c] = False
+        assert a[rest.cuda()].isnan().all() and b[rest.cuda()].isnan().all()
+
+
 def test_lists_that_take_several_launches():
     hkv, d = 1, 32
     # 600 short requests of 8 words and a page each, and one whose pages alone are too many

@@ -174,6 +174,23 @@ def test_few_rows_against_many_keys(m, heads, dtype, n):
     b.check(4, m // 2, 0)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(seed):
+    rng = np.random.default_rng(seed)
+    heads = ["gqa7", "gqa4", "mha2", "mha32", "mha4_64", "d32"][seed % 6]
+    dtype = torch.float32 if heads == "mha4_64" else torch.bfloat16
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(2500), rng.integers(1, 5)))]
+    most = 700 if heads == "mha32" else 300
+    requests = []
+    for _ in range(rng.integers(1, 9)):
+        i = int(rng.integers(0, len(lens)))
+        n = int(rng.choice([1, rng.integers(1, 20), rng.integers(1, most)]))
+        requests.append((i, int(rng.choice([max(0, lens[i] - n), rng.integers(0, lens[i] + 50)])), n))
+    window = (int(rng.choice([0, 1, 4, rng.integers(0, 300)])), int(rng.choice([-1, 0, rng.integers(0, 900)])),
+              int(rng.choice([-1, 0, rng.integers(0, 200)])))
+    Batch(heads, dtype, lens, requests, spare=int(rng.integers(0, 40)), shuffled=bool(seed % 4)).check(*window)
+
+
 def test_split_and_whole_requests_in_one_call():
     lens = [20000, 40, 9000, 17]
     Batch("gqa28", torch.bfloat16, lens, [(1, 39, 1), (0, 19999, 1), (3, 3, 14), (2, 8990, 10), (1, 0, 16)]).check(2, -1, 0)
