@@ -96,6 +96,28 @@ def test_decoding(hq, hkv, d, dtype):
     assert (np.abs(f64(out) - ref) <= mag * 0.01 + np.abs(ref) * torch.finfo(dtype).eps).all()
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,d,pages", [(torch.bfloat16, 32, 32, 128, 40000), (torch.float32, 32, 32, 64, 40000)])
+def test_pages_beyond_32_bits_of_bytes(dtype, hq, hkv, d, pages):
+    """The last pages of pools of 5.2 GB each."""
+    m, n = 300, 40
+    for order in (list(range(pages))[::-1], list(range(pages - 19, pages)) + list(range(pages - 19))):     # listed, consecutive
+        bc = binding.BiCache(1, hq, hkv, d, pages, dtype, 64, 1, free_order=order)
+        pid, _, own = bc.reserve_prefix(1, m)
+        assert min(own) >= pages - 19
+        k, v, q = randn((m, hkv, d), 1, dtype), randn((m, hkv, d), 2, dtype), randn((n, hq, d), 3, dtype)
+        kb, vb, out = torch.empty_like(k), torch.empty_like(v), torch.empty_like(q)
+        bc.append_tokens(0, [pid], [0], [0], [m], k, v)
+        bc.read_tokens(0, [pid], [0], [0], [m], kb, vb)
+        assert torch.equal(kb, k) and torch.equal(vb, v)
+        bc.attend_window(0, [pid], [m], [m - n], [0], [n], q, out, None, 4, 100, 0)
+        assert bc.device_status() == 0
+        ref, _, mag, size = gc.attend_window(f64(q), f64(k), f64(v), m - n, 4, 100, 0, d ** -0.5)
+        e = ((d + 8) * 2.0 ** -23 * size + 2.0 ** -20)[..., None]
+        tol = mag * ((2.0 ** -8 if dtype == torch.bfloat16 else 0) + 2 * e + 90 * 2.0 ** -23)
+        assert (np.abs(f64(out) - ref) <= tol + (np.abs(ref) + tol) * torch.finfo(dtype).eps / 2).all()
+        bc.close()
+
+
 FIRST = """
 import torch
 from paper_2606_07571_b200 import binding
