@@ -297,3 +297,19 @@ def test_another_stream_and_device_guard():
         got, gl = b.call(0, -1, 0)
     s.synchronize()
     assert torch.equal(got, want) and torch.equal(gl, wl)
+
+
+@pytest.mark.parametrize("window", [(0, 2 ** 31 - 1, 0), (5, 40, 2 ** 31 - 1), (2 ** 31 - 1, 3, 0), (0, 2 ** 31 - 1, 2 ** 31 - 1), (7, 2 ** 31 - 1, 90)])
+@pytest.mark.parametrize("heads,dtype", [("gqa4", torch.bfloat16), ("gqa7", torch.bfloat16), ("mha4_64", torch.float32)])
+def test_windows_and_positions_at_the_end_of_their_range(window, heads, dtype):
+    """Sums of two of them do not fit 32 bits: a window as wide as numbers go is one without bound, and the last row
+    that has a position stands at 2^31 - 2."""
+    top = 2 ** 31 - 1
+    Batch(heads, dtype, [0, 100, 700], [(2, 0, 90), (2, 600, 100), (2, top - 90, 90), (1, top - 1, 1), (0, top - 4, 4), (1, 99, 1)]).check(*window)
+
+
+@pytest.mark.parametrize("window", [(0, 2 ** 31 - 1, 2 ** 31 - 1), (40, 2 ** 31 - 1, 0)])
+def test_row_tiles_of_256_at_the_end_of_their_range(window):
+    b = Batch("mha32", torch.bfloat16, [300], [(0, 2 ** 31 - 1 - 4000, 4000), (0, 100, 200)])
+    b.check(*window)
+    assert b.bc.last_attention_kernel() == binding.KERNEL_TENSOR
