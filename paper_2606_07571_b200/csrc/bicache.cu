@@ -723,9 +723,10 @@ int prepare_attention(bicache_ctx* ctx, int kind, int32_t layer, int32_t R, cons
   pc->entry = entry;
   pc->key_ranges = key_ranges;
   if (pc->use_tensor && !key_ranges) {
-    // rows the tensors are known to have: up to the end of the last request
+    // rows the tensors are known to have: up to the end of the last request that has rows
     long long rows_total = 0;
-    for (int i = 0; i < R; ++i) rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
+    for (int i = 0; i < R; ++i)
+      if (seqlen[i] > 0) rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
     const int G = cfg.num_q_heads / cfg.num_kv_heads;
     TcTensorMaps& maps = pc->maps;
     maps.q_tma = (128 % G == 0) ? 1 : 0;

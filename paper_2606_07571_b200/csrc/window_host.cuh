@@ -644,7 +644,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
     // items 115 against 102.
     long long tiles = 0, rows_total = 0;
     for (int i = 0; i < R; ++i) {
-      rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);
+      if (seqlen[i] > 0) rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);     // an empty one's row says nothing
       if ((long long)seqlen[i] * G > 128) tiles += ((long long)seqlen[i] * G + kTileRows - 1) / kTileRows * cfg.num_kv_heads;
     }
     TcTensorMaps maps;
