@@ -662,6 +662,7 @@ int prepare_attention(bicache_ctx* ctx, int kind, int32_t layer, int32_t R, cons
   long long total = 0;
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative length or offset");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     total += seqlen[i];
   }
   if (total > 0x7fffffffLL / std::max(1, cfg.num_q_heads / cfg.num_kv_heads))
@@ -1523,6 +1524,7 @@ int32_t bicache_attend_layer(bicache_ctx* ctx, int32_t layer, int32_t R, const i
   std::vector<int64_t> r_off, f_off;
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative length or offset");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     if (layer < depth[i] && prefix_id[i] >= 0) {
       auto found = ctx->by_id.find(prefix_id[i]);
       if (found == ctx->by_id.end()) return fail(ctx, BICACHE_ERR_NOTFOUND, "unknown or evicted prefix id");
@@ -1582,6 +1584,7 @@ int32_t bicache_attend_step(bicache_ctx* ctx, int32_t layer, int32_t t, int32_t 
   std::unordered_map<int32_t, int> first_seen;
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative length or offset");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     int32_t pid = -1;
     if (layer < depth[i] && shared_id[i] >= 0) pid = shared_id[i];
     else if (private_id[i] >= 0 && !refresh) pid = private_id[i];

@@ -224,6 +224,7 @@ int prefix_weights_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_
   std::vector<std::pair<int64_t, int64_t>> blocks;               // score elements [begin, end) of every prefix
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0) return fail(ctx, BICACHE_ERR_INVALID, "negative length or offset");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     const int32_t p = prefix_id[i];
     if (p < -1) return fail(ctx, BICACHE_ERR_INVALID, "bad prefix id");
     if (p < 0) continue;

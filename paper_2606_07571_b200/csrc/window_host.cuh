@@ -80,6 +80,7 @@ int check_tokens(const bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0 || token_off[i] < 0)
       return fail(ctx, BICACHE_ERR_INVALID, "negative length or offset");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     auto found = ctx->by_id.find(prefix_id[i]);
     if (found == ctx->by_id.end()) return fail(ctx, BICACHE_ERR_NOTFOUND, "unknown or evicted prefix id");
     const PrefixEntry& e = *found->second;
@@ -573,6 +574,7 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   for (int i = 0; i < R; ++i) {
     if (seqlen[i] < 0 || row_off[i] < 0 || query_pos[i] < 0 || cached_len[i] < 0)
       return fail(ctx, BICACHE_ERR_INVALID, "negative length, offset or position");
+    if (row_off[i] > INT64_MAX - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "rows beyond 2^63");
     if (query_pos[i] > 0x7fffffff - seqlen[i]) return fail(ctx, BICACHE_ERR_INVALID, "positions beyond 2^31");
     total += seqlen[i];
     if (prefix_id[i] < -1) return fail(ctx, BICACHE_ERR_INVALID, "bad prefix id");
