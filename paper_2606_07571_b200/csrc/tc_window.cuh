@@ -397,8 +397,10 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
       ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
       if (ok) load_tile(j, p);
     }
-    // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-    if ((!ok || *abort_flag) && lane == 0) {
+    // No copy may land after the CTA has gone: wait (bounded) for the tiles requested last.  Always: another warp may give up
+    // after this one has issued them all, and an item with no more tiles than slots has waited for nothing so far.  If
+    // nobody gives up they have landed or are about to, and the end of the item takes longer.
+    if (lane == 0) {
       for (int b = 0; b < stages; ++b)
         if (armed[b] >= 0) {
           const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);

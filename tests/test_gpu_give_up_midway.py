@@ -1,0 +1,73 @@
+"""Wait budgets shorter than what the kernels wait for, but not the strictest one, which gives up before any work: a role may
+give up while the others still work and copies are under way.  (A wait asks the hardware first, which itself waits a
+while: waits of a few microseconds end before the budget counts, those for a whole item run out.)  Whatever happens the call
+ends with its copies landed: a call of another context, which follows at once and may be placed on the same SMs, has the
+right bits; the status says what happened; a call whose waits did not run out is right; and the context works
+again."""
+import pytest
+import torch
+
+import __graft_entry__ as entry
+from paper_2606_07571_b200 import binding
+
+pytestmark = pytest.mark.gpu
+BUDGETS = [1024, 1500, 2500, 4000, 7000, 12000, 20000, 40000]         # SM cycles
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    entry.build()
+    binding.load_library()
+
+
+def randn(shape, seed, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+
+def give_up(make, call):
+    """make(): a context and what its calls need; call(context, ...): the outputs of one call."""
+    (bc, *args), (other, *other_args) = make(), make()
+    want = call(bc, *args)
+    assert bc.device_status() == binding.OK
+    for a, b in zip(want, call(other, *other_args)):
+        assert torch.equal(a, b)
+    for budget in BUDGETS * 3:
+        bc.set_wait_budget(budget)
+        first = call(bc, *args)
+        after = call(other, *other_args)
+        status = bc.device_status(clear=True)
+        assert status in (binding.OK, binding.ERR_TIMEOUT) and other.device_status() == binding.OK
+        for a, b in zip(want, after):
+            assert torch.equal(a, b)
+        if status == binding.OK:
+            for a, b in zip(want, first):
+                assert torch.equal(a, b)
+    bc.set_wait_budget(0)
+    for a, b in zip(want, call(bc, *args)):
+        assert torch.equal(a, b)
+    assert bc.device_status() == binding.OK
+    bc.close()
+    other.close()
+
+
+# heads, cached tokens, rows, window, kernel: items of many tiles, ranges of keys and their join; items of no more tiles
+# than there are slots for
+WINDOWS = [(14, 2, 20000, 5, (4, 10000, 0), binding.KERNEL_KEY_RANGES), (32, 32, 700, 300, (4, 350, 0), binding.KERNEL_KEY_RANGES),
+           (28, 4, 1500, 1500, (0, 20, 0), binding.KERNEL_KEY_RANGES), (4, 4, 60, 40, (0, -1, -1), binding.KERNEL_KEY_RANGES)]
+
+
+@pytest.mark.parametrize("hq,hkv,m,n,window,kernel", WINDOWS)
+def test_windowed_attention(hq, hkv, m, n, window, kernel):
+    k, q = randn((1, m, hkv, 128), 1), randn((n, hq, 128), 2)
+
+    def make():
+        bc = binding.BiCache(1, hq, hkv, 128, (m + 15) // 16, torch.bfloat16, n, 1)
+        return bc, bc.put_prefix(1, k, k.flip(1))[0]
+
+    def call(bc, pid):
+        out, lse = torch.zeros_like(q), torch.zeros((n, hq), device="cuda")
+        bc.attend_window(0, [pid], [m], [m - n], [0], [n], q, out, lse, *window)
+        assert bc.last_attention_kernel() == kernel
+        return out, lse
+    give_up(make, call)
