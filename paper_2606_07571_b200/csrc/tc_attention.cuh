@@ -1253,8 +1253,9 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       ++n_it;
     }
     cp_async_wait<0>();
-    // After a give-up, the Q loads issued last may still be in flight: wait (bounded) for them.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
+    // No load may land after the CTA has gone: wait (bounded) for the Q tiles requested last.  Always: another warp may give up
+    // after this one has come here.
+    if (lane == 0) {
       for (int x = 0; x < 2; ++x)
         if (eq[x] > 0)
           for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->q_full[x]), (eq[x] - 1) & 1); ++it)
@@ -1392,9 +1393,9 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
     }
     cp_async_wait<0>();
     // On the normal path every tile loaded has been consumed by the time the CTA ends (the
-    // epilogue waits for the last MMA).  After a give-up, bulk copies may still be in flight:
-    // wait (bounded) for the last barriers this lane armed.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
+    // epilogue waits for the last MMA).  After a give-up, which may come after this warp has issued all its
+    // tiles, bulk copies may still be in flight: wait (bounded) for the last barriers this lane armed.
+    if (lane == 0) {
       for (int i = 0; i < kRing; ++i)
         if (armed[i] >= 0)
           for (unsigned it = 0;

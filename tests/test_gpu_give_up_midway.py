@@ -26,12 +26,13 @@ def randn(shape, seed, dtype=torch.bfloat16):
 
 
 def give_up(make, call):
-    """make(): a context and what its calls need; call(context, ...): the outputs of one call."""
+    """make(): a context and what its calls need; call(context, ...): the outputs of one call.  How many calls gave up."""
     (bc, *args), (other, *other_args) = make(), make()
     want = call(bc, *args)
     assert bc.device_status() == binding.OK
     for a, b in zip(want, call(other, *other_args)):
         assert torch.equal(a, b)
+    gave_up = 0
     for budget in BUDGETS * 3:
         bc.set_wait_budget(budget)
         first = call(bc, *args)
@@ -40,6 +41,7 @@ def give_up(make, call):
         assert status in (binding.OK, binding.ERR_TIMEOUT) and other.device_status() == binding.OK
         for a, b in zip(want, after):
             assert torch.equal(a, b)
+        gave_up += status != binding.OK
         if status == binding.OK:
             for a, b in zip(want, first):
                 assert torch.equal(a, b)
@@ -49,12 +51,14 @@ def give_up(make, call):
     assert bc.device_status() == binding.OK
     bc.close()
     other.close()
+    return gave_up
 
 
 # heads, cached tokens, rows, window, kernel: items of many tiles, ranges of keys and their join; items of no more tiles
 # than there are slots for
 WINDOWS = [(14, 2, 20000, 5, (4, 10000, 0), binding.KERNEL_KEY_RANGES), (32, 32, 700, 300, (4, 350, 0), binding.KERNEL_KEY_RANGES),
-           (28, 4, 1500, 1500, (0, 20, 0), binding.KERNEL_KEY_RANGES), (4, 4, 60, 40, (0, -1, -1), binding.KERNEL_KEY_RANGES)]
+           (28, 4, 1500, 1500, (0, 20, 0), binding.KERNEL_KEY_RANGES), (4, 4, 60, 40, (0, -1, -1), binding.KERNEL_KEY_RANGES),
+           (32, 32, 3500, 3500, (4, 1750, 0), binding.KERNEL_TENSOR), (8, 8, 15000, 15000, (0, -1, -1), binding.KERNEL_TENSOR)]
 
 
 @pytest.mark.parametrize("hq,hkv,m,n,window,kernel", WINDOWS)
@@ -70,4 +74,28 @@ def test_windowed_attention(hq, hkv, m, n, window, kernel):
         bc.attend_window(0, [pid], [m], [m - n], [0], [n], q, out, lse, *window)
         assert bc.last_attention_kernel() == kernel
         return out, lse
-    give_up(make, call)
+    assert give_up(make, call) or m < 10000 or kernel != binding.KERNEL_TENSOR       # items of 100 us: some waits run out
+
+
+@pytest.mark.parametrize("full", [False, True])
+@pytest.mark.parametrize("hq,hkv,m,lens", [(32, 8, 500, [700, 130, 256, 513, 64, 900]), (8, 8, 1200, [12000]), (14, 2, 300, [40, 7, 333])])
+def test_attention(hq, hkv, m, lens, full):
+    """Row tiles of one and of several requests; items that take long, and that are split."""
+    n = sum(lens)
+    off = [sum(lens[:i]) for i in range(len(lens))]
+    pk, q, k, v = randn((1, m, hkv, 128), 1), randn((n, hq, 128), 2), randn((n, hkv, 128), 3), randn((n, hkv, 128), 4)
+
+    def make():
+        bc = binding.BiCache(1, hq, hkv, 128, (m + 15) // 16, torch.bfloat16, n, len(lens))
+        bc.set_path(binding.PATH_TENSOR)
+        return bc, bc.put_prefix(1, pk, -pk)[0]
+
+    def call(bc, pid):
+        out, lse = torch.zeros_like(q), torch.zeros((n, hq), device="cuda")
+        if full:
+            bc.attend_full(0, off, lens, q, k, v, out, lse)
+        else:
+            bc.attend(0, [pid] * len(lens), off, lens, q, k, v, out, lse)
+        assert bc.last_attention_kernel() == binding.KERNEL_TENSOR
+        return out, lse
+    assert give_up(make, call) or lens != [12000]
