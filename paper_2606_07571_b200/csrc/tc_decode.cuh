@@ -404,8 +404,9 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
       }
     }
     cp_async_wait<0>();
-    // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
+    // No copy may land after the CTA has gone: wait (bounded) for the barriers armed last.  Always: another warp may give up
+    // after this one has issued all its tiles.
+    if (lane == 0) {
       for (int b = 0; b < stages; ++b)
         if (armed[b] >= 0) {
           const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);

@@ -99,3 +99,21 @@ def test_attention(hq, hkv, m, lens, full):
         assert bc.last_attention_kernel() == binding.KERNEL_TENSOR
         return out, lse
     assert give_up(make, call) or lens != [12000]
+
+
+@pytest.mark.parametrize("hq,hkv,m,lens", [(28, 4, 16384, [16]), (4, 4, 2000, [7, 12]), (32, 8, 5000, [1] * 30)])
+def test_few_rows_against_a_long_prefix(hq, hkv, m, lens):
+    n = sum(lens)
+    off = [sum(lens[:i]) for i in range(len(lens))]
+    pk, q, k, v = randn((1, m, hkv, 128), 1), randn((n, hq, 128), 2), randn((n, hkv, 128), 3), randn((n, hkv, 128), 4)
+
+    def make():
+        bc = binding.BiCache(1, hq, hkv, 128, (m + 15) // 16, torch.bfloat16, n, len(lens))
+        return bc, bc.put_prefix(1, pk, -pk)[0]
+
+    def call(bc, pid):
+        out, lse = torch.zeros_like(q), torch.zeros((n, hq), device="cuda")
+        bc.attend(0, [pid] * len(lens), off, lens, q, k, v, out, lse)
+        assert bc.last_attention_kernel() == binding.KERNEL_KEY_RANGES
+        return out, lse
+    give_up(make, call)
