@@ -411,8 +411,9 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sy->k_free[kt % kKSlots]), ((kt / kKSlots) & 1) ^ 1, abort_flag));
         if (ok) fetch();
       }
-      // After a give-up, bulk copies may still be in flight: wait (bounded) for the barriers armed last.
-      if ((!ok || *abort_flag) && lane == 0) {
+      // No copy may land after the CTA has gone: wait (bounded) for the barriers armed last.  Always: another warp may give
+      // up after this one has issued all its copies.
+      if (lane == 0) {
         for (int s = 0; s < kKSlots; ++s)
           if (armed[s] >= 0)
             for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->k_full[s]), (unsigned)armed[s]); ++n) __nanosleep(256);
@@ -575,8 +576,8 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       }
       cp_async_wait<0>();
       if (pending >= 0) announce();
-      // After a give-up, boxes may still be in flight: wait (bounded) for the barriers armed last.
-      if (!dead && (!ok || *abort_flag) && lane == 0) {
+      // The same for the boxes.
+      if (lane == 0) {
         for (int s = 0; s < kQSlots; ++s)
           if (boxed[s] >= 0)
             for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->q_full[s]), (unsigned)boxed[s]); ++n) __nanosleep(256);

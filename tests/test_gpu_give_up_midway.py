@@ -117,3 +117,22 @@ def test_few_rows_against_a_long_prefix(hq, hkv, m, lens):
         assert bc.last_attention_kernel() == binding.KERNEL_KEY_RANGES
         return out, lse
     give_up(make, call)
+
+
+@pytest.mark.parametrize("hq,hkv,m,lens", [(28, 4, 4000, [2048]), (4, 4, 300, [40, 7, 3000]), (14, 2, 16384, [16])])
+def test_accumulated_weights(hq, hkv, m, lens):
+    """Rows by boxes and gathered, items of many row tiles and of few."""
+    n = sum(lens) + len(lens)
+    off = [sum(lens[:i]) + i for i in range(len(lens))]          # a row between two requests
+    pk, q = randn((1, m, hkv, 128), 1), randn((n, hq, 128), 2)
+    lse = torch.full((n, hq), 5.0, device="cuda")
+
+    def make():
+        bc = binding.BiCache(1, hq, hkv, 128, (m + 15) // 16, torch.bfloat16, n, len(lens))
+        return bc, bc.put_prefix(1, pk, -pk)[0]
+
+    def call(bc, pid):
+        scores = torch.zeros((hkv, m), device="cuda")
+        bc.prefix_weights(0, [pid] * len(lens), off, lens, q, lse, scores, [0] * len(lens))
+        return scores,
+    give_up(make, call)
