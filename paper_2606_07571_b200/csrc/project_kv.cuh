@@ -60,6 +60,7 @@ struct Sync {
   int abort_flag;
   unsigned tmem_base;
   int dead;
+  int peer_gave_up;                      // written by the other CTA of the pair at its end
 };
 constexpr int kProjSmemBytes = 1024 + kStages * kProjStageBytes + kOutBytes + (int)sizeof(Sync);
 static_assert(kProjSmemBytes <= 232448, "shared memory of one CTA");
@@ -105,6 +106,17 @@ __device__ __forceinline__ void mbar_arrive_remote(unsigned local_bar, unsigned 
   unsigned raddr;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(raddr) : "r"(local_bar), "r"(rank));
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(raddr) : "memory");
+}
+// write the word at the same shared-memory offset in CTA `rank` of the cluster
+__device__ __forceinline__ void st_remote(unsigned local, unsigned rank, unsigned v) {
+  unsigned raddr;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(raddr) : "r"(local), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(raddr), "r"(v) : "memory");
+}
+// After a give-up: about a millisecond, by which every load that was under way has landed.
+__device__ __forceinline__ void wait_out_loads() {
+  const long long t0 = clock64();
+  while (clock64() - t0 < 2000000) __nanosleep(1000);
 }
 // The two-SM MMA, issued by one elected lane of a converged warp of the pair's first CTA.  The
 // descriptors name the same shared-memory offsets in both CTAs: CTA r supplies rows 128 r .. of A
@@ -201,6 +213,7 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
     sy->wait_cycles = wait_cycles;
     sy->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
     sy->abort_flag = (sy->dead || wait_cycles < kStrictBudget) ? 1 : 0;
+    sy->peer_gave_up = 0;
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_u32(&sy->full[i]), 1);
       mbar_init(smem_u32(&sy->empty[i]), 1);
@@ -254,20 +267,14 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
         }
       }
     }
-    // After a give-up, loads may still be in flight.  CTA 0 waits (bounded) for the barriers it
-    // armed last, which count the bytes of both CTAs.  CTA 1 cannot see those barriers: if it has
-    // issued loads it waits out the same limit before it joins the pair's last barrier.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
+    // No load may land after the CTAs have gone.  CTA 0 waits (bounded) for the barriers it armed last, which count the
+    // bytes of both; always, since another warp may give up after this one has issued all its loads.  What CTA 1 has
+    // loaded besides, after a give-up, the end of the kernel waits out.
+    if (rank == 0 && lane == 0) {
       for (int s = 0; s < kStages; ++s)
-        if (armed[s] >= 0) {
-          if (rank == 0) {
-            for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->full[s]), (armed[s] / kStages) & 1); ++n)
-              __nanosleep(256);
-          } else {
-            for (unsigned n = 0; n < 4096; ++n) __nanosleep(256);
-            break;
-          }
-        }
+        if (armed[s] >= 0)
+          for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->full[s]), (armed[s] / kStages) & 1); ++n)
+            __nanosleep(256);
     }
   } else if (warp == 1 && rank == 1) {
     // CTA 1's warp 1 only owns the pair's TMEM allocation with its counterpart
@@ -427,12 +434,19 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
     if (e < 8) bulk_wait_all();                              // this thread's page copies have completed
   }
 
-  // The pair leaves together: CTA 0's MMAs read CTA 1's shared memory and write its TMEM.
+  // The pair leaves together: CTA 0's MMAs read CTA 1's shared memory and write its TMEM.  If a role of either has given
+  // up (known once all of them are done), loads may be under way into either: then both stay until they have landed.
   tc_fence_before();
+  __syncthreads();
+  const bool gave_up = !dead && *abort_flag;
+  if (tid == 0) st_remote(smem_u32(&sy->peer_gave_up), rank ^ 1, gave_up ? 1u : 0u);
   cluster.sync();
   tc_fence_after();
   if (warp == 1) tmem_dealloc2(tmem, 512);
-  if (tid == 0 && !dead && *abort_flag) atomicCAS(status, kDevOk, kDevTimeout);
+  if (tid == 0) {
+    if (gave_up) atomicCAS(status, kDevOk, kDevTimeout);
+    if (gave_up || *reinterpret_cast<volatile int*>(&sy->peer_gave_up)) wait_out_loads();
+  }
 }
 
 // Sets the kernel's shared-memory limit and returns how many CTA pairs the device runs at once.

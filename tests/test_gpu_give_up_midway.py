@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import __graft_entry__ as entry
-from paper_2606_07571_b200 import binding
+from paper_2606_07571_b200 import binding, workloads
 
 pytestmark = pytest.mark.gpu
 BUDGETS = [1024, 1500, 2500, 4000, 7000, 12000, 20000, 40000]         # SM cycles
@@ -135,4 +135,23 @@ def test_accumulated_weights(hq, hkv, m, lens):
         scores = torch.zeros((hkv, m), device="cuda")
         bc.prefix_weights(0, [pid] * len(lens), off, lens, q, lse, scores, [0] * len(lens))
         return scores,
+    give_up(make, call)
+
+
+@pytest.mark.parametrize("hkv,m,d_model", [(4, 700, 512), (1, 256, 64), (8, 20000, 4096)])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_projection(hkv, m, d_model, rotated):
+    """CTAs in pairs: fewer K steps than stages, and many tiles to a pair."""
+    h, w_k, w_v = workloads.draw_hidden_and_weights(m, d_model, hkv, 128, 9, device="cuda")
+    table = torch.rand((m, 64, 2), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") if rotated else None
+
+    def make():
+        bc = binding.BiCache(1, hkv, hkv, 128, (m + 15) // 16, torch.bfloat16, 16, 1)
+        return bc, bc.reserve_prefix(1, m)[0]
+
+    def call(bc, pid):
+        bc.project_prefix_layer(pid, 0, h, w_k, w_v, table)
+        k, v = torch.zeros((m, hkv, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((m, hkv, 128), dtype=torch.bfloat16, device="cuda")
+        bc.read_prefix_layer(pid, 0, k, v)
+        return k, v
     give_up(make, call)
