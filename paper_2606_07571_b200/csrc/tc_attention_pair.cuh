@@ -29,9 +29,11 @@ namespace tcp {
 
 using namespace tc;
 using proj::mbar_arrive_remote;
+using proj::st_remote;
 using proj::tmem_alloc2;
 using proj::tmem_dealloc2;
 using proj::tmem_relinquish2;
+using proj::wait_out_loads;
 
 constexpr int kPairRows = 2 * kTileRows;         // query rows of one item of a pair
 constexpr int kHalfBytes = kTileBytes / 2;       // 16 KB: this CTA's half of a K or V tile
@@ -56,6 +58,7 @@ struct alignas(8) PairBarriers {
   int abort_flag;
   unsigned tmem_base;
   int dead;
+  int peer_gave_up;                      // written by the other CTA of the pair at its end
   ItemInfo info[2];
 };
 constexpr int kPairSmemBytes = 1024 + kTileBytes * 2 + kHalfBytes * kRing2 + kStageBytes + (int)sizeof(PairBarriers) + 64;
@@ -227,6 +230,7 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
     bars->wait_cycles = wait_cycles;
     bars->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
     bars->abort_flag = (bars->dead || wait_cycles < kStrictBudget) ? 1 : 0;
+    bars->peer_gave_up = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars->info_full[i]), 1);
       mbar_init(smem_u32(&bars->info_free[i]), rank == 0 ? kInfoReaders : kInfoReaders - 1);   // no MMA warp in CTA 1
@@ -624,17 +628,14 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
       __syncwarp();
       ++n_it;
     }
-    // After a give-up the Q loads issued last may still be in flight (they complete on the first CTA's
-    // barrier): the first CTA waits (bounded) for them, the second waits out the same limit.
-    if (!dead && (!ok || *abort_flag) && lane == 0) {
-      if (rank == 0) {
-        for (int x = 0; x < 2; ++x)
-          if (eq[x] > 0)
-            for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->q_full[x]), (eq[x] - 1) & 1); ++it)
-              __nanosleep(256);
-      } else if (eq[0] > 0) {
-        for (unsigned it = 0; it < 4096; ++it) __nanosleep(256);
-      }
+    // No load may land after the CTAs have gone.  The first CTA, on whose barriers the loads of both complete, waits
+    // (bounded) for the Q tiles requested last; always, since another warp may give up after this one has come here.
+    // What the second CTA has loaded besides, after a give-up, the end of the kernel waits out.
+    if (rank == 0 && lane == 0) {
+      for (int x = 0; x < 2; ++x)
+        if (eq[x] > 0)
+          for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->q_full[x]), (eq[x] - 1) & 1); ++it)
+            __nanosleep(256);
     }
   } else if (warp >= 10) {
     // ====================================== loads =======================================
@@ -644,7 +645,7 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
     const int is_v = warp - 10;
     bool ok = !dead;
     int n_it = 0, U = 0;
-    int last_armed = -1;
+    int last = -1;                           // the last use of the ring that this warp has issued
     while (ok) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->info_full[n_it & 1]), (n_it >> 1) & 1, abort_flag));
       if (!ok) break;
@@ -658,6 +659,7 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
         const int slot = u % kRing2;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->free_[slot]), ((u / kRing2) & 1) ^ 1, abort_flag));
         if (!ok) break;
+        last = u;
         const unsigned dst = ring_smem + slot * kHalfBytes;
         const unsigned full = smem_u32(&bars->full[slot]);
         const int key0 = j * kTileKeys, cnt = min(kTileKeys, g.n0 - key0);
@@ -674,7 +676,6 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
               tma_load_3d_pair(dst, &tm_v, 64 * (int)rank, kv_head, row, full);
             }
             if (rank != 0) mbar_arrive_remote(full, 0);
-            last_armed = u;
           }
           __syncwarp();
           continue;
@@ -720,14 +721,11 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
       ++n_it;
     }
     cp_async_wait<0>();
-    if (!dead && (!ok || *abort_flag) && lane == 0 && last_armed >= 0) {
-      if (rank == 0) {
-        for (unsigned it = 0;
-             it < 4096 && !mbar_try_wait(smem_u32(&bars->full[last_armed % kRing2]), (last_armed / kRing2) & 1); ++it)
+    // The same for the keys and values: the uses of the ring whose slots have not been issued again since.
+    if (rank == 0 && lane == 0) {
+      for (int u = last; u >= 0 && u > last - kRing2; u -= 2)
+        for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->full[u % kRing2]), (u / kRing2) & 1); ++it)
           __nanosleep(256);
-      } else {
-        for (unsigned it = 0; it < 4096; ++it) __nanosleep(256);
-      }
     }
   } else if (warp == kMmaWarp && rank == 0) {
     // ===================================== MMA issue =====================================
@@ -922,13 +920,19 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
     __syncwarp();
   }
 
-  // The pair leaves together: the first CTA's MMAs read the partner's shared memory and write its TMEM.
+  // The pair leaves together: the first CTA's MMAs read the partner's shared memory and write its TMEM.  If a role of
+  // either has given up (known once all of them are done), loads may be under way into either: then both stay until
+  // they have landed.
   tc_fence_before();
+  __syncthreads();
+  const bool gave_up = !dead && *abort_flag;
+  if (tid == 0) st_remote(smem_u32(&bars->peer_gave_up), rank ^ 1, gave_up ? 1u : 0u);
   cluster.sync();
   tc_fence_after();
   if (warp == kMmaWarp) tmem_dealloc2(tmem, kTmemCols);
   if (tid == 0) {
-    if (!dead && *abort_flag) atomicCAS(status, kDevOk, kDevTimeout);
+    if (gave_up) atomicCAS(status, kDevOk, kDevTimeout);
+    if (gave_up || *reinterpret_cast<volatile int*>(&bars->peer_gave_up)) wait_out_loads();
     __threadfence();
     if (atomicAdd(ctas_done, 1) == (int)gridDim.x - 1) {
       *next_item = 0;

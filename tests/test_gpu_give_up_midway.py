@@ -155,3 +155,22 @@ def test_projection(hkv, m, d_model, rotated):
         bc.read_prefix_layer(pid, 0, k, v)
         return k, v
     give_up(make, call)
+
+
+@pytest.mark.parametrize("hq,hkv,lens", [(4, 4, [300, 517]), (28, 4, [1000]), (8, 8, [12000])])
+def test_attention_on_pairs(hq, hkv, lens):
+    n = sum(lens)
+    off = [sum(lens[:i]) for i in range(len(lens))]
+    q, k, v = randn((n, hq, 128), 2), randn((n, hkv, 128), 3), randn((n, hkv, 128), 4)
+
+    def make():
+        bc = binding.BiCache(1, hq, hkv, 128, 4, torch.bfloat16, n, len(lens))
+        bc.set_path(binding.PATH_TENSOR_PAIRS)
+        return bc, None
+
+    def call(bc, _):
+        out, lse = torch.zeros_like(q), torch.zeros((n, hq), device="cuda")
+        bc.attend_full(0, off, lens, q, k, v, out, lse)
+        assert bc.last_attention_kernel() == binding.KERNEL_TENSOR_PAIRS
+        return out, lse
+    assert give_up(make, call) or lens != [12000]
