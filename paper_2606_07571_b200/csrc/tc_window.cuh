@@ -113,7 +113,8 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
     }
     __syncwarp();
     asm volatile("barrier.cta.arrive 1, 224;" ::: "memory");       // the others may use the barriers
-    begun = status_now == 0 && (q_smem & 1023u) == 0;
+    // (one lane's answer for the warp: another CTA may raise the status at any time, and load_tile is for all lanes)
+    begun = __shfl_sync(0xffffffffu, status_now, 0) == 0 && (q_smem & 1023u) == 0;
     if (begun)
       for (int j = 0; j < ahead; ++j) load_tile(j, find_tile(j));
     asm volatile("barrier.cta.sync 2, 96;" ::: "memory");          // the flags that warp 4 sets
