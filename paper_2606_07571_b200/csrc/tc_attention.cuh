@@ -1275,7 +1275,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
     for (int q = 0; q < 4; ++q) dst_q[q] = tile_chunk_offset(r0 + 2 * q, c16);
     bool ok = !dead;
     int n_it = 0, U = 0;
-    int armed[kRing] = {-1, -1, -1, -1};     // the last use armed with bulk copies, per slot
+    int armed[kRing] = {-1, -1, -1, -1};     // the last use, per slot
     while (ok) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->info_full[n_it & 1]), (n_it >> 1) & 1, abort_flag));
       if (!ok) break;
@@ -1384,6 +1384,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         cp_async_wait<0>();
         fence_proxy_async();
         mbar_arrive(full);
+        armed[slot] = u;                         // by nobody else: the waits at the end name each slot's last use
       }
       if (!ok) break;
       U += 2 * g.T;

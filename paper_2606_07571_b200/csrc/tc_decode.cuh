@@ -355,7 +355,7 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
     const int r0 = lane >> 4, c16 = lane & 15;
     bool ok = !dead;
     const int stages = is_v ? kVStages : kKStages;
-    int armed[kKStages] = {-1, -1, -1};      // the last tile armed with bulk copies, per stage
+    int armed[kKStages] = {-1, -1, -1};      // the last tile, per stage
     const unsigned ring = is_v ? v_ring : k_ring;
     for (int j = 0; j < T && ok; ++j) {
       const int b = j % stages;
@@ -401,6 +401,7 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
         cp_async_wait<0>();
         fence_proxy_async();
         mbar_arrive(full);
+        armed[b] = j;
       }
     }
     cp_async_wait<0>();

@@ -438,7 +438,7 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         head_in[i] = r - tok_in[i] * G;
       }
       unsigned qt = 0;
-      int boxed[kQSlots] = {-1, -1, -1};                      // the last phase armed with a box, per slot
+      int used[kQSlots] = {-1, -1, -1};                       // the phase of the last tile, per slot
       int pending = -1;                                       // slot whose copies have not been announced yet
       auto announce = [&]() {
         fence_proxy_async();
@@ -525,13 +525,13 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
         }
         ok = __all_sync(0xffffffffu, mbar_wait(q_free, free_parity, abort_flag));
         if (!ok) break;
+        used[slot] = (int)(((qt - 1) / kQSlots) & 1);
         const unsigned dst = q_ring + slot * kTileBytes;
         if (boxes) {
           // rows past the tile's last token come along (or as zeros, past the tensor): they add nothing
           if (lane == 0) {
             mbar_expect_tx(q_full, (unsigned)(T * G * 128));                // each warp fetches one half of the dims
             tma_load_3d(dst + w * 16384, &q_map, w * 64, box_head, box_first, q_full);
-            boxed[slot] = (int)(((qt - 1) / kQSlots) & 1);
           }
         } else {
 #pragma unroll
@@ -576,11 +576,11 @@ tc_weights_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ 
       }
       cp_async_wait<0>();
       if (pending >= 0) announce();
-      // The same for the boxes.
+      // The same for the rows, boxes and gathered ones.
       if (lane == 0) {
         for (int s = 0; s < kQSlots; ++s)
-          if (boxed[s] >= 0)
-            for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->q_full[s]), (unsigned)boxed[s]); ++n) __nanosleep(256);
+          if (used[s] >= 0)
+            for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->q_full[s]), (unsigned)used[s]); ++n) __nanosleep(256);
       }
     }
   }

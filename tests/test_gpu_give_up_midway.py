@@ -174,3 +174,42 @@ def test_attention_on_pairs(hq, hkv, lens):
         assert bc.last_attention_kernel() == binding.KERNEL_TENSOR_PAIRS
         return out, lse
     assert give_up(make, call) or lens != [12000]
+
+
+def test_no_wait_runs_out_in_ordinary_calls():
+    """The load warps' waits at the end of a block name the last use of every slot, whichever way its tile came (bulk copies,
+    boxes, gathered rows): calls of 10 to 200 us take no milliseconds, which a wait that cannot end would."""
+    hq, hkv, m = 28, 4, 2000
+    lens = [333, 1, 700, 16]
+    n, off = sum(lens), [0, 333, 334, 1034]
+    pk, q, k, v = randn((1, m, hkv, 128), 1), randn((n, hq, 128), 2), randn((n, hkv, 128), 3), randn((n, hkv, 128), 4)
+    bc = binding.BiCache(1, hq, hkv, 128, 126, torch.bfloat16, n, 4)
+    pid = bc.put_prefix(1, pk, -pk)[0]
+    out, lse, scores = torch.empty_like(q), torch.full((n, hq), 5.0, device="cuda"), torch.empty((hkv, m), device="cuda")
+    h, w_k, w_v = workloads.draw_hidden_and_weights(m, 512, hkv, 128, 9, device="cuda")
+    short = bc.reserve_prefix(2, 16)[0]
+
+    def paths(path, call):
+        def f():
+            bc.set_path(path)
+            call()
+            bc.set_path(binding.PATH_AUTO)
+        return f
+    for call in (lambda: bc.attend(0, [pid] * 4, off, lens, q, k, v, out), lambda: bc.attend(0, [-1, pid], [0, 333], [100, 1], q, k, v, out),
+                 lambda: bc.attend(0, [pid], [1034], [16], q, k, v, out), lambda: bc.attend_full(0, off, lens, q, k, v, out),
+                 paths(binding.PATH_TENSOR_PAIRS, lambda: bc.attend_full(0, off, lens, q, k, v, out)),
+                 lambda: bc.prefix_weights(0, [pid] * 4, off, lens, q, lse, scores, [0] * 4),
+                 lambda: bc.prefix_weights(0, [pid] * 2, [0, 900], [333, 77], q, lse, scores, [0] * 2),
+                 lambda: bc.attend_window(0, [pid] * 4, [m] * 4, [5, 1999, 800, 0], off, lens, q, out, None, 4, 100, 0),
+                 lambda: bc.project_prefix_layer(short, 0, h[:16], w_k, w_v)):
+        best = 1e9
+        for _ in range(12):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            start.record()
+            call()
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        assert best < 1.0, best
+    assert bc.device_status() == binding.OK
