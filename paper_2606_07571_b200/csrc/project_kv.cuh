@@ -242,9 +242,6 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
     // this CTA's 128 tokens of the H tile and its 128 rows of the W tile
     bool ok = !dead;
     int it = 0;                              // stage uses over the life of the CTA
-    int armed[kStages];
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) armed[i] = -1;
     for (int idx = pair; ok; idx += num_pairs) {
       const TileCoord c = tile_coord(idx, a);
       if (!c.valid) break;
@@ -263,18 +260,8 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
           tma_load_2d_pair(dst, &tm_h, kb * kBK, (c.mt * 2 + (int)rank) * kBM, full);
           tma_load_2d_pair(dst + kABytes, tm_w, kb * kBK, w_row, full);
           if (c.half < 0) tma_load_2d_pair(dst + kABytes + kBBytes / 2, tm_w, kb * kBK, w_row + 64, full);
-          armed[s] = it;
         }
       }
-    }
-    // No load may land after the CTAs have gone.  CTA 0 waits (bounded) for the barriers it armed last, which count the
-    // bytes of both; always, since another warp may give up after this one has issued all its loads.  What CTA 1 has
-    // loaded besides, after a give-up, the end of the kernel waits out.
-    if (rank == 0 && lane == 0) {
-      for (int s = 0; s < kStages; ++s)
-        if (armed[s] >= 0)
-          for (unsigned n = 0; n < 4096 && !mbar_try_wait(smem_u32(&sy->full[s]), (armed[s] / kStages) & 1); ++n)
-            __nanosleep(256);
     }
   } else if (warp == 1 && rank == 1) {
     // CTA 1's warp 1 only owns the pair's TMEM allocation with its counterpart
@@ -435,7 +422,8 @@ project_kv_kernel(proj::ProjArgs a, int* status, const __grid_constant__ CUtenso
   }
 
   // The pair leaves together: CTA 0's MMAs read CTA 1's shared memory and write its TMEM.  If a role of either has given
-  // up (known once all of them are done), loads may be under way into either: then both stay until they have landed.
+  // up (known once all of them are done), loads may be under way into either: then both stay until they have landed.  (A
+  // loader that always waits for its last loads, as in the kernels of one CTA, cost 0.9 of 26 us at 300 tokens, d_model 4096.)
   tc_fence_before();
   __syncthreads();
   const bool gave_up = !dead && *abort_flag;

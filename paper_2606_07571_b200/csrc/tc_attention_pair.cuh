@@ -628,15 +628,6 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
       __syncwarp();
       ++n_it;
     }
-    // No load may land after the CTAs have gone.  The first CTA, on whose barriers the loads of both complete, waits
-    // (bounded) for the Q tiles requested last; always, since another warp may give up after this one has come here.
-    // What the second CTA has loaded besides, after a give-up, the end of the kernel waits out.
-    if (rank == 0 && lane == 0) {
-      for (int x = 0; x < 2; ++x)
-        if (eq[x] > 0)
-          for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->q_full[x]), (eq[x] - 1) & 1); ++it)
-            __nanosleep(256);
-    }
   } else if (warp >= 10) {
     // ====================================== loads =======================================
     // Warp 10 stages this CTA's half of every K tile (the rows of keys 64 r .. 64 r + 63), warp 11 its
@@ -645,7 +636,6 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
     const int is_v = warp - 10;
     bool ok = !dead;
     int n_it = 0, U = 0;
-    int last = -1;                           // the last use of the ring that this warp has issued
     while (ok) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->info_full[n_it & 1]), (n_it >> 1) & 1, abort_flag));
       if (!ok) break;
@@ -659,7 +649,6 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
         const int slot = u % kRing2;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->free_[slot]), ((u / kRing2) & 1) ^ 1, abort_flag));
         if (!ok) break;
-        last = u;
         const unsigned dst = ring_smem + slot * kHalfBytes;
         const unsigned full = smem_u32(&bars->full[slot]);
         const int key0 = j * kTileKeys, cnt = min(kTileKeys, g.n0 - key0);
@@ -721,12 +710,6 @@ tc_attention_pair_kernel(ScheduleView s, TensorArgs t, int* status, const __grid
       ++n_it;
     }
     cp_async_wait<0>();
-    // The same for the keys and values: the uses of the ring whose slots have not been issued again since.
-    if (rank == 0 && lane == 0) {
-      for (int u = last; u >= 0 && u > last - kRing2; u -= 2)
-        for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->full[u % kRing2]), (u / kRing2) & 1); ++it)
-          __nanosleep(256);
-    }
   } else if (warp == kMmaWarp && rank == 0) {
     // ===================================== MMA issue =====================================
     // The issue order of the one-CTA kernel, every MMA for tile X of both CTAs at once:
