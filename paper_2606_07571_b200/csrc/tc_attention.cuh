@@ -101,6 +101,8 @@ struct alignas(8) Barriers {
   int abort_flag;
   unsigned tmem_base;
   int dead;                              // the context's status word was already set when the CTA started
+  int q_loads[2];                        // at the end: loads of each query tile
+  int last_use[kRing];                   // of the ring, per slot; -1: none
   ItemInfo info[2];
   WindowInfo window[2];
 };
@@ -672,6 +674,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
     bars->wait_cycles = wait_cycles;
     bars->dead = (*reinterpret_cast<volatile int*>(status) != 0) ? 1 : 0;
     bars->abort_flag = (bars->dead || wait_cycles < kStrictBudget) ? 1 : 0;
+    for (int i = 0; i < kRing; ++i) bars->last_use[i] = -1;
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars->info_full[i]), 1);
       mbar_init(smem_u32(&bars->info_free[i]), kInfoReaders);
@@ -1253,14 +1256,8 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       ++n_it;
     }
     cp_async_wait<0>();
-    // No load may land after the CTA has gone: wait (bounded) for the Q tiles requested last.  Always: another warp may give up
-    // after this one has come here.
-    if (lane == 0) {
-      for (int x = 0; x < 2; ++x)
-        if (eq[x] > 0)
-          for (unsigned it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bars->q_full[x]), (eq[x] - 1) & 1); ++it)
-            __nanosleep(256);
-    }
+    if (lane == 0)
+      for (int x = 0; x < 2; ++x) bars->q_loads[x] = eq[x];
   } else if (warp >= 10) {
     // ====================================== loads =======================================
     // Warp 10 stages the K tiles, warp 11 the V tiles, each running ahead of the MMAs by the depth
@@ -1275,7 +1272,6 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
     for (int q = 0; q < 4; ++q) dst_q[q] = tile_chunk_offset(r0 + 2 * q, c16);
     bool ok = !dead;
     int n_it = 0, U = 0;
-    int armed[kRing] = {-1, -1, -1, -1};     // the last use, per slot
     while (ok) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->info_full[n_it & 1]), (n_it >> 1) & 1, abort_flag));
       if (!ok) break;
@@ -1317,7 +1313,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
           if (lane == 0) {
             mbar_arrive_expect_tx(full, bytes);
-            armed[slot] = u;
+            bars->last_use[slot] = u;
           } else {
             mbar_arrive(full);
           }
@@ -1347,7 +1343,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
           // every lane arrives, so the phase cannot complete before lane 0 has announced the bytes
           if (lane == 0) {
             mbar_arrive_expect_tx(full, (unsigned)(npages * kPageBytes));
-            armed[slot] = u;
+            bars->last_use[slot] = u;
           } else {
             mbar_arrive(full);
           }
@@ -1364,7 +1360,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             mbar_arrive_expect_tx(full, (unsigned)kTileBytes);
             tma_load_3d(dst, tm, 0, kv_head, row, full);
             tma_load_3d(dst + kTileBytes / 2, tm, 64, kv_head, row, full);
-            armed[slot] = u;
+            bars->last_use[slot] = u;
           } else {
             mbar_arrive(full);
           }
@@ -1384,7 +1380,7 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
         cp_async_wait<0>();
         fence_proxy_async();
         mbar_arrive(full);
-        armed[slot] = u;                         // by nobody else: the waits at the end name each slot's last use
+        if (lane == 0) bars->last_use[slot] = u;
       }
       if (!ok) break;
       U += 2 * g.T;
@@ -1393,16 +1389,6 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
       ++n_it;
     }
     cp_async_wait<0>();
-    // On the normal path every tile loaded has been consumed by the time the CTA ends (the
-    // epilogue waits for the last MMA).  After a give-up, which may come after this warp has issued all its
-    // tiles, bulk copies may still be in flight: wait (bounded) for the last barriers this lane armed.
-    if (lane == 0) {
-      for (int i = 0; i < kRing; ++i)
-        if (armed[i] >= 0)
-          for (unsigned it = 0;
-               it < 4096 && !mbar_try_wait(smem_u32(&bars->full[armed[i] % kRing]), (armed[i] / kRing) & 1); ++it)
-            __nanosleep(256);
-    }
   } else if (warp == kMmaWarp) {
     // ===================================== MMA issue =====================================
     // The whole warp runs this control flow converged and one elected lane issues each batch of
@@ -1658,6 +1644,18 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
   }
 
   __syncthreads();
+  // No load may land after the CTA has gone.  Without a give-up every tile has been used (the epilogue waits for the last
+  // MMA); after one, which is known now that all roles are done, wait (bounded) for what was requested last.  (What that
+  // was stands in shared memory: kept in registers up to here it made the roles spill.)
+  if (warp == 9 && lane == 0 && !dead && *abort_flag) {
+    auto landed = [](unsigned bar, int phase) {
+      for (unsigned n = 0; n < 4096 && !mbar_try_wait(bar, phase & 1); ++n) __nanosleep(256);
+    };
+    for (int x = 0; x < 2; ++x)
+      if (bars->q_loads[x] > 0) landed(smem_u32(&bars->q_full[x]), bars->q_loads[x] - 1);
+    for (int i = 0; i < kRing; ++i)
+      if (bars->last_use[i] >= 0) landed(smem_u32(&bars->full[i]), bars->last_use[i] / kRing);
+  }
   if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);

@@ -128,6 +128,10 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&sy->tmem_base);
   const bool dead = *reinterpret_cast<volatile int*>(&sy->dead) != 0;
   const unsigned tmem_o = tmem + 128;
+  // load warps (5: K tiles, 6: V tiles)
+  const int is_v = warp - 5;
+  const int stages = is_v ? kVStages : kKStages;
+  int armed[kKStages] = {-1, -1, -1};        // the last tile, per stage
 
   if (warp < 4) {
     // ================================ softmax and epilogue =================================
@@ -351,11 +355,8 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
   } else {
     // ======================================= loads ========================================
     // Warp 5 stages the K tiles, warp 6 the V tiles.
-    const int is_v = warp - 5;
     const int r0 = lane >> 4, c16 = lane & 15;
     bool ok = !dead;
-    const int stages = is_v ? kVStages : kKStages;
-    int armed[kKStages] = {-1, -1, -1};      // the last tile, per stage
     const unsigned ring = is_v ? v_ring : k_ring;
     for (int j = 0; j < T && ok; ++j) {
       const int b = j % stages;
@@ -405,18 +406,18 @@ tc_decode_kernel(const dec::DecodeItem* __restrict__ items, const long long* __r
       }
     }
     cp_async_wait<0>();
-    // No copy may land after the CTA has gone: wait (bounded) for the barriers armed last.  Always: another warp may give up
-    // after this one has issued all its tiles.
-    if (lane == 0) {
-      for (int b = 0; b < stages; ++b)
-        if (armed[b] >= 0) {
-          const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
-          for (unsigned n = 0; n < 4096 && !mbar_try_wait(full, (armed[b] / stages) & 1); ++n) __nanosleep(256);
-        }
-    }
   }
 
   __syncthreads();
+  // No copy may land after the CTA has gone.  Without a give-up all tiles have been used; after one, which is known now that
+  // all roles are done, the load warps wait (bounded) for the last tile of every stage.
+  if (warp >= 5 && lane == 0 && *abort_flag) {
+    for (int b = 0; b < stages; ++b)
+      if (armed[b] >= 0) {
+        const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
+        for (unsigned n = 0; n < 4096 && !mbar_try_wait(full, (armed[b] / stages) & 1); ++n) __nanosleep(256);
+      }
+  }
   if (warp == 4) {
     tc_fence_after();
     tmem_dealloc(tmem, kDecTmemCols);

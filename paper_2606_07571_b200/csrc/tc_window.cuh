@@ -398,19 +398,18 @@ tc_window_kernel(const __grid_constant__ WindowArgs a, int* status, long long wa
       ok = __all_sync(0xffffffffu, mbar_wait(free_bar, ((j / stages) & 1) ^ 1, abort_flag));
       if (ok) load_tile(j, p);
     }
-    // No copy may land after the CTA has gone: wait (bounded) for the tiles requested last.  Always: another warp may give up
-    // after this one has issued them all, and an item with no more tiles than slots has waited for nothing so far.  If
-    // nobody gives up they have landed or are about to, and the end of the item takes longer.
-    if (lane == 0) {
-      for (int b = 0; b < stages; ++b)
-        if (armed[b] >= 0) {
-          const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
-          for (unsigned n = 0; n < 4096 && !mbar_try_wait(full, (armed[b] / stages) & 1); ++n) __nanosleep(256);
-        }
-    }
   }
 
   __syncthreads();
+  // No copy may land after the CTA has gone.  Without a give-up all tiles have been used; after one, which is known now that
+  // all roles are done, the load warps wait (bounded) for the tiles that they requested last.
+  if (warp >= 5 && lane == 0 && *abort_flag) {
+    for (int b = 0; b < stages; ++b)
+      if (armed[b] >= 0) {
+        const unsigned full = smem_u32(is_v ? &sy->v_full[b] : &sy->k_full[b]);
+        for (unsigned n = 0; n < 4096 && !mbar_try_wait(full, (armed[b] / stages) & 1); ++n) __nanosleep(256);
+      }
+  }
   if (warp == 4) {
     tc_fence_after();
     tmem_dealloc(tmem, kDecTmemCols);
