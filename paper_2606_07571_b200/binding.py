@@ -232,8 +232,10 @@ def _host_list(a, code):
     """_host for the calls that take an entry per request, as (bytes, length): packing converts a list in two thirds of
     the time, a short one in half."""
     if isinstance(a, np.ndarray):
-        a = np.ascontiguousarray(a, dtype=_TYPE_CODES[code])
-        return a.tobytes(), a.size
+        b = np.ascontiguousarray(a, dtype=_TYPE_CODES[code])
+        if b.dtype != a.dtype and not (b == a).all():
+            raise OverflowError("an entry is no whole number of %d bytes" % b.itemsize)
+        return b.tobytes(), b.size
     n = len(a)
     return (_PACK[n, code](*a) if n <= 64 else struct.pack("%d%s" % (n, code), *a)), n
 
