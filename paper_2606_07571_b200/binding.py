@@ -243,12 +243,14 @@ def _host_list(a, code):
 def _rows_within(row_off, seqlen, off, n, rows):
     """Does no run of rows end past `rows`?  off, n: row_off and seqlen as _host_list packs them.  An empty request has
     no rows, wherever it says that they begin."""
-    if len(n) > 32:
+    if len(n) > 32 or isinstance(row_off, np.ndarray) or isinstance(seqlen, np.ndarray):
+        if not n:
+            return True
         lengths = np.frombuffer(n, np.int32)
         ends = np.frombuffer(off, np.int64) + lengths
         return int(ends.max()) <= rows or int(ends[lengths > 0].max(initial=0)) <= rows
     for o, k in zip(row_off, seqlen):
-        if o + k > rows and k > 0:
+        if o > rows - k and k > 0:                                 # (a sum of NumPy's numbers may wrap around)
             return False
     return True
 

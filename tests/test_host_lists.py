@@ -31,3 +31,23 @@ def test_fractions():
     for a in ([1.5], np.array([1.5])):
         with pytest.raises((struct.error, OverflowError)):
             b._host_list(a, "i")
+
+
+@pytest.mark.parametrize("count", [1, 8, 9, 100])              # by a loop, by arrays
+@pytest.mark.parametrize("dtype", [np.int32, np.int64, list])
+def test_rows_past_the_tensor(count, dtype):
+    def within(off, n, rows):
+        off, n = [0] * (count - 1) + [off], [5] * (count - 1) + [n]
+        if dtype is not list:
+            off, n = np.array(off, dtype=dtype), np.array(n, dtype=dtype)
+        return b._rows_within(off, n, b._host_list(off, "q")[0], b._host_list(n, "i")[0], rows)
+    assert within(20, 10, 30) and not within(21, 10, 30) and not within(20, 11, 30)
+    assert not within(2 ** 31 - 5, 10, 30) and not within(2 ** 31 - 1, 2 ** 31 - 1, 30)
+    assert not within(2 ** 31 - 5, 10, 2 ** 31) and within(2 ** 31 - 5, 10, 2 ** 31 + 5)
+
+
+def test_rows_in_lists_of_numpy_numbers():
+    off, n = [np.int32(2 ** 31 - 5), np.int32(0)], [np.int32(10), np.int32(0)]
+    assert not b._rows_within(off, n, b._host_list(off, "q")[0], b._host_list(n, "i")[0], 30)
+    none = np.empty(0, dtype=np.int32)
+    assert b._rows_within(none, none, b"", b"", 0)
