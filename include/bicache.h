@@ -473,7 +473,12 @@ int32_t bicache_rope_axes_table(bicache_ctx* ctx, int64_t rows, const bicache_ro
  * (bicache_reserve_prefix*) and fills up: new tokens are written behind the ones it holds
  * (bicache_append_tokens), rows attend over the tokens it holds so far (bicache_attend_window).  Like the calls above they
  * upload nothing and can be captured into a CUDA graph without a run before it; the graph holds page lists, lengths and
- * offsets.  They run on the context's device whichever device is current. */
+ * offsets.  They run on the context's device whichever device is current.
+ * A growing prefix is evicted like any other: the store is first-in-first-out, and putting or reserving another prefix for
+ * which there are not enough free pages takes the oldest ones, also while they are decoded; the next call on them answers
+ * NOTFOUND.  Reserve no more than the pools hold beside the prefixes in use.
+ * A request of length 0 has no rows: its row offset is not looked at (it must not be negative).  A last row whose number does
+ * not fit 63 bits is INVALID. */
 
 /* Keys and values of a ragged batch into one layer of live prefixes: row row_off[i] + a of k and v becomes token
  * token_off[i] + a of prefix prefix_id[i], for a < seqlen[i] (0: nothing).  Host metadata arrays of length R.  A token that is
@@ -538,8 +543,8 @@ int32_t bicache_attend_window(bicache_ctx* ctx, int32_t layer, int32_t R, const 
 int32_t bicache_device_status(bicache_ctx* ctx, void* stream, int32_t clear);
 
 /* Budget, in SM clock cycles, of every device-side wait of the tensor-core kernel (on a barrier that a
- * copy, an MMA or another warp completes).  A wait that exceeds it gives up: the CTA drains its copies
- * and MMAs, releases its tensor memory and exits, and bicache_device_status reports TIMEOUT; outputs of
+ * copy, an MMA or another warp completes).  A wait that exceeds it gives up: the CTA lets its copies and MMAs
+ * end, whichever of its warps gave up and when, releases its tensor memory and exits, and bicache_device_status reports TIMEOUT; outputs of
  * that call are then undefined, the context stays usable once the status is cleared.  0 restores the
  * default (about 0.2 s).  A tiny budget makes ordinary waits run out: that is how the tests exercise
  * the give-up path without any barrier that could never complete.  INVALID for a negative value. */

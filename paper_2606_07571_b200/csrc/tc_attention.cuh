@@ -639,8 +639,9 @@ __device__ __forceinline__ unsigned low_bits(int x) { return x >= 32 ? ~0u : x <
 // kWindowed: bicache_attend_window, whose batch travels in the parameters (`win`).  Its items read cached tokens alone: the
 // pages of an item's sequence take the place of a prefix's, a row knows the columns it sees as an interval and a number
 // of first columns, and a tile that some row of a warp does not see in full is masked by bits.  16,384 rows of 32 heads under
-// a window of 4096 with 4 first tokens take 890 to 980 us (1084 to 990 TFLOP/s of what is visible, the edges of the window
-// cost 7 % more; the clock follows the power), 1165 TFLOP/s where all rows see all keys.
+// a window of 4096 with 4 first tokens take 863 us in runs of three calls and 1000 in runs of forty, where the clock follows
+// the power limit (1115 and 962 TFLOP/s of what is visible; the edges of the window cost 7 % more); where all rows see all
+// keys, 1343 and 1172 TFLOP/s.
 enum { kPlain = 0, kShared = 1, kWindowed = 2 };
 struct NoWindow {};
 template <int kWords>
@@ -814,7 +815,9 @@ tc_attention_kernel(ScheduleView s, PoolView pool, TensorArgs t, int* status,
             mx2 = max3(mx2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
             mx3 = max3(mx3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
           }
-          m_ref = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * sl2;   // scale > 0; finite: a tile has a key
+          m_ref = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * sl2;   // scale > 0
+          // Finite, since a tile has a key; but under a window a row may see no key of the item's first tile: then it is
+          // -inf, for which the choice of neg_m_eff and of neg_m below and the epilogue's test of l_sum are there.
         }
         {
           // The exponentials use the reference maximum of

@@ -220,7 +220,9 @@ __device__ __forceinline__ long long window_part(const WindowArgs& a, const Wind
 // are computed, the next tile's keys during the rest.
 // Bound by instructions and their latency: 4500 to a warp and tile, less than half of them products, 12 warps to an SM.
 // 10,334 causal fp32 rows of 4 heads of 64 dims take 1555 us (35 TFLOP/s; 256 threads with 4 rows each took 3390, products of
-// the output by single rows 1670), three requests of up to 1000 rows under a window of 700 78 us.
+// the output by single rows 1670), three requests of up to 1000 rows under a window of 700 78 us.  bf16
+// with 64 dims, 32 query heads over 8: 4096 causal rows 1783 us (39 TFLOP/s; 165 us with 128 dims on the tensor cores), one
+// token over 16,384 keys 37 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWinThreads = 128;
 constexpr int kWinKeys = 64;

@@ -640,10 +640,16 @@ int attend_window_impl(bicache_ctx* ctx, int32_t layer, int32_t R, const int32_t
   if (ctx->tensor_ok && ctx->path != BICACHE_PATH_SIMT && softmax_scale > 0.f) {
     // Requests with more than 128 packed rows go through the kernel with row tiles of 256, which shares every key tile
     // between two tiles of 128 rows, if there are three of them to an SM and the query heads of a KV head divide 128 (else
-    // one warp gathers the query tiles, and short items wait for it); it does not split the keys.  Both sides measured: 32
-    // query heads, 16,384 rows, window of 4096: 865 us, as tiles of 128 rows 920; window of 1024: 407 and 425; 8 KV heads,
-    // 4096 rows, window of 1024 (512 items): 111 and 115.  28 query heads, window of 500 + 201: 224 items 71 us against 57, 550
-    // items 115 against 102.
+    // one warp gathers the query tiles, and short items wait for it); it does not split the keys.  Both sides, 256 first, in
+    // turn in one process, runs of 3 calls / of 40, where long ones meet the power limit; us:
+    //   32 heads, 16,384 rows: all keys 3276, 3609 / 3752, 4086; window 4096 844, 884 / 893, 893, with 4 first tokens 863, 897
+    //   / 1000, 998; window 1024 327, 324 / 315, 319.  8 KV heads, 16,384 rows, window 4096: 784, 847 / 920, 946.
+    //   few tiles, 32 heads over 8192 keys: 3.0 tiles to an SM, all keys 366, 368 / 356, 361, window 2048 168, 153 / 161, 146,
+    //   window 512 81, 68 / 77, 65; 1.1 to an SM, all keys 240, 143 / 235, 138.
+    //   28 heads over 4: 16,384 rows, window 4096 737, 737 / 864, 801, window 1024 305, 267 / 296, 255; five ragged requests,
+    //   window 500 + 201 94, 80 / 90, 76.
+    // So it pays for long windows; calls with three to five tiles to an SM under a window of 2048 or less would be 10 to
+    // 20 % faster in the other form.
     long long tiles = 0, rows_total = 0;
     for (int i = 0; i < R; ++i) {
       if (seqlen[i] > 0) rows_total = std::max<long long>(rows_total, row_off[i] + seqlen[i]);     // an empty one's row says nothing
